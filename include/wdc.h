@@ -490,6 +490,111 @@ wdc_status wdc_op_gemm(wdc_ctx* ctx, const void* A, const void* W, const float* 
 wdc_status wdc_op_attention(wdc_ctx* ctx, const void* q, const void* k, const void* vt, void* o,
                             int heads, int L, int d, wdc_stream stream);
 
+/* ------------------------------------------------------------------ chunk operators
+ * A model rolled out chunk by chunk: the projections of a chunk's tokens in
+ * 8-bit floating point, the norms and rotations of its heads, and its attention
+ * over a paged cache of the tokens before it (the paper's models attend densely
+ * over one clip; these stand beside wdc_op_gemm and wdc_op_attention).  All are
+ * asynchronous on `stream`, need a context with a denoiser (layers > 0: it gives
+ * the model dtype), check their arguments before any launch (pointers 16-byte
+ * aligned unless said) and may be captured into a graph.  A call with no rows
+ * (M == 0, T == 0 or no sequences) returns WDC_OK and launches nothing.  What
+ * only the device knows (page numbers, lengths, starts, positions) cannot be
+ * refused: a value out of range sets bit 2 (wdc_device_errors), and nothing is
+ * read or written outside the arrays given here. */
+
+/* q = e4m3(x / s) with a scale for each block of 128 columns of one row
+ * (block_rows 1) or of 128 rows (block_rows 128): s = max |x| / 448 over the
+ * block, so the block's largest magnitude becomes 448, and a row of M or K that
+ * 128 does not divide ends in a narrower block.  x [M, K] in the model dtype,
+ * row stride ldx >= K elements; q [M, K] e4m3, contiguous; scale fp32
+ * [ceil(K/128)][M] (block_rows 1: one block column's scales side by side, as
+ * wdc_op_gemm_fp8 reads them) or [ceil(M/128)][ceil(K/128)] (block_rows 128,
+ * for weights).  Division and rounding (to nearest even) are IEEE's; a block of
+ * zeros has scale 0; an infinity makes its block's scale infinite (finite
+ * values there become 0, infinities NaN), a NaN makes scale and block NaN.
+ * K % 16 == 0, ldx % 8 == 0 (WDC_ERR_UNSUPPORTED otherwise). */
+wdc_status wdc_op_quantize_fp8(wdc_ctx* ctx, const void* x, long long ldx, void* q, float* scale, int M, int K,
+                               int block_rows, wdc_stream stream);
+
+/* C = epilogue(A W^T) of e4m3 matrices with block scales: A [M, K] with
+ * a_scale [ceil(K/128)][M], W [N, K] with w_scale [ceil(N/128)][ceil(K/128)]
+ * (wdc_op_quantize_fp8's layouts), any fp32 scales:
+ *   sum over blocks b of a_scale[b][m] w_scale[n/128][b] sum_{k in b} A[m,k] W[n,k].
+ * A block's 128 products are summed by the tensor core, the scaled block sums
+ * in fp32.  bias, gelu, res, gate and C as in wdc_op_gemm (C and res [M, N] in
+ * the model dtype, res may equal C).  N % 8 == 0 and K % 16 == 0
+ * (WDC_ERR_UNSUPPORTED otherwise). */
+wdc_status wdc_op_gemm_fp8(wdc_ctx* ctx, const void* A, const float* a_scale, const void* W, const float* w_scale,
+                           const float* bias, void* C, int M, int N, int K, int gelu, const void* res,
+                           const float* gate, wdc_stream stream);
+
+/* A paged cache of keys and values: sequence b's token p lies in row p % page
+ * of page table[b][p / page].  bf16 models only. */
+typedef struct wdc_paged_cache {
+    void* k;                    /* device bf16 [pages][kv_heads][page][head_dim]  */
+    void* v;                    /* device fp16, the same shape (fp16: see wdc_op_attention) */
+    const int* table;           /* device [sequences][table_width] page numbers (4-byte aligned) */
+    const int* length;          /* device [sequences]: tokens of each sequence, those of the
+                                   present chunk included (4-byte aligned) */
+    int pages, page;            /* pages of the pool; tokens a page: 16, 32, 64, 128 or 256 */
+    int kv_heads, head_dim;     /* head_dim 64 or 128 */
+    int sequences, table_width;
+} wdc_paged_cache;
+
+/* What is done to the heads of a chunk's QKV rows: each query and key head is
+ * normalised to y = x / sqrt(mean(x^2) + eps) * weight and its first rot_dim
+ * elements are turned by the angles of the token's position p: of each pair
+ * (a, b), a' = a cos - b sin and b' = b cos + a sin.  Statistics, weights and
+ * angles in fp32, one rounding to the model dtype. */
+typedef struct wdc_head_norm {
+    const float* q_weight;      /* device [head_dim], or NULL (= 1)               */
+    const float* k_weight;
+    float eps;                  /* >= 0                                           */
+    const float* rot;           /* device [rot_positions][rot_dim / 2][cos, sin], or NULL: no rotation */
+    int rot_positions, rot_dim; /* rot_dim a multiple of 16, at most head_dim     */
+    int interleaved;            /* 1: pairs (2 i, 2 i + 1); 0: pairs (i, i + rot_dim / 2) */
+    const int* positions;       /* device [T] (4-byte aligned), or NULL: the token's place in its
+                                   sequence.  A position outside the table sets bit 2, and the
+                                   nearest one of the table is used */
+} wdc_head_norm;
+
+/* Norm and rotation of T rows qkv [T][(heads + 2 kv_heads) * d] (model dtype,
+ * row stride ld elements, ld % 8 == 0: query heads, key heads, value heads) into
+ * wdc_op_attention's operands: q [heads, T, d], k [kv_heads, T, d] and, unless
+ * vt is NULL, V^T [kv_heads, d, ldv] (fp16 for a bf16 model, beyond whose range
+ * values are saturated and set bit 8; ldv as there, its padding columns are left
+ * as they are).  d 64 or 128. */
+wdc_status wdc_op_qk_norm_rope(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
+                               const wdc_head_norm* norm, void* q, void* k, void* vt, wdc_stream stream);
+/* The same for a chunk of new tokens of the cache's sequences: rows
+ * q_start[b] .. q_start[b + 1] - 1 are the last tokens of sequence b (q_start
+ * device [sequences + 1], non-decreasing, 4-byte aligned).  Writes q [T, heads, d]
+ * and appends keys and values to their pages (values fp16, saturated as above).
+ * Rows from q_start[sequences] on are not read and their q is left as it is.
+ * The pages that a chunk is appended to belong to one sequence each. */
+wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads,
+                                      const wdc_head_norm* norm, const wdc_paged_cache* cache, const int* q_start,
+                                      void* q, wdc_stream stream);
+
+/* Attention of a chunk of new tokens over the cache, which already holds their
+ * own keys and values: o = softmax(q K^T / sqrt(d)) V for rows q_start[b] ..
+ * q_start[b + 1] - 1 of q and o ([T, heads, d] and [T, heads * d], bf16; heads a
+ * multiple of kv_heads, at most 128 of them to a key head), the last tokens of
+ * sequence b.  max_new: no sequence has more new tokens (rows beyond set bit 2
+ * and are left as they are).  The token at place p of a sequence of length L sees
+ *   frame == 0: all L tokens;   frame == 1: tokens 0 .. p;
+ *   frame >= 2: its frame and those before it, tokens 0 .. min(L, (p / frame + 1) frame) - 1.
+ * A row that sees nothing is zero.  Whatever a page holds behind its sequence's
+ * last token is not used, infinities and NaN included; a non-finite value V of a
+ * token within the sequence may reach every row of the chunk.  Rows from
+ * q_start[sequences] on are left as they are.  A bf16 model may split a
+ * sequence's keys over several CTAs and merge them with a second kernel through
+ * the workspace wdc_op_attention uses: two attention calls of one context must
+ * not run concurrently on different streams. */
+wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_cache* cache, const int* q_start,
+                                  int T, int heads, int max_new, int frame, void* o, wdc_stream stream);
+
 /* ------------------------------------------------------------------ allocation-free variant
  * wdc_observe_noalloc: the streaming half of the skip pass -- the kernelised
  * observation z_hat = sum_i kappa_i z_out_i over K latents together with the

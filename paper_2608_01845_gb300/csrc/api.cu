@@ -279,6 +279,24 @@ wdc_status sync(Ctx* c, cudaStream_t s) {
 
 }  // namespace
 
+// What the chunk operators share: the context has a model dtype, its device is
+// current, and no exception (of a string, in an error's path) leaves the library.
+template <class F>
+static wdc_status chunk_op(wdc_ctx* h, F&& run) {
+    Ctx* c = reinterpret_cast<Ctx*>(h);
+    if (!c) return WDC_ERR_INVALID_ARG;
+    try {
+        if (c->cfg.layers == 0) return fail(c, WDC_ERR_UNSUPPORTED, "operators need a model dtype (layers > 0)");
+        if (cudaSetDevice(c->device) != cudaSuccess) {
+            cudaGetLastError();
+            return fail(c, WDC_ERR_CUDA, "the context's device is not available");
+        }
+        return run(c);
+    } catch (...) {
+        return WDC_ERR_OOM;
+    }
+}
+
 extern "C" {
 
 const char* wdc_status_string(wdc_status s) {
@@ -1039,6 +1057,41 @@ wdc_status wdc_op_attention(wdc_ctx* h, const void* q, const void* k, const void
     if (c->cfg.layers == 0) return fail(c, WDC_ERR_UNSUPPORTED, "operators need a model dtype (layers > 0)");
     cudaSetDevice(c->device);
     return op_attention(c, q, k, vt, o, heads, L, d, (cudaStream_t)stream);
+}
+
+wdc_status wdc_op_quantize_fp8(wdc_ctx* h, const void* x, long long ldx, void* q, float* scale, int M, int K,
+                               int block_rows, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) { return op_quantize_fp8(c, x, ldx, q, scale, M, K, block_rows, (cudaStream_t)stream); });
+}
+
+wdc_status wdc_op_gemm_fp8(wdc_ctx* h, const void* A, const float* a_scale, const void* W, const float* w_scale,
+                           const float* bias, void* C, int M, int N, int K, int gelu, const void* res, const float* gate,
+                           wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        return op_gemm_fp8(c, A, a_scale, W, w_scale, bias, C, M, N, K, gelu, res, gate, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_qk_norm_rope(wdc_ctx* h, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
+                               const wdc_head_norm* norm, void* q, void* k, void* vt, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        return op_qk_norm_rope(c, qkv, ld, T, heads, kv_heads, d, norm, q, k, vt, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* h, const void* qkv, long long ld, int T, int heads,
+                                      const wdc_head_norm* norm, const wdc_paged_cache* cache, const int* q_start,
+                                      void* q, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        return op_qk_norm_rope_append(c, qkv, ld, T, heads, norm, cache, q_start, q, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_attention_paged(wdc_ctx* h, const void* q, const wdc_paged_cache* cache, const int* q_start, int T,
+                                  int heads, int max_new, int frame, void* o, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        return op_attention_paged(c, q, cache, q_start, T, heads, max_new, frame, o, (cudaStream_t)stream);
+    });
 }
 
 }  // extern "C"

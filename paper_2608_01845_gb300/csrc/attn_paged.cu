@@ -1,0 +1,598 @@
+// Attention of a chunk of new tokens over a paged cache on the tcgen05 tensor
+// cores (sm_103a): o = softmax(q K^T / sqrt(d)) V, a token seeing the tokens of
+// its sequence up to a limit (include/wdc.h).  Q bf16 [T, heads, d]; K bf16 and
+// V fp16 in pages [page][d] of a key head; S = Q K^T in fp32, P in fp16, O and the
+// row sums in fp32; d = 64 or 128.
+//
+// One CTA per (sequence, key head, block of query rows), 12 warps in three
+// warpgroups as in the dense attention (attn_tc.cu): a TMA producer and two MMA
+// issuers with few registers, two softmax warpgroups of one thread a row.  What
+// differs:
+//  * Rows are (token, query head of the key head's group), token-major: a tile
+//    of 128 rows is 128 / G tokens of all G heads of a group, one TMA box of the
+//    packed q.  A single token's group shares one read of the cache.
+//  * K and V come page by page: a step of BK keys is BK / page boxes (or a part
+//    of one), whose page numbers the producer's lanes look up a step ahead.  A
+//    page number out of range becomes a coordinate past the pool, which TMA fills
+//    with zeros, like the pages behind a sequence's end.
+//  * V lies as the cache holds it, keys along its rows: the MMA takes it as an
+//    MN-major operand.
+//  * Behind the sequence's last token its last page may hold anything.  Scores
+//    there are masked; a probability of 0 times an infinity or NaN of V would not
+//    be 0, so the producer zeroes those rows of the last step's V in shared
+//    memory before that step's PV products.
+//  * Each row has a limit of its own.  A row that has seen nothing yet takes the
+//    next tile's maximum as its exponent base, as at the first step.
+//  * Row sums add the fp16 probabilities in fp32 (mixed-precision adds).
+// Where the units are fewer than the SMs, each is split over its keys into
+// g.split CTAs, whose partial rows paged_combine_kernel merges in order.
+#include "attn_softmax.cuh"
+#include "dit_kernels.cuh"
+#include "paged_index.h"
+#include "ptx.cuh"
+
+#include <climits>
+
+namespace wdc {
+
+namespace {
+
+constexpr int BQ = 128;                // rows a tile, two tiles a CTA
+constexpr uint32_t kRegsLaunch = 168;  // 65536 / 384 rounded down to a multiple of 8
+
+template <int D>
+struct PagedCfg {
+    static constexpr int BK = D == 64 ? 128 : 64;           // keys a step
+    static constexpr int THREADS = 384;
+    static constexpr int ATOMS = D / 64;                    // 128-byte atoms along d
+    static constexpr uint32_t Q_TILE = BQ * D * 2;
+    static constexpr uint32_t K_TILE = BK * D * 2;
+    static constexpr uint32_t STAGE = 2 * K_TILE;           // 32 KB for both head sizes
+    static constexpr int STAGES = 5;
+    static constexpr uint32_t SMEM = 2 * Q_TILE + STAGES * STAGE + 1024 + 256;
+    static constexpr uint32_t TMEM_COLS = 512;
+    static constexpr uint32_t REGS_CONTROL = 40;
+    static constexpr uint32_t REGS_SOFTMAX = 232;
+    static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= 384 * kRegsLaunch, "register split exceeds the launch");
+    static_assert(2 * (BK + BK / 2 + D) <= (int)TMEM_COLS, "S, P and O of two tiles exceed tensor memory");
+    static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
+    __device__ static constexpr uint32_t s_col(int t) { return (uint32_t)(BK + BK / 2 + D) * t; }
+    __device__ static constexpr uint32_t p_col(int t) { return s_col(t) + BK; }
+    __device__ static constexpr uint32_t o_col(int t) { return s_col(t) + BK + BK / 2; }
+};
+
+struct PagedArgs {
+    int T, heads, kv, G, tpt;          // G query heads a key head, tpt tokens a tile
+    int q_blocks, max_new, split;
+    int page_log2, pages, width, frame;
+    const int *table, *length, *start;
+    float scale_log2;
+    __nv_bfloat16* o;
+    float* part_o;                     // [unit][split][256 rows][d]
+    float2* part_ml;                   // [unit][split][256 rows] base, row sum
+    unsigned* err;
+};
+
+// A unit: sequence, key head, query block; the blocks with the most keys first.
+struct Unit : PagedSeq {
+    int b, h, qb;
+    __device__ Unit(const PagedArgs& g, int u) {
+        qb = g.q_blocks - 1 - u % g.q_blocks;
+        const int r = u / g.q_blocks;
+        h = r % g.kv;
+        b = r / g.kv;
+        static_cast<PagedSeq&>(*this) = paged_seq(g.start[b], g.start[b + 1], g.length[b], g.T, g.width << g.page_log2);
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
+    attn_paged_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                      const __grid_constant__ CUtensorMap tv, const __grid_constant__ PagedArgs g) {
+    using C = PagedCfg<D>;
+    constexpr int BKV = C::BK;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sq = smem;                                       // [2 tiles][ATOMS][128 x 128 B]
+    uint8_t* skv = smem + 2 * C::Q_TILE;                      // [STAGES][K | V], each [ATOMS][BK x 128 B]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(skv + C::STAGES * C::STAGE);
+    uint64_t* q_full = bars;
+    uint64_t* kv_full = q_full + 1;
+    uint64_t* kv_empty = kv_full + C::STAGES;
+    uint64_t* s_full = kv_empty + C::STAGES;                  // [2]
+    uint64_t* s_free = s_full + 2;                            // [2]
+    uint64_t* p_full = s_free + 2;                            // [2]
+    uint64_t* p_free = p_full + 2;                            // [2]
+    uint64_t* o_final = p_free + 2;                           // [2]
+    uint64_t* v_ready = o_final + 2;                          // the last step's V is clear behind the sequence
+    uint64_t* mma_done = v_ready + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(&kv_full[s], 1);
+            mbar_init(&kv_empty[s], 2);        // each MMA issuer's, or the one's and the producer's
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(&s_full[w], 1);
+            mbar_init(&s_free[w], 4);
+            mbar_init(&p_full[w], 4);
+            mbar_init(&p_free[w], 1);
+            mbar_init(&o_final[w], 1);
+        }
+        mbar_init(v_ready, 1);
+        mbar_init(mma_done, 2);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 0 && lane == 0) {
+        prefetch_tmap(&tq);
+        prefetch_tmap(&tk);
+        prefetch_tmap(&tv);
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, C::TMEM_COLS);
+        tmem_relinquish();
+    }
+    __syncthreads();
+    tc_fence_after();
+    chain_release();
+    chain_wait();
+    const uint32_t tmem = *tmem_slot;
+
+    const int u = blockIdx.x / g.split, part = blockIdx.x - u * g.split;
+    const Unit un(g, u);
+    const int tok0 = un.qb * 2 * g.tpt;                       // the chunk's first token here
+    const bool idle = tok0 >= un.n;
+    const int nt = tok0 + g.tpt < un.n ? 2 : 1;               // tiles with rows
+    const int keys = idle ? 0 : paged_limit(un, g.frame, min(tok0 + 2 * g.tpt, un.n) - 1);
+    const int steps = (keys + BKV - 1) / BKV;
+    const int j0 = (int)((long long)part * steps / g.split);
+    const int nj = (int)((long long)(part + 1) * steps / g.split) - j0;
+    const int page = 1 << g.page_log2;
+    const int used = (un.len + page - 1) >> g.page_log2;      // pages of the sequence
+    // rows of the last step's V that lie behind the sequence, in its last page
+    const int last0 = (j0 + nj - 1) * BKV;
+    const int clear0 = un.len - last0, clear1 = min(BKV, (used << g.page_log2) - last0);
+    const bool clear = nj > 0 && clear0 < clear1;
+
+    if (wg == 0) {
+        setmaxnreg_dec<C::REGS_CONTROL>();
+        if (warp == 0) {
+            if (part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
+                const int given = g.length[un.b];
+                if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
+            }
+            if (nj > 0) {
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(q_full, (uint32_t)(nt * C::ATOMS * g.G * g.tpt) * 128u);
+                    for (int t = 0; t < nt; ++t)
+                        for (int a = 0; a < C::ATOMS; ++a)
+                            tma_load_4d(sq + t * C::Q_TILE + a * (BQ * 128), &tq, q_full, 64 * a, 0, un.h,
+                                        un.row0 + tok0 + t * g.tpt);
+                }
+                __syncwarp();
+                const int rows = min(page, BKV), boxes = BKV / rows;
+                // page of this lane's box of step j
+                auto lookup = [&](int j) {
+                    int p = g.pages;                          // past the pool: filled with zeros
+                    const int i = ((j * BKV) >> g.page_log2) + lane;
+                    if (lane < boxes && i < used) {
+                        p = paged_page(g.table[(size_t)un.b * g.width + i], g.pages);
+                        if (p < 0) {
+                            atomicOr(g.err, kErrBounds);
+                            p = g.pages;
+                        }
+                    }
+                    return p;
+                };
+                int stage = 0;
+                uint32_t phase = 0;
+                uint32_t armed = 0, parity = 0;               // per stage: a copy was issued; its phase
+                int next = lookup(j0);
+                bool ok = true;
+                for (int j = j0; j < j0 + nj; ++j) {
+                    const int p = next;
+                    if (j + 1 < j0 + nj) next = lookup(j + 1);
+                    if (!mbar_wait_warp(&kv_empty[stage], phase ^ 1u, abort_flag, g.err)) { ok = false; break; }
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(&kv_full[stage], C::STAGE);
+                        if (nt == 1) mbar_arrive(&kv_empty[stage]);
+                    }
+                    __syncwarp();
+                    if (lane < boxes) {
+                        uint8_t* sk = skv + stage * C::STAGE + lane * rows * 128;
+                        const int y = (j * BKV) & (page - 1);
+                        for (int a = 0; a < C::ATOMS; ++a)
+                            tma_load_4d(sk + a * (BKV * 128), &tk, &kv_full[stage], 64 * a, boxes > 1 ? 0 : y, un.h, p);
+                        for (int a = 0; a < C::ATOMS; ++a)
+                            tma_load_4d(sk + C::K_TILE + a * (BKV * 128), &tv, &kv_full[stage], 64 * a, boxes > 1 ? 0 : y,
+                                        un.h, p);
+                    }
+                    __syncwarp();
+                    armed |= 1u << stage;
+                    parity = (parity & ~(1u << stage)) | (phase << stage);
+                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (ok && clear) {
+                    const int st = (nj - 1) % C::STAGES;
+                    if (mbar_wait_warp(&kv_full[st], (parity >> st) & 1, abort_flag, g.err)) {
+                        for (int a = 0; a < C::ATOMS; ++a) {
+                            uint4* v = reinterpret_cast<uint4*>(skv + st * C::STAGE + C::K_TILE + a * (BKV * 128));
+                            for (int i = clear0 * 8 + lane; i < clear1 * 8; i += 32) v[i] = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(v_ready);
+                    }
+                }
+                {
+                    const unsigned long long t0 = globaltimer();
+                    while (!mbar_try_wait(q_full, 0) && globaltimer() - t0 < kWaitLimitNs) {
+                    }
+                }
+                for (int s = 0; s < C::STAGES; ++s) {
+                    if (!((armed >> s) & 1)) continue;
+                    const unsigned long long t0 = globaltimer();
+                    while (!mbar_try_wait(&kv_full[s], (parity >> s) & 1) && globaltimer() - t0 < kWaitLimitNs) {
+                    }
+                }
+            }
+        } else if ((warp == 1 || (warp == 2 && nt == 2)) && nj > 0) {
+            constexpr uint32_t idesc_s = idesc_bf16(BQ, BKV);
+            constexpr uint32_t idesc_o = idesc_f16_mn(BQ, D);    // P (fp16, TMEM) x V (fp16, MN-major)
+            const int t = warp - 1;
+            constexpr bool kOneLane = D == 128;                  // (as in the dense attention)
+            auto leads = [] { return kOneLane || elect_one(); };
+            auto rejoin = [] { if (!kOneLane) __syncwarp(); };
+            if (!kOneLane || elect_one()) {
+                const uint64_t dq = sdesc_sw128(smem_u32(sq) + t * C::Q_TILE), dk = sdesc_sw128(smem_u32(skv));
+                const uint64_t dv = sdesc_sw128_mn(smem_u32(skv) + C::K_TILE, BKV * 128);
+                bool ok = mbar_wait(q_full, 0, abort_flag, g.err);        // this lane's waits (elect_one)
+                int stage = 0, prev = 0;
+                uint32_t phase = 0;
+                auto issue_s = [&](int st) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const uint32_t off = (ks >> 2) * (BQ * 128) + (ks & 3) * 32;
+                        const uint32_t koff = (ks >> 2) * (BKV * 128) + (ks & 3) * 32;
+                        tc_mma(tmem + C::s_col(t), sdesc_at(dq, off), sdesc_at(dk, st * C::STAGE + koff), idesc_s, ks != 0);
+                    }
+                };
+                // O(t) (+)= P(t) V: 16 keys (rows of V, 2 KB) = 8 columns of P an MMA
+                auto issue_pv = [&](int st, bool acc) {
+#pragma unroll
+                    for (int ks = 0; ks < BKV / 16; ++ks)
+                        tc_mma_ts(tmem + C::o_col(t), tmem + C::p_col(t) + ks * 8, sdesc_at(dv, st * C::STAGE + ks * 2048),
+                                  idesc_o, (acc || ks != 0) ? 1u : 0u);
+                };
+                ok = ok && mbar_wait(&kv_full[0], 0, abort_flag, g.err);
+                for (int j = 0; j < nj; ++j) {
+                    // here K(j) has landed, and S(t, j - 1) is in the softmax's registers
+                    tc_fence_after();
+                    if (leads() && ok) {
+                        issue_s(stage);
+                        tc_commit(&s_full[t]);
+                    }
+                    rejoin();
+                    const int cur = stage;
+                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                    auto next_k = [&]() { if (j + 1 < nj) ok = ok && mbar_wait(&kv_full[stage], phase, abort_flag, g.err); };
+                    if (D == 128) next_k();
+                    if (j > 0) {
+                        ok = ok && mbar_wait(&p_full[t], (j - 1) & 1, abort_flag, g.err);
+                        tc_fence_after();
+                        if (leads() && ok) {
+                            issue_pv(prev, j > 1);
+                            tc_commit(&p_free[t]);
+                            tc_commit(&kv_empty[prev]);
+                        }
+                        rejoin();
+                    }
+                    prev = cur;
+                    if (D == 64) next_k();
+                    if (j + 1 < nj) ok = ok && mbar_wait(&s_free[t], j & 1, abort_flag, g.err);
+                }
+                ok = ok && mbar_wait(&p_full[t], (nj - 1) & 1, abort_flag, g.err);
+                if (clear) ok = ok && mbar_wait(v_ready, 0, abort_flag, g.err);
+                tc_fence_after();
+                if (leads() && ok) {
+                    issue_pv(prev, nj > 1);
+                    tc_commit(&kv_empty[prev]);
+                    tc_commit(&o_final[t]);
+                }
+                rejoin();
+                if (leads()) {
+                    tc_commit(mma_done);
+                    if (nt == 1) mbar_arrive(mma_done);
+                }
+            }
+            __syncwarp();
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(mma_done, 0) && globaltimer() - t0 < kWaitLimitNs) {
+            }
+        }
+    } else {
+        setmaxnreg_inc<C::REGS_SOFTMAX>();
+        // softmax warpgroups: t = tile, quarter = TMEM lane quarter
+        const int t = wg - 1;
+        const int quarter = warp & 3;
+        const int row = quarter * 32 + lane;                 // row within the tile = TMEM lane
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t s_addr = tmem + lane_base + C::s_col(t);
+        const uint32_t p_addr = tmem + lane_base + C::p_col(t);
+        const uint32_t o_addr = tmem + lane_base + C::o_col(t);
+        const int i = tok0 + t * g.tpt + row / g.G;          // the chunk's token
+        const bool valid = !idle && row < g.tpt * g.G && i < un.n;
+        const int lim = valid ? paged_limit(un, g.frame, i) : INT_MAX;    // (other rows hold what they hold)
+        const int min_lim = __reduce_min_sync(0xffffffffu, lim);
+        const bool work = __any_sync(0xffffffffu, valid);    // else the warp only keeps step
+        float m_run = -INFINITY, l_run = 0.f;
+        const uint64_t scale2 = pair(g.scale_log2, g.scale_log2);
+        bool ok = true, s_ready = false;
+        const int mine = t < nt ? nj : 0;
+        for (int j = 0; j < mine; ++j) {                     // j counts this CTA's steps
+            if (!s_ready && !mbar_wait_warp(&s_full[t], j & 1, abort_flag, g.err)) { ok = false; break; }
+            tc_fence_after();
+            if (!work) {
+                if (lane == 0) mbar_arrive(&s_free[t]);
+                if (j > 0 && !mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) { ok = false; break; }
+                if (lane == 0) mbar_arrive(&p_full[t]);
+                continue;
+            }
+            float s[BKV];
+#pragma unroll
+            for (int c = 0; c < BKV / 32; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+            tmem_ld_wait();
+            // S(t) is in registers: the MMA may compute S(t, j+1) now
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s_free[t]);
+            const int k0 = (j0 + j) * BKV;
+            if (min_lim - k0 < BKV) {
+                const int left = lim - k0;
+#pragma unroll
+                for (int c = 0; c < BKV; ++c)
+                    if (c >= left) s[c] = -INFINITY;
+            }
+            auto tile_max = [&]() {
+                // 8 independent partial maxima (short dependency chains)
+                float m8[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) m8[q] = fmaxf(s[q], s[8 + q]);
+#pragma unroll
+                for (int c = 16; c < BKV; c += 16)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) m8[q] = fmax3(m8[q], s[c + q], s[c + 8 + q]);
+                return fmax3(fmax3(m8[0], m8[1], m8[2]), fmax3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7]));
+            };
+            // numerators 2^(s * scale - base) into p (fp16 pairs); returns their fp32 sum
+            uint32_t p[BKV / 2];
+            auto numerators = [&](float base) {
+                float lo[2] = {0.f, 0.f}, hi[2] = {0.f, 0.f};
+                const uint64_t nm2 = pair(-base, -base);
+#pragma unroll
+                for (int c = 0; c < BKV; c += 2)
+                    p[c / 2] = exp2_pair_f(s[c], s[c + 1], scale2, nm2, lo[(c / 2) & 1], hi[(c / 2) & 1]);
+                return (lo[0] + lo[1]) + (hi[0] + hi[1]);
+            };
+            float base = m_run;
+            if (__any_sync(0xffffffffu, l_run == 0.f)) {     // a row that has seen nothing yet
+                const float top = tile_max() * g.scale_log2;
+                if (l_run == 0.f) base = top == -INFINITY ? 0.f : top;
+            }
+            float sum;
+            // A numerator above 2^8 implies a row sum above 2^8 (so does a
+            // non-finite one): only then take the tile max, move the base and
+            // recompute, as a second pass of the same code.
+#pragma unroll 1
+            for (int pass = 0;; ++pass) {
+                sum = numerators(base);
+                const bool redo = pass == 0 && valid && !(sum <= 256.0f);
+                if (!__any_sync(0xffffffffu, redo)) break;
+                if (redo) base = fmaxf(base, tile_max() * g.scale_log2);
+            }
+            const bool moved = __any_sync(0xffffffffu, base != m_run);
+            const float corr = ex2(m_run - base);            // 1 when the base stays; 0 before the first tile
+            l_run = l_run * corr + sum;
+            m_run = base;
+            // PV(t, j-1) must be done before P(t) is overwritten and O(t) rescaled
+            if (j > 0) {
+                if (!mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) { ok = false; break; }
+                tc_fence_after();
+            }
+            if (j > 0 && moved) {
+                // PV(t, j-1) is complete: rescale O in place
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(o_addr + c, o);
+                    tmem_ld_wait();
+                    uint32_t lo[16], hi[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        lo[q] = __float_as_uint(__uint_as_float(o[q]) * corr);
+                        hi[q] = __float_as_uint(__uint_as_float(o[16 + q]) * corr);
+                    }
+                    tmem_st16(o_addr + c, lo);
+                    tmem_st16(o_addr + c + 16, hi);
+                }
+            }
+            // P (BK / 2 columns of fp16 pairs)
+#pragma unroll
+            for (int c = 0; c < BKV / 2; c += 16) tmem_st16(p_addr + c, *reinterpret_cast<uint32_t(*)[16]>(&p[c]));
+            const bool next = D == 64 && mbar_test(&s_full[t], (j + 1) & 1);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[t]);
+            if (D == 64) s_ready = __all_sync(0xffffffffu, next);
+        }
+        if (ok && mine > 0) ok = mbar_wait_warp(&o_final[t], 0, abort_flag, g.err);
+        if (ok && work) {
+            tc_fence_after();
+            const bool seen = l_run != 0.f;                  // (a NaN is seen)
+            const bool split = g.split > 1;
+            const size_t prow = ((size_t)blockIdx.x * 2 + t) * BQ + row;
+            const float inv = seen ? 1.0f / l_run : 0.f;
+            __nv_bfloat16* out = g.o + ((size_t)(un.row0 + i) * g.heads + un.h * g.G + row % g.G) * D;
+            float* po = g.part_o + prow * D;
+            if (split && valid) g.part_ml[prow] = make_float2(seen ? m_run : -INFINITY, l_run);
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                if (mine > 0) {
+                    tmem_ld32(o_addr + c, o);
+                    tmem_ld_wait();
+                }
+                if (!valid) continue;
+                if (split) {
+                    if (!seen) continue;
+                    float4* dst = reinterpret_cast<float4*>(po + c);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        dst[q] = make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
+                                             __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]));
+                } else {
+                    uint4* dst = reinterpret_cast<uint4*>(out + c);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (seen) {
+                            w.x = pack2(__uint_as_float(o[8 * q + 0]) * inv, __uint_as_float(o[8 * q + 1]) * inv);
+                            w.y = pack2(__uint_as_float(o[8 * q + 2]) * inv, __uint_as_float(o[8 * q + 3]) * inv);
+                            w.z = pack2(__uint_as_float(o[8 * q + 4]) * inv, __uint_as_float(o[8 * q + 5]) * inv);
+                            w.w = pack2(__uint_as_float(o[8 * q + 6]) * inv, __uint_as_float(o[8 * q + 7]) * inv);
+                        }
+                        dst[q] = w;
+                    }
+                }
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, C::TMEM_COLS);
+    }
+}
+
+// Merges the parts of each row, in order: one warp a row, lane l owning columns
+// l, l + 32, ...: o = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, m = max m_p.
+template <int D>
+__global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constant__ PagedArgs g, int rows_unit, int units) {
+    chain_release();
+    chain_wait();
+    const long long w = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31;
+    const int u = (int)(w / rows_unit), r = (int)(w - (long long)u * rows_unit);
+    if (u >= units) return;
+    const Unit un(g, u);
+    const int ti = r / g.G, i = un.qb * 2 * g.tpt + ti;
+    if (i >= un.n) return;
+    const int t = ti / g.tpt, row = (ti - t * g.tpt) * g.G + r % g.G;
+    float m = -INFINITY;
+    const size_t p0 = ((size_t)u * g.split * 2 + t) * BQ + row;      // part p lies p * 2 * BQ rows on
+    for (int p = 0; p < g.split; ++p) m = fmaxf(m, g.part_ml[p0 + (size_t)p * 2 * BQ].x);
+    float l = 0.f, acc[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) acc[c] = 0.f;
+    for (int p = 0; p < g.split; ++p) {
+        const size_t prow = p0 + (size_t)p * 2 * BQ;
+        const float2 ml = g.part_ml[prow];
+        if (ml.x == -INFINITY) continue;                             // saw nothing: has no O
+        const float f = ex2(ml.x - m);
+        l = fmaf(ml.y, f, l);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) acc[c] = fmaf(f, g.part_o[prow * D + lane + 32 * c], acc[c]);
+    }
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    __nv_bfloat16* out = g.o + ((size_t)(un.row0 + i) * g.heads + un.h * g.G + r % g.G) * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) out[lane + 32 * c] = __float2bfloat16_rn(acc[c] * inv);
+}
+
+template <int D>
+wdc_status launch(Ctx* c, const void* q, const wdc_paged_cache* p, PagedArgs g, cudaStream_t s) {
+    using Cf = PagedCfg<D>;
+    static PerDevice<bool> fits;
+    const bool regs_ok = fits.get(c->device, [](bool& ok) {
+        const bool smem = allow_smem(attn_paged_kernel<D>, Cf::SMEM);
+        // the warpgroups' register requests must fit the launch allocation,
+        // or setmaxnreg.inc would wait forever: refuse to launch otherwise
+        cudaFuncAttributes fa;
+        ok = cudaFuncGetAttributes(&fa, attn_paged_kernel<D>) == cudaSuccess && fa.maxThreadsPerBlock >= Cf::THREADS &&
+             (uint32_t)fa.numRegs * Cf::THREADS >= 128 * Cf::REGS_CONTROL + 256 * Cf::REGS_SOFTMAX;
+        cudaGetLastError();
+        return smem && ok;
+    });
+    if (!regs_ok) return fail(c, WDC_ERR_UNSUPPORTED, "paged attention kernel's register allocation is below its warpgroup split");
+    CUtensorMap tq, tk, tv;
+    std::string why;
+    const uint64_t row = (uint64_t)D * 2, pg = (uint64_t)p->page;
+    const uint64_t qd[4] = {D, (uint64_t)g.G, (uint64_t)g.kv, (uint64_t)g.T}, qs[3] = {row, row * g.G, row * g.heads};
+    const uint32_t qb[4] = {64, (uint32_t)g.G, 1, (uint32_t)g.tpt};
+    const uint64_t kd[4] = {D, pg, (uint64_t)g.kv, (uint64_t)g.pages}, ks[3] = {row, row * pg, row * pg * g.kv};
+    const uint32_t kb[4] = {64, (uint32_t)(p->page < Cf::BK ? p->page : Cf::BK), 1, 1};
+    if (!encode_tmap_4d(&tq, q, qd, qs, qb, false, &why) || !encode_tmap_4d(&tk, p->k, kd, ks, kb, false, &why) ||
+        !encode_tmap_4d(&tv, p->v, kd, ks, kb, true, &why))
+        return fail(c, WDC_ERR_CUDA, why);
+    g.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+    g.q_blocks = (g.max_new + 2 * g.tpt - 1) / (2 * g.tpt);
+    const long long units = (long long)p->sequences * g.kv * g.q_blocks;
+    if (units > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "paged attention: more than 2^31 - 1 thread blocks");
+    const long long steps = (((long long)g.width << g.page_log2) + Cf::BK - 1) / Cf::BK;
+    g.split = 1;
+    // (the workspace holds the partial rows of num_sms CTAs a sample)
+    if (c->attn_part && 2 * units <= c->num_sms) {
+        long long sp = c->num_sms / units;
+        if (sp > steps / 2) sp = steps / 2;
+        g.split = sp > 1 ? (int)sp : 1;
+    }
+    g.part_o = c->attn_part;
+    g.part_ml = reinterpret_cast<float2*>(c->attn_ml);
+    OverlapScope ov(c, s);
+    {
+        LaunchScope ls(c, WDC_K_ATTN, s);
+        launch_kernel(attn_paged_kernel<D>, dim3((unsigned)(units * g.split)), Cf::THREADS, Cf::SMEM, s, 1, tq, tk, tv, g);
+    }
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention launch: ") + cudaGetErrorString(e));
+    if (g.split > 1) {
+        const int tokens = g.max_new < 2 * g.tpt ? g.max_new : 2 * g.tpt;
+        const long long rows = units * tokens * g.G;
+        LaunchScope ls(c, WDC_K_OTHER, s);
+        launch_kernel(paged_combine_kernel<D>, dim3((unsigned)((rows + 7) / 8)), 256, 0, s, 1, g, tokens * g.G, (int)units);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention merge launch: ") + cudaGetErrorString(e));
+    }
+    return WDC_OK;
+}
+
+}  // namespace
+
+wdc_status op_attention_paged(Ctx* c, const void* q, const wdc_paged_cache* p, const int* q_start, int T, int heads,
+                              int max_new, int frame, void* o, cudaStream_t s) {
+    PagedArgs g{};
+    if (wdc_status st = check_cache(c, p, &g.page_log2)) return st;
+    if (T < 0 || heads < 1 || max_new < 0 || frame < 0) return fail(c, WDC_ERR_INVALID_ARG, "paged attention: bad sizes");
+    if (heads % p->kv_heads) return fail(c, WDC_ERR_INVALID_ARG, "paged attention: heads must be a multiple of kv_heads");
+    if (heads / p->kv_heads > BQ) return fail(c, WDC_ERR_UNSUPPORTED, "paged attention: at most 128 query heads a key head");
+    if (T == 0 || p->sequences == 0 || max_new == 0) return WDC_OK;
+    if (!q || !o || !q_start) return fail(c, WDC_ERR_INVALID_ARG, "paged attention: null pointer");
+    if (((uintptr_t)q | (uintptr_t)o) & 15) return fail(c, WDC_ERR_INVALID_ARG, "paged attention: q and o must be 16-byte aligned");
+    if ((uintptr_t)q_start & 3) return fail(c, WDC_ERR_INVALID_ARG, "paged attention: q_start must be 4-byte aligned");
+    g.T = T; g.heads = heads; g.kv = p->kv_heads; g.G = heads / p->kv_heads; g.tpt = BQ / g.G;
+    g.max_new = max_new < T ? max_new : T;
+    g.pages = p->pages; g.width = p->table_width; g.frame = frame;
+    g.table = p->table; g.length = p->length; g.start = q_start;
+    g.o = reinterpret_cast<__nv_bfloat16*>(o);
+    g.err = c->err;
+    return p->head_dim == 64 ? launch<64>(c, q, p, g, s) : launch<128>(c, q, p, g, s);
+}
+
+}  // namespace wdc

@@ -56,10 +56,9 @@
 // the SMs.
 // Keys past L are masked (TMA zero-fills out-of-range K / V^T).  Every
 // mbarrier wait is bounded.
+#include "attn_softmax.cuh"
 #include "dit_kernels.cuh"
 #include "ptx.cuh"
-
-#include <cuda_fp16.h>
 
 namespace wdc {
 
@@ -115,54 +114,6 @@ struct AttnArgs {
     float* part_o;            // [part slot][256 rows][d]
     float* part_ml;           // [part slot][256 rows][base, row sum]
 };
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Three-input maximum (one instruction for two comparisons).
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&h);
-}
-
-// Two f32 values as one paired-fp32 operand (lo = a, hi = b).
-__device__ __forceinline__ uint64_t pair(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-
-// Two softmax numerators: x pair (fma.f32x2) -> f16x2 -> ex2.approx.f16x2
-// (one SFU instruction for both) = the P word; the pair is added into an
-// f16x2 partial sum.
-__device__ __forceinline__ uint32_t exp2_pair_h(float s0, float s1, uint64_t scale2, uint64_t nm2, uint32_t& acc) {
-    uint32_t p;
-    asm("{\n .reg .b64 x;\n .reg .f32 a, b;\n .reg .b32 h;\n"
-        " mov.b64 x, {%2, %3};\n"
-        " fma.rn.f32x2 x, x, %4, %5;\n"
-        " mov.b64 {a, b}, x;\n"
-        " cvt.rn.f16x2.f32 h, b, a;\n"
-        " ex2.approx.f16x2 %0, h;\n"
-        " add.rn.f16x2 %1, %1, %0;\n}"
-        : "=r"(p), "+r"(acc)
-        : "f"(s0), "f"(s1), "l"(scale2), "l"(nm2));
-    return p;
-}
-
-__device__ __forceinline__ float half2_sum(uint32_t v) {
-    __half2 h = *reinterpret_cast<__half2*>(&v);
-    return __low2float(h) + __high2float(h);
-}
-
 
 // BATCH: heads of several samples, output rows through the batch's
 // stream-major token layout; otherwise row = token, head = h (one sample).

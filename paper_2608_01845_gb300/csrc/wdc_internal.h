@@ -339,4 +339,19 @@ wdc_status op_gemm(Ctx* c, const void* A, const void* W, const float* bias, void
 wdc_status op_attention(Ctx* c, const void* q, const void* k, const void* vt, void* o, int heads, int L,
                         int d, cudaStream_t s);
 
+// quant_fp8.cu, gemm_fp8.cu, qk_norm_rope.cu, attn_paged.cu: the chunk operators
+wdc_status op_quantize_fp8(Ctx* c, const void* x, long long ldx, void* q, float* scale, int M, int K, int block_rows,
+                           cudaStream_t s);
+wdc_status op_gemm_fp8(Ctx* c, const void* A, const float* a_scale, const void* W, const float* w_scale,
+                       const float* bias, void* C, int M, int N, int K, int gelu, const void* res, const float* gate,
+                       cudaStream_t s);
+wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n,
+                           void* q, void* k, void* vt, cudaStream_t s);
+wdc_status op_qk_norm_rope_append(Ctx* c, const void* qkv, long long ld, int T, int heads, const wdc_head_norm* n,
+                                  const wdc_paged_cache* p, const int* q_start, void* q, cudaStream_t s);
+wdc_status op_attention_paged(Ctx* c, const void* q, const wdc_paged_cache* p, const int* q_start, int T, int heads,
+                              int max_new, int frame, void* o, cudaStream_t s);
+// Checks a cache's description; *page_log2: its page size.
+wdc_status check_cache(Ctx* c, const wdc_paged_cache* p, int* page_log2);
+
 }  // namespace wdc

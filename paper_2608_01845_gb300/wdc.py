@@ -109,6 +109,17 @@ class StateHost(ctypes.Structure):
                 ("cand_supported", ctypes.c_int), ("cand_finite", ctypes.c_int), ("cand_p", ctypes.c_double)]
 
 
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rot", ctypes.c_void_p), ("rot_positions", ctypes.c_int), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("positions", ctypes.c_void_p)]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ["k", "v", "table", "length"]]
+                + [(n, ctypes.c_int) for n in ["pages", "page", "kv_heads", "head_dim", "sequences", "table_width"]])
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libwdc.so not built at {LIB_PATH}; run `python -m paper_2608_01845_gb300.build`")
@@ -152,6 +163,12 @@ def _load():
         "wdc_native_rollout": (I, [P, P, ctypes.POINTER(Cond), I, P, P]),
         "wdc_op_gemm": (I, [P, P, P, P, P, I, I, I, I, P, P, P]),
         "wdc_op_attention": (I, [P, P, P, P, P, I, I, I, P]),
+        "wdc_op_quantize_fp8": (I, [P, P, ctypes.c_longlong, P, P, I, I, I, P]),
+        "wdc_op_gemm_fp8": (I, [P, P, P, P, P, P, P, I, I, I, I, P, P, P]),
+        "wdc_op_qk_norm_rope": (I, [P, P, ctypes.c_longlong, I, I, I, I, ctypes.POINTER(HeadNorm), P, P, P, P]),
+        "wdc_op_qk_norm_rope_append": (I, [P, P, ctypes.c_longlong, I, I, ctypes.POINTER(HeadNorm),
+                                           ctypes.POINTER(PagedCacheC), P, P, P]),
+        "wdc_op_attention_paged": (I, [P, P, ctypes.POINTER(PagedCacheC), P, I, I, I, I, P, P]),
         "wdc_observe_noalloc": (I, [ctypes.POINTER(P), I, ctypes.POINTER(D), P, P, P, S, ctypes.c_uint32, P]),
     }
     for name, (res, args) in sig.items():
@@ -210,6 +227,39 @@ def make_cond(tokens=None, cam=None, depth=None):
     return c
 
 
+class PagedCache:
+    """wdc_paged_cache over torch tensors, which it keeps alive: k (bf16) and v
+    (fp16) [pages, kv_heads, page, head_dim], table [sequences, table_width]
+    and length [sequences] int32."""
+
+    def __init__(self, k, v, table, length):
+        import torch
+        if k.dim() != 4 or table.dim() != 2 or length.dim() != 1 or table.shape[0] != length.shape[0]:
+            raise ValueError("PagedCache: k [pages, kv_heads, page, d], table [sequences, width], length [sequences]")
+        _tensor("PagedCache", "k", k, torch.bfloat16, k.shape, k.device)
+        _tensor("PagedCache", "v", v, torch.float16, k.shape, k.device)
+        _tensor("PagedCache", "table", table, torch.int32, table.shape, k.device)
+        _tensor("PagedCache", "length", length, torch.int32, length.shape, k.device)
+        self.k, self.v, self.table, self.length = k, v, table, length
+        self.c = PagedCacheC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), k.shape[0], k.shape[2],
+                             k.shape[1], k.shape[3], table.shape[0], table.shape[1])
+
+
+def _tensor(what, name, t, dtype, shape, device, row_stride=False):
+    """Checks a tensor that an operator takes; row_stride: its rows may lie apart."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: {name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what}: {name} is on {t.device}, not {device}")
+    if not t.is_contiguous() and not (row_stride and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)):
+        raise ValueError(f"{what}: {name} must be contiguous")
+
+
+def _row_stride(t):
+    """Elements from one row to the next; of a single row, its length."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
 class Context:
     """Owns one wdc_ctx.  Method names follow the C entry points."""
 
@@ -222,6 +272,7 @@ class Context:
                             ctypes.byref(self._h))
         if st != 0:
             raise WdcError(st, "wdc_create failed")
+        self.device = device
 
     def close(self):
         if self._h:
@@ -422,6 +473,120 @@ class Context:
         H, L, d = q.shape
         self._check(LIB.wdc_op_attention(self._h, _ptr(q), _ptr(k), _ptr(vt), _ptr(o), H, L, d, _stream(stream)),
                     "op_attention")
+
+
+    # ---- chunk operators: the tensors' types, shapes and device are checked here, the rest behind the C ABI
+
+    def _operand_types(self):
+        import torch
+        return (torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32), torch.device("cuda", self.device)
+
+    def _op_stream(self, stream):
+        import torch
+        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+
+    def op_quantize_fp8(self, x, q, scale, block_rows=1, stream=None):
+        """wdc_op_quantize_fp8: x [M, K] (rows may lie apart) to q (float8_e4m3fn [M, K]) and scale
+        ([ceil(K/128), M], or with block_rows=128 [ceil(M/128), ceil(K/128)])."""
+        import torch
+        dt, dev = self._operand_types()
+        if x.dim() != 2:
+            raise ValueError("op_quantize_fp8: x must be [M, K]")
+        M, K = x.shape
+        kb = -(-K // 128)
+        _tensor("op_quantize_fp8", "x", x, dt, (M, K), dev, row_stride=True)
+        _tensor("op_quantize_fp8", "q", q, torch.float8_e4m3fn, (M, K), dev)
+        _tensor("op_quantize_fp8", "scale", scale, torch.float32, (kb, M) if block_rows == 1 else (-(-M // 128), kb), dev)
+        self._check(LIB.wdc_op_quantize_fp8(self._h, _ptr(x), _row_stride(x), _ptr(q), _ptr(scale), M, K, block_rows,
+                                            self._op_stream(stream)), "op_quantize_fp8")
+
+    def op_gemm_fp8(self, A, a_scale, W, w_scale, C, bias=None, gelu=False, res=None, gate=None, stream=None):
+        """wdc_op_gemm_fp8: C = epilogue(A W^T) of float8_e4m3fn matrices with the scales of op_quantize_fp8
+        (block_rows=1 for A, 128 for W)."""
+        import torch
+        dt, dev = self._operand_types()
+        if A.dim() != 2 or W.dim() != 2:
+            raise ValueError("op_gemm_fp8: A must be [M, K] and W [N, K]")
+        (M, K), N = A.shape, W.shape[0]
+        kb = -(-K // 128)
+        for name, t, ty, shape in (("A", A, torch.float8_e4m3fn, (M, K)), ("W", W, torch.float8_e4m3fn, (N, K)),
+                                   ("a_scale", a_scale, torch.float32, (kb, M)),
+                                   ("w_scale", w_scale, torch.float32, (-(-N // 128), kb)), ("C", C, dt, (M, N)),
+                                   ("bias", bias, torch.float32, (N,)), ("res", res, dt, (M, N)),
+                                   ("gate", gate, torch.float32, (N,))):
+            if t is not None:
+                _tensor("op_gemm_fp8", name, t, ty, shape, dev)
+        self._check(LIB.wdc_op_gemm_fp8(self._h, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(C), M,
+                                        N, K, int(gelu), _ptr(res), _ptr(gate), self._op_stream(stream)), "op_gemm_fp8")
+
+    def _head_norm(self, what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved):
+        import torch
+        for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if t is not None:
+                _tensor(what, name, t, torch.float32, (d,), dev)
+        if positions is not None:
+            _tensor(what, "positions", positions, torch.int32, (T,), dev)
+        n = HeadNorm(eps=eps, interleaved=int(bool(interleaved)))
+        n.q_weight, n.k_weight, n.positions = _ptr(q_weight), _ptr(k_weight), _ptr(positions)
+        if rot is not None:
+            if rot.dim() != 3 or rot.shape[2] != 2:
+                raise ValueError(f"{what}: rot must be [positions, rot_dim / 2, 2]")
+            _tensor(what, "rot", rot, torch.float32, rot.shape, dev)
+            n.rot, n.rot_positions, n.rot_dim = _ptr(rot), rot.shape[0], 2 * rot.shape[1]
+        return n
+
+    def op_qk_norm_rope(self, qkv, q, k, vt=None, q_weight=None, k_weight=None, eps=1e-6, rot=None, positions=None,
+                        interleaved=True, stream=None):
+        """wdc_op_qk_norm_rope: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) to q [heads, T, d],
+        k [kv_heads, T, d] and vt [kv_heads, d, T rounded up to 8] (fp16; fp32 and T for an fp32 model)."""
+        import torch
+        what, (dt, dev) = "op_qk_norm_rope", self._operand_types()
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError(f"{what}: q must be [heads, T, d] and k [kv_heads, T, d]")
+        (H, T, d), kv = q.shape, k.shape[0]
+        _tensor(what, "qkv", qkv, dt, (T, (H + 2 * kv) * d), dev, row_stride=True)
+        _tensor(what, "q", q, dt, (H, T, d), dev)
+        _tensor(what, "k", k, dt, (kv, T, d), dev)
+        if vt is not None:
+            bf16 = dt == torch.bfloat16
+            _tensor(what, "vt", vt, torch.float16 if bf16 else dt, (kv, d, -(-T // 8) * 8 if bf16 else T), dev)
+        n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        self._check(LIB.wdc_op_qk_norm_rope(self._h, _ptr(qkv), _row_stride(qkv), T, H, kv, d, ctypes.byref(n), _ptr(q),
+                                            _ptr(k), _ptr(vt), self._op_stream(stream)), what)
+
+    def op_qk_norm_rope_append(self, qkv, q, cache, q_start, q_weight=None, k_weight=None, eps=1e-6, rot=None,
+                               positions=None, interleaved=True, stream=None):
+        """wdc_op_qk_norm_rope_append: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) of new tokens to
+        q [T, heads, d], their keys and values into ``cache`` (a PagedCache); q_start int32 [sequences + 1]."""
+        import torch
+        what, (dt, dev) = "op_qk_norm_rope_append", self._operand_types()
+        if q.dim() != 3:
+            raise ValueError(f"{what}: q must be [T, heads, d]")
+        (T, H, d), c = q.shape, cache.c
+        if cache.k.device != dev or d != c.head_dim:
+            raise ValueError(f"{what}: the cache must be on {dev} with heads of {d}")
+        _tensor(what, "qkv", qkv, dt, (T, (H + 2 * c.kv_heads) * d), dev, row_stride=True)
+        _tensor(what, "q", q, dt, (T, H, d), dev)
+        _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
+        n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        self._check(LIB.wdc_op_qk_norm_rope_append(self._h, _ptr(qkv), _row_stride(qkv), T, H, ctypes.byref(n),
+                                                   ctypes.byref(c), _ptr(q_start), _ptr(q), self._op_stream(stream)), what)
+
+    def op_attention_paged(self, q, cache, q_start, o, max_new, frame=1, stream=None):
+        """wdc_op_attention_paged: q [T, heads, d] over ``cache`` (a PagedCache) into o [T, heads * d]; no
+        sequence has more than max_new new tokens."""
+        import torch
+        what, (dt, dev) = "op_attention_paged", self._operand_types()
+        if q.dim() != 3:
+            raise ValueError(f"{what}: q must be [T, heads, d]")
+        (T, H, d), c = q.shape, cache.c
+        if cache.k.device != dev or d != c.head_dim:
+            raise ValueError(f"{what}: the cache must be on {dev} with heads of {d}")
+        _tensor(what, "q", q, dt, (T, H, d), dev)
+        _tensor(what, "o", o, dt, (T, H * d), dev)
+        _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
+        self._check(LIB.wdc_op_attention_paged(self._h, _ptr(q), ctypes.byref(c), _ptr(q_start), T, H, int(max_new),
+                                               int(frame), _ptr(o), self._op_stream(stream)), what)
 
 
 def correlations(x, y):
