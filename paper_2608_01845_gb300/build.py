@@ -16,7 +16,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libwdc.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "step_kernels.cu", "dit.cu", "gemm_tc.cu", "attn_tc.cu", "graph_rollout.cu", "quant_fp8.cu",
-           "gemm_fp8.cu", "qk_norm_rope.cu", "attn_paged.cu"]
+           "gemm_fp8.cu", "gemm_fp8_pair.cu", "qk_norm_rope.cu", "attn_paged.cu"]
 
 
 def nvcc():

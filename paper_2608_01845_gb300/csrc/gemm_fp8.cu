@@ -6,30 +6,15 @@
 // own; the epilogue warps then add the buffer, times its scales, to sums in
 // their registers, while the next blocks' MMAs fill the other buffers.  So a
 // sum over K is fp32 beyond a block, whatever the scales.
-#include "dit_kernels.cuh"
-#include "ptx.cuh"
+#include "gemm_fp8.cuh"
 
 namespace wdc {
 
 namespace {
 
-constexpr int kBlock = 128;             // of K: bytes of a tile row
+constexpr int kBlock = kBlock8;
 constexpr int kThreads = 192;           // TMA producer, MMA issuer, 4 epilogue warps
 
-struct Gemm8Args {
-    int M, N, K, kb;                    // kb: blocks of K
-    int m_tiles, n_tiles, split;
-    const float *sa, *sw, *bias, *gate;
-    const void* res;
-    void* out;
-    int gelu;
-    unsigned* err;
-};
-
-__device__ __forceinline__ void cp_async4(float* dst, const float* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------
@@ -181,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                 cp_async_wait();
                 for (int i = tid; i < C::WINDOW * BN; i += 128) {
                     const int b = kb + i / BN;
-                    if (b < kb1) own[i] *= __ldg(g.sw + (size_t)nb * g.kb + b);
+                    if (b < kb1) own[i] *= ld_chain(g.sw + (size_t)nb * g.kb + b);
                 }
                 epilogue_barrier();
                 if (kb + C::WINDOW < kb1) fetch(w + 1);
@@ -224,8 +209,8 @@ __global__ void __launch_bounds__(kThreads, 2)
     const bool mine = warp >= 2 && ok && n < g.N;
     float bias = 0.f, gate = 1.f;
     if (mine) {
-        if (g.bias) bias = g.bias[n];
-        if (g.gate) gate = g.gate[n];
+        if (g.bias) bias = ld_chain(g.bias + n);
+        if (g.gate) gate = ld_chain(g.gate + n);
     }
     auto put = [&](int c, float v) {
         const int m = m0 + c;
@@ -300,8 +285,8 @@ wdc_status launch(Ctx* c, const void* A, const void* W, Gemm8Args g, cudaStream_
     if (tiles * g.split > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp8 GEMM: more than 2^31 - 1 thread blocks");
     CUtensorMap tw, ta;
     std::string why;
-    if (!encode_tmap_bytes(&tw, W, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.K, kBlock, 128, &why) ||
-        !encode_tmap_bytes(&ta, A, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.K, kBlock, bn, &why))
+    if (!encode_tmap_2d(&tw, W, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.K, kBlock, 128, &why, CU_TENSOR_MAP_DATA_TYPE_UINT8) ||
+        !encode_tmap_2d(&ta, A, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.K, kBlock, bn, &why, CU_TENSOR_MAP_DATA_TYPE_UINT8))
         return fail(c, WDC_ERR_CUDA, why);
     {
         OverlapScope ov(c, s);
@@ -327,9 +312,10 @@ wdc_status op_gemm_fp8(Ctx* c, const void* A, const float* a_scale, const void* 
          (uintptr_t)res | (uintptr_t)gate) & 15)
         return fail(c, WDC_ERR_INVALID_ARG, "fp8 GEMM: pointers must be 16-byte aligned");
     Gemm8Args g{};
-    g.M = M; g.N = N; g.K = K; g.kb = (K + kBlock - 1) / kBlock;
+    g.M = M; g.N = N; g.K = K; g.kb = (K + kBlock - 1) / kBlock; g.sw_rows = (N + 127) / 128;
     g.sa = a_scale; g.sw = w_scale; g.bias = bias; g.gate = res ? gate : nullptr; g.res = res; g.out = C; g.gelu = gelu;
     g.err = c->err;
+    if (M >= 512) return launch_gemm8_pair(c, A, W, g, 256, s);
     return c->cfg.dtype == WDC_BF16 ? launch<__nv_bfloat16>(c, A, W, g, s) : launch<float>(c, A, W, g, s);
 }
 
