@@ -4,10 +4,9 @@
 // V fp16 in pages [page][d] of a key head; S = Q K^T in fp32, P in fp16, O and the
 // row sums in fp32; d = 64 or 128.
 //
-// One CTA per (sequence, key head, block of query rows), 12 warps in three
-// warpgroups as in the dense attention (attn_tc.cu): a TMA producer and two MMA
-// issuers with few registers, two softmax warpgroups of one thread a row.  What
-// differs:
+// One CTA per (sequence, key head, block of query rows) or a part of its keys, with
+// the roles of the dense attention (attn_tc.cu): a TMA producer, an MMA issuer and
+// a softmax warpgroup of one thread a row for each tile.  What differs:
 //  * Rows are (token, query head of the key head's group), token-major: a tile
 //    of 128 rows is 128 / G tokens of all G heads of a group, one TMA box of the
 //    packed q.  A single token's group shares one read of the cache.
@@ -24,8 +23,9 @@
 //  * Each row has a limit of its own.  A row that has seen nothing yet takes the
 //    next tile's maximum as its exponent base, as at the first step.
 //  * Row sums add the fp16 probabilities in fp32 (mixed-precision adds).
-// Where the units are fewer than the SMs, each is split over its keys into
-// g.split CTAs, whose partial rows paged_combine_kernel merges in order.
+// Where there are few units, each is split over its keys into parts of equal
+// numbers of steps (find_item), which the last of them to be done (one tile) or a second kernel
+// (two) merges in order.
 #include "attn_softmax.cuh"
 #include "dit_kernels.cuh"
 #include "paged_index.h"
@@ -37,25 +37,31 @@ namespace wdc {
 
 namespace {
 
-constexpr int BQ = 128;                // rows a tile, two tiles a CTA
-constexpr uint32_t kRegsLaunch = 168;  // 65536 / 384 rounded down to a multiple of 8
+constexpr int BQ = 128;                // rows a tile
 
-template <int D>
+// NT tiles a CTA.  Two: chunks, 12 warps, one CTA an SM.  One: chunks whose rows
+// fit a tile (single tokens above all), 8 warps, two CTAs an SM, so that one
+// streams the cache while the other starts or ends.
+template <int D, int NT>
 struct PagedCfg {
-    static constexpr int BK = D == 64 ? 128 : 64;           // keys a step
-    static constexpr int THREADS = 384;
-    static constexpr int ATOMS = D / 64;                    // 128-byte atoms along d
+    static constexpr int BK = (NT == 2 ? 128 : 64) * 64 / D;   // keys a step
+    static constexpr int THREADS = 128 * (1 + NT);
+    static constexpr int ATOMS = D / 64;                       // 128-byte atoms along d
     static constexpr uint32_t Q_TILE = BQ * D * 2;
     static constexpr uint32_t K_TILE = BK * D * 2;
-    static constexpr uint32_t STAGE = 2 * K_TILE;           // 32 KB for both head sizes
-    static constexpr int STAGES = 5;
-    static constexpr uint32_t SMEM = 2 * Q_TILE + STAGES * STAGE + 1024 + 256;
-    static constexpr uint32_t TMEM_COLS = 512;
+    static constexpr uint32_t STAGE = 2 * K_TILE;              // 32 KB, or 16 KB for one tile
+    static constexpr int STAGES = NT == 2 ? 5 : (D == 64 ? 5 : 4);
+    static constexpr uint32_t SMEM = NT * Q_TILE + STAGES * STAGE + 1024 + 256;
+    static constexpr uint32_t TMEM_COLS = NT == 2 ? 512 : 256;
+    static constexpr int CTAS = 3 - NT;                        // an SM
+    static constexpr int MIN_STEPS = 8;                        // of a part of a split unit
+    // two tiles: registers a thread, 168 at launch (65536 / 384, a multiple of 8),
+    // of which the control warpgroup hands most to the softmax warpgroups
     static constexpr uint32_t REGS_CONTROL = 40;
     static constexpr uint32_t REGS_SOFTMAX = 232;
-    static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= 384 * kRegsLaunch, "register split exceeds the launch");
-    static_assert(2 * (BK + BK / 2 + D) <= (int)TMEM_COLS, "S, P and O of two tiles exceed tensor memory");
-    static_assert(SMEM <= 227 * 1024, "shared memory per CTA");
+    static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= 384 * 168, "register split exceeds the launch");
+    static_assert(NT * (BK + BK / 2 + D) <= (int)TMEM_COLS, "S, P and O exceed tensor memory");
+    static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
     __device__ static constexpr uint32_t s_col(int t) { return (uint32_t)(BK + BK / 2 + D) * t; }
     __device__ static constexpr uint32_t p_col(int t) { return s_col(t) + BK; }
     __device__ static constexpr uint32_t o_col(int t) { return s_col(t) + BK + BK / 2; }
@@ -63,38 +69,228 @@ struct PagedCfg {
 
 struct PagedArgs {
     int T, heads, kv, G, tpt;          // G query heads a key head, tpt tokens a tile
-    int q_blocks, max_new, split;
+    int sequences, q_blocks, max_new;  // q_blocks: of max_new tokens
+    int items, wave;                   // most parts of units (0: none is split); parts that run at a time
     int page_log2, pages, width, frame;
     const int *table, *length, *start;
     float scale_log2;
     __nv_bfloat16* o;
-    float* part_o;                     // [unit][split][256 rows][d]
-    float2* part_ml;                   // [unit][split][256 rows] base, row sum
+    float* part_o;                     // [item][rows_unit][d]
+    float2* part_ml;                   // [item][rows_unit] base, row sum
+    int rows_unit;                     // rows of a unit (host's bound)
+    unsigned* counter;                 // one tile: [item] parts of a split unit that are done; 0 between launches
+    int4* record;                      // two tiles: [item] sequence, head, query block and parts of a split unit at its first part's
     unsigned* err;
 };
 
-// A unit: sequence, key head, query block; the blocks with the most keys first.
-struct Unit : PagedSeq {
-    int b, h, qb;
-    __device__ Unit(const PagedArgs& g, int u) {
-        qb = g.q_blocks - 1 - u % g.q_blocks;
-        const int r = u / g.q_blocks;
-        h = r % g.kv;
-        b = r / g.kv;
-        static_cast<PagedSeq&>(*this) = paged_seq(g.start[b], g.start[b + 1], g.length[b], g.T, g.width << g.page_log2);
-    }
+__device__ __forceinline__ PagedSeq sequence(const PagedArgs& g, int b) {
+    return paged_seq(g.start[b], g.start[b + 1], g.length[b], g.T, g.width << g.page_log2);
+}
+
+// A unit is (sequence, key head, block of NT * tpt tokens).  Where there are so
+// few that whole units would leave SMs without work, or units of different
+// lengths, each is split into parts of `chunk` steps: the fewest for which all
+// parts run in k rounds of the SMs, with the k = 1 .. kRounds of the least
+// estimated time, if that is less than the whole units'.  Estimates are in steps:
+// kStart a part for its start and end, kMerge for merging parts.  One tile is bound
+// by memory, whose bandwidth few CTAs fill too (0.55: one step's time of a lone
+// CTA); of two tiles, units of like length take whole rounds, others fill the gaps
+// that the longest leave.  The lengths are the device's, so the first warp of each CTA works the plan out, two
+// sequences a lane, in whole numbers as floats (exact below 2^24).  (A kernel of
+// its own for the plan and one for the merging cost 10 of 48 us at one token of 32
+// heads over 32000.)
+constexpr int kRounds = 3;
+constexpr int kPlanned = 2;            // sequences a lane; more than 32 of these are not split
+
+// What a CTA does: part `part` of `parts` of a unit.  The blocks with the most keys
+// come first within a head.
+struct Item : PagedSeq {
+    int b, h, qb, part, parts, chunk;
+    int slot;                          // of the unit's first part in the plan: where its workspace rows begin
 };
 
+template <int D, int NT>
+__device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
+    constexpr int BK = PagedCfg<D, NT>::BK, kMin = PagedCfg<D, NT>::MIN_STEPS;
+    constexpr float kStart = NT == 2 ? 8.f : 6.f, kMerge = NT == 2 ? 12.f : 8.f;
+    constexpr unsigned kAll = 0xffffffffu;
+    const int block = NT * g.tpt;
+    float with = 0.f;                  // steps a part; 0: whole units
+    float units[kPlanned], steps[kPlanned];
+    if (g.items > 0) {
+        float n = 0.f, work = 0.f, bound = 0.f, most = 0.f, least = 3e38f;
+#pragma unroll
+        for (int i = 0; i < kPlanned; ++i) {
+            const int b = 32 * i + lane;
+            units[i] = steps[i] = 0.f;
+            if (b < g.sequences) {
+                const PagedSeq s = sequence(g, b);
+                const int rows = min(s.n, g.max_new);
+                if (rows > 0) {
+                    const float low = (float)((paged_limit(s, g.frame, min(rows, block) - 1) + BK - 1) / BK);
+                    units[i] = (float)((rows + block - 1) / block * g.kv);
+                    steps[i] = (float)((paged_limit(s, g.frame, s.n - 1) + BK - 1) / BK);
+                    least = fminf(least, low);
+                    most = fmaxf(most, steps[i]);
+                    n += units[i];
+                    work += units[i] * 0.5f * (steps[i] + low);
+                    bound += units[i] * steps[i];
+                }
+            }
+        }
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) {
+            n += __shfl_xor_sync(kAll, n, o);
+            work += __shfl_xor_sync(kAll, work, o);
+            bound += __shfl_xor_sync(kAll, bound, o);
+            most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
+            least = fminf(least, __shfl_xor_sync(kAll, least, o));
+        }
+        const float wave = (float)g.wave;
+        const bool alike = 4.f * least >= 3.f * most;
+        auto estimate = [&](float c, float parts) {
+            const float rounds = ceilf(parts / wave);
+            if (NT == 1) return fmaxf(work / wave, 0.55f * c) + rounds * kStart;
+            return alike ? rounds * (c + kStart) : fmaxf(c, work / wave + 0.5f * c) + rounds * kStart;
+        };
+        float best = estimate(most, n) - kMerge;
+#pragma unroll 1
+        for (int k = 1; k <= kRounds && most > (float)kMin; ++k) {
+            const float items = (float)min(k * g.wave, g.items);
+            if (n >= items) continue;
+            // sum u ceil(s / c) lies between sum u s / c and that + n
+            float lo = fminf(most, fmaxf((float)kMin, floorf(bound / items)));
+            float hi = fminf(most, fmaxf(lo, ceilf(bound / (items - n)) + 1.f)), c, parts;
+#pragma unroll 1
+            do {
+                c = lo < hi ? floorf(0.5f * (lo + hi)) : lo;
+                parts = 0.f;
+#pragma unroll
+                for (int i = 0; i < kPlanned; ++i) parts += units[i] * fmaxf(1.f, ceilf(steps[i] / c));
+                parts = (float)__reduce_add_sync(kAll, (unsigned)parts);
+                if (lo == hi) break;
+                if (parts <= items) hi = c;
+                else lo = c + 1.f;
+            } while (true);
+            const float est = estimate(c, parts);
+            if (c < most && parts <= items && est < best) {
+                best = est;
+                with = c;
+            }
+        }
+    }
+    if (with == 0.f) {                 // whole units in order, some of them empty
+        const int r = index / g.q_blocks;
+        it.qb = g.q_blocks - 1 - index % g.q_blocks;
+        it.h = r % g.kv;
+        it.b = r / g.kv;
+        if (it.b >= g.sequences) return false;
+        static_cast<PagedSeq&>(it) = sequence(g, it.b);
+        it.part = it.slot = 0;
+        it.parts = 1;
+        it.chunk = INT_MAX;
+        return it.qb * block < it.n;
+    }
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanned; ++i) {
+        const int mine = (int)fmaxf(1.f, ceilf(steps[i] / with)), n = (int)units[i] * mine;
+        int sum = n;                   // inclusive over the lanes
+#pragma unroll 1
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(kAll, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const unsigned past = __ballot_sync(kAll, before + sum > index);
+        if (past) {
+            const int at = __ffs(past) - 1;
+            const int r = index - before - __shfl_sync(kAll, sum - n, at);
+            it.b = 32 * i + at;
+            it.parts = __shfl_sync(kAll, mine, at);
+            static_cast<PagedSeq&>(it) = sequence(g, it.b);
+            const int nq = (min(it.n, g.max_new) + block - 1) / block, unit = r / it.parts;
+            it.part = r - unit * it.parts;
+            it.h = unit / nq;
+            it.qb = nq - 1 - (unit - it.h * nq);
+            it.chunk = (int)with;
+            it.slot = index - it.part;
+            return true;
+        }
+        before += __shfl_sync(kAll, sum, 31);
+    }
+    return false;
+}
+
+template <int N>
+__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory"); }
+
+// Merges the parts of a unit's rows, in the parts' order: o = sum_p 2^(m_p - m) O_p /
+// sum_p 2^(m_p - m) l_p with m the largest base so far.  D / 4 lanes a row, rows
+// w, w + step, ... of the unit's by this warp; AHEAD parts loaded at a time (past
+// L1, which may hold the workspace's earlier contents).
+template <int D, int NT>
+__device__ __forceinline__ void merge_parts(const PagedArgs& g, const Item& un, int w, int step, int lane) {
+    constexpr int LANES = D / 4, ROWS = 32 / LANES, AHEAD = NT == 1 ? 8 : 4;
+    const int tok0 = un.qb * NT * g.tpt, rows = min(min(un.n, g.max_new) - tok0, NT * g.tpt) * g.G;
+    const int col = (lane % LANES) * 4;
+    for (int r = w * ROWS + lane / LANES; r < rows; r += step * ROWS) {
+        const size_t p0 = (size_t)un.slot * g.rows_unit + r;
+        float m = -INFINITY, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < un.parts; p += AHEAD) {
+            float2 ml[AHEAD];
+            float4 v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const size_t row = p0 + (size_t)min(p + k, un.parts - 1) * g.rows_unit;
+                ml[k] = __ldcg(g.part_ml + row);
+                v[k] = __ldcg(reinterpret_cast<const float4*>(g.part_o + row * D + col));
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (p + k >= un.parts || ml[k].x == -INFINITY) continue;     // (saw nothing)
+                const float top = fmaxf(m, ml[k].x), a = ex2(m - top), b = ex2(ml[k].x - top);
+                l = l * a + ml[k].y * b;
+                acc.x = acc.x * a + v[k].x * b;
+                acc.y = acc.y * a + v[k].y * b;
+                acc.z = acc.z * a + v[k].z * b;
+                acc.w = acc.w * a + v[k].w * b;
+                m = top;
+            }
+        }
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
+        const size_t t = (size_t)un.row0 + tok0 + r / g.G;
+        *reinterpret_cast<uint2*>(g.o + (t * g.heads + un.h * g.G + r % g.G) * D + col) =
+            make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    }
+}
+
+// Two tiles: the merging of a split unit's rows is work for more than one CTA.
 template <int D>
-__global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
+__global__ void __launch_bounds__(256) paged_merge_kernel(const __grid_constant__ PagedArgs g) {
+    chain_release();
+    chain_wait();
+    const int4 rec = g.record[blockIdx.x];
+    if (rec.w < 2) return;
+    Item un;
+    static_cast<PagedSeq&>(un) = sequence(g, rec.x);
+    un.h = rec.y;
+    un.qb = rec.z;
+    un.parts = rec.w;
+    un.slot = blockIdx.x;
+    merge_parts<D, 2>(g, un, blockIdx.y * 8 + (threadIdx.x >> 5), gridDim.y * 8, threadIdx.x & 31);
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTAS)
     attn_paged_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                       const __grid_constant__ CUtensorMap tv, const __grid_constant__ PagedArgs g) {
-    using C = PagedCfg<D>;
+    using C = PagedCfg<D, NT>;
     constexpr int BKV = C::BK;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* sq = smem;                                       // [2 tiles][ATOMS][128 x 128 B]
-    uint8_t* skv = smem + 2 * C::Q_TILE;                      // [STAGES][K | V], each [ATOMS][BK x 128 B]
+    uint8_t* sq = smem;                                       // [NT tiles][ATOMS][128 x 128 B]
+    uint8_t* skv = smem + NT * C::Q_TILE;                     // [STAGES][K | V], each [ATOMS][BK x 128 B]
     uint64_t* bars = reinterpret_cast<uint64_t*>(skv + C::STAGES * C::STAGE);
     uint64_t* q_full = bars;
     uint64_t* kv_full = q_full + 1;
@@ -105,16 +301,19 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
     uint64_t* p_free = p_full + 2;                            // [2]
     uint64_t* o_final = p_free + 2;                           // [2]
     uint64_t* v_ready = o_final + 2;                          // the last step's V is clear behind the sequence
-    uint64_t* mma_done = v_ready + 1;
+    uint64_t* stagger = v_ready + 1;                          // tile 0 has stored its first P
+    uint64_t* mma_done = stagger + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
-    if (threadIdx.x == 0) {
+    __shared__ Item s_item;
+    __shared__ int s_has, s_last;
+    if (threadIdx.x == 64) {
         mbar_init(q_full, 1);
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(&kv_full[s], 1);
-            mbar_init(&kv_empty[s], 2);        // each MMA issuer's, or the one's and the producer's
+            mbar_init(&kv_empty[s], NT);       // each MMA issuer's, or the one's and the producer's
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(&s_full[w], 1);
@@ -124,34 +323,57 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             mbar_init(&o_final[w], 1);
         }
         mbar_init(v_ready, 1);
-        mbar_init(mma_done, 2);
+        mbar_init(stagger, 4);
+        mbar_init(mma_done, NT);
         *abort_flag = 0;
         fence_barrier_init();
-    }
-    if (warp == 0 && lane == 0) {
         prefetch_tmap(&tq);
         prefetch_tmap(&tk);
         prefetch_tmap(&tv);
     }
-    if (warp == 1) {
+    // (a CTA past the first round may have nothing to do: it asks before it allocates)
+    const bool early = blockIdx.x < (unsigned)g.wave;
+    if (warp == 1 && early) {
         tmem_alloc(tmem_slot, C::TMEM_COLS);
         tmem_relinquish();
     }
+    chain_wait();
+    if (warp == 0) {
+        Item it{};
+        const bool has = find_item<D, NT>(g, blockIdx.x, lane, it);
+        if (lane == 0) {
+            s_item = it;
+            s_has = has;
+            if (NT == 2 && (int)blockIdx.x < g.items)
+                g.record[blockIdx.x] = make_int4(it.b, it.h, it.qb, has && it.part == 0 ? it.parts : 0);
+        }
+    }
     __syncthreads();
+    if (!s_has) {
+        if (warp == 1 && early) {
+            tc_fence_after();
+            tmem_dealloc(*tmem_slot, C::TMEM_COLS);
+        }
+        return;
+    }
+    if (!early) {
+        if (warp == 1) {
+            tmem_alloc(tmem_slot, C::TMEM_COLS);
+            tmem_relinquish();
+        }
+        __syncthreads();
+    }
     tc_fence_after();
     chain_release();
-    chain_wait();
     const uint32_t tmem = *tmem_slot;
+    const Item un = s_item;
 
-    const int u = blockIdx.x / g.split, part = blockIdx.x - u * g.split;
-    const Unit un(g, u);
-    const int tok0 = un.qb * 2 * g.tpt;                       // the chunk's first token here
-    const bool idle = tok0 >= un.n;
-    const int nt = tok0 + g.tpt < un.n ? 2 : 1;               // tiles with rows
-    const int keys = idle ? 0 : paged_limit(un, g.frame, min(tok0 + 2 * g.tpt, un.n) - 1);
+    const int tok0 = un.qb * NT * g.tpt;                      // the chunk's first token here
+    const int nt = NT == 2 && tok0 + g.tpt < un.n ? 2 : 1;    // tiles with rows
+    const int keys = paged_limit(un, g.frame, min(tok0 + NT * g.tpt, un.n) - 1);
     const int steps = (keys + BKV - 1) / BKV;
-    const int j0 = (int)((long long)part * steps / g.split);
-    const int nj = (int)((long long)(part + 1) * steps / g.split) - j0;
+    const int j0 = un.parts > 1 ? min(un.part * un.chunk, steps) : 0;
+    const int nj = (un.parts > 1 ? min(j0 + un.chunk, steps) : steps) - j0;
     const int page = 1 << g.page_log2;
     const int used = (un.len + page - 1) >> g.page_log2;      // pages of the sequence
     // rows of the last step's V that lie behind the sequence, in its last page
@@ -160,9 +382,9 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
     const bool clear = nj > 0 && clear0 < clear1;
 
     if (wg == 0) {
-        setmaxnreg_dec<C::REGS_CONTROL>();
+        if constexpr (NT == 2) setmaxnreg_dec<C::REGS_CONTROL>();
         if (warp == 0) {
-            if (part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
+            if (un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
                 const int given = g.length[un.b];
                 if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
             }
@@ -200,7 +422,7 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
                     if (!mbar_wait_warp(&kv_empty[stage], phase ^ 1u, abort_flag, g.err)) { ok = false; break; }
                     if (elect_one()) {
                         mbar_arrive_expect_tx(&kv_full[stage], C::STAGE);
-                        if (nt == 1) mbar_arrive(&kv_empty[stage]);
+                        if (NT == 2 && nt == 1) mbar_arrive(&kv_empty[stage]);
                     }
                     __syncwarp();
                     if (lane < boxes) {
@@ -241,10 +463,10 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
                     }
                 }
             }
-        } else if ((warp == 1 || (warp == 2 && nt == 2)) && nj > 0) {
+        } else if (((NT == 1 && warp == 1) || (NT == 2 && warp - 1 < nt && warp <= 2)) && nj > 0) {
             constexpr uint32_t idesc_s = idesc_bf16(BQ, BKV);
             constexpr uint32_t idesc_o = idesc_f16_mn(BQ, D);    // P (fp16, TMEM) x V (fp16, MN-major)
-            const int t = warp - 1;
+            const int t = NT == 1 ? 0 : warp - 1;
             constexpr bool kOneLane = D == 128;                  // (as in the dense attention)
             auto leads = [] { return kOneLane || elect_one(); };
             auto rejoin = [] { if (!kOneLane) __syncwarp(); };
@@ -269,6 +491,8 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
                         tc_mma_ts(tmem + C::o_col(t), tmem + C::p_col(t) + ks * 8, sdesc_at(dv, st * C::STAGE + ks * 2048),
                                   idesc_o, (acc || ks != 0) ? 1u : 0u);
                 };
+                // tiles half a step apart (as in the dense attention), from two steps on
+                if (t == 1 && nj > 1) ok = ok && mbar_wait(stagger, 0, abort_flag, g.err);
                 ok = ok && mbar_wait(&kv_full[0], 0, abort_flag, g.err);
                 for (int j = 0; j < nj; ++j) {
                     // here K(j) has landed, and S(t, j - 1) is in the softmax's registers
@@ -307,7 +531,7 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
                 rejoin();
                 if (leads()) {
                     tc_commit(mma_done);
-                    if (nt == 1) mbar_arrive(mma_done);
+                    if (NT == 2 && nt == 1) mbar_arrive(mma_done);
                 }
             }
             __syncwarp();
@@ -316,7 +540,7 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             }
         }
     } else {
-        setmaxnreg_inc<C::REGS_SOFTMAX>();
+        if constexpr (NT == 2) setmaxnreg_inc<C::REGS_SOFTMAX>();
         // softmax warpgroups: t = tile, quarter = TMEM lane quarter
         const int t = wg - 1;
         const int quarter = warp & 3;
@@ -326,7 +550,7 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
         const uint32_t p_addr = tmem + lane_base + C::p_col(t);
         const uint32_t o_addr = tmem + lane_base + C::o_col(t);
         const int i = tok0 + t * g.tpt + row / g.G;          // the chunk's token
-        const bool valid = !idle && row < g.tpt * g.G && i < un.n;
+        const bool valid = row < g.tpt * g.G && i < min(un.n, g.max_new);
         const int lim = valid ? paged_limit(un, g.frame, i) : INT_MAX;    // (other rows hold what they hold)
         const int min_lim = __reduce_min_sync(0xffffffffu, lim);
         const bool work = __any_sync(0xffffffffu, valid);    // else the warp only keeps step
@@ -340,7 +564,10 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             if (!work) {
                 if (lane == 0) mbar_arrive(&s_free[t]);
                 if (j > 0 && !mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) { ok = false; break; }
-                if (lane == 0) mbar_arrive(&p_full[t]);
+                if (lane == 0) {
+                    mbar_arrive(&p_full[t]);
+                    if (NT == 2 && j == 0 && t == 0) mbar_arrive(stagger);
+                }
                 continue;
             }
             float s[BKV];
@@ -353,6 +580,7 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             if (lane == 0) mbar_arrive(&s_free[t]);
             const int k0 = (j0 + j) * BKV;
             if (min_lim - k0 < BKV) {
+                asm volatile("");                            // a branch, not a select for each score of every step
                 const int left = lim - k0;
 #pragma unroll
                 for (int c = 0; c < BKV; ++c)
@@ -428,15 +656,18 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[t]);
+            if (lane == 0) {
+                mbar_arrive(&p_full[t]);
+                if (NT == 2 && j == 0 && t == 0) mbar_arrive(stagger);
+            }
             if (D == 64) s_ready = __all_sync(0xffffffffu, next);
         }
         if (ok && mine > 0) ok = mbar_wait_warp(&o_final[t], 0, abort_flag, g.err);
         if (ok && work) {
             tc_fence_after();
             const bool seen = l_run != 0.f;                  // (a NaN is seen)
-            const bool split = g.split > 1;
-            const size_t prow = ((size_t)blockIdx.x * 2 + t) * BQ + row;
+            const bool split = un.parts > 1;
+            const size_t prow = (size_t)(un.slot + un.part) * g.rows_unit + t * g.tpt * g.G + row;
             const float inv = seen ? 1.0f / l_run : 0.f;
             __nv_bfloat16* out = g.o + ((size_t)(un.row0 + i) * g.heads + un.h * g.G + row % g.G) * D;
             float* po = g.part_o + prow * D;
@@ -450,12 +681,12 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
                 }
                 if (!valid) continue;
                 if (split) {
-                    if (!seen) continue;
                     float4* dst = reinterpret_cast<float4*>(po + c);
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        dst[q] = make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
-                                             __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]));
+                        dst[q] = seen ? make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
+                                                    __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]))
+                                      : make_float4(0.f, 0.f, 0.f, 0.f);
                 } else {
                     uint4* dst = reinterpret_cast<uint4*>(out + c);
 #pragma unroll
@@ -473,6 +704,19 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
             }
         }
         tc_fence_before();
+        if (NT == 1 && un.parts > 1) {
+            // the last of a unit's parts to be done merges them
+            __threadfence();
+            softmax_barrier<NT * 128>();
+            if (threadIdx.x == 128) {
+                unsigned* counter = g.counter + un.slot;
+                const bool last = atomicInc(counter, (unsigned)un.parts - 1u) == (unsigned)un.parts - 1u;
+                __threadfence();
+                s_last = last;
+            }
+            softmax_barrier<NT * 128>();
+            if (s_last) merge_parts<D, NT>(g, un, warp - 4, NT * 4, lane);
+        }
     }
     __syncthreads();
     if (warp == 1) {
@@ -481,52 +725,17 @@ __global__ void __launch_bounds__(PagedCfg<D>::THREADS, 1)
     }
 }
 
-// Merges the parts of each row, in order: one warp a row, lane l owning columns
-// l, l + 32, ...: o = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, m = max m_p.
-template <int D>
-__global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constant__ PagedArgs g, int rows_unit, int units) {
-    chain_release();
-    chain_wait();
-    const long long w = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    const int u = (int)(w / rows_unit), r = (int)(w - (long long)u * rows_unit);
-    if (u >= units) return;
-    const Unit un(g, u);
-    const int ti = r / g.G, i = un.qb * 2 * g.tpt + ti;
-    if (i >= un.n) return;
-    const int t = ti / g.tpt, row = (ti - t * g.tpt) * g.G + r % g.G;
-    float m = -INFINITY;
-    const size_t p0 = ((size_t)u * g.split * 2 + t) * BQ + row;      // part p lies p * 2 * BQ rows on
-    for (int p = 0; p < g.split; ++p) m = fmaxf(m, g.part_ml[p0 + (size_t)p * 2 * BQ].x);
-    float l = 0.f, acc[D / 32];
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) acc[c] = 0.f;
-    for (int p = 0; p < g.split; ++p) {
-        const size_t prow = p0 + (size_t)p * 2 * BQ;
-        const float2 ml = g.part_ml[prow];
-        if (ml.x == -INFINITY) continue;                             // saw nothing: has no O
-        const float f = ex2(ml.x - m);
-        l = fmaf(ml.y, f, l);
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) acc[c] = fmaf(f, g.part_o[prow * D + lane + 32 * c], acc[c]);
-    }
-    const float inv = l != 0.f ? 1.0f / l : 0.f;
-    __nv_bfloat16* out = g.o + ((size_t)(un.row0 + i) * g.heads + un.h * g.G + r % g.G) * D;
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) out[lane + 32 * c] = __float2bfloat16_rn(acc[c] * inv);
-}
-
-template <int D>
+template <int D, int NT>
 wdc_status launch(Ctx* c, const void* q, const wdc_paged_cache* p, PagedArgs g, cudaStream_t s) {
-    using Cf = PagedCfg<D>;
+    using Cf = PagedCfg<D, NT>;
     static PerDevice<bool> fits;
     const bool regs_ok = fits.get(c->device, [](bool& ok) {
-        const bool smem = allow_smem(attn_paged_kernel<D>, Cf::SMEM);
+        const bool smem = allow_smem(attn_paged_kernel<D, NT>, Cf::SMEM);
         // the warpgroups' register requests must fit the launch allocation,
         // or setmaxnreg.inc would wait forever: refuse to launch otherwise
         cudaFuncAttributes fa;
-        ok = cudaFuncGetAttributes(&fa, attn_paged_kernel<D>) == cudaSuccess && fa.maxThreadsPerBlock >= Cf::THREADS &&
-             (uint32_t)fa.numRegs * Cf::THREADS >= 128 * Cf::REGS_CONTROL + 256 * Cf::REGS_SOFTMAX;
+        ok = cudaFuncGetAttributes(&fa, attn_paged_kernel<D, NT>) == cudaSuccess && fa.maxThreadsPerBlock >= Cf::THREADS &&
+             (NT == 1 || (uint32_t)fa.numRegs * Cf::THREADS >= 128 * Cf::REGS_CONTROL + 256 * Cf::REGS_SOFTMAX);
         cudaGetLastError();
         return smem && ok;
     });
@@ -542,31 +751,39 @@ wdc_status launch(Ctx* c, const void* q, const wdc_paged_cache* p, PagedArgs g, 
         !encode_tmap_4d(&tv, p->v, kd, ks, kb, true, &why))
         return fail(c, WDC_ERR_CUDA, why);
     g.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
-    g.q_blocks = (g.max_new + 2 * g.tpt - 1) / (2 * g.tpt);
-    const long long units = (long long)p->sequences * g.kv * g.q_blocks;
+    const int block = NT * g.tpt;
+    g.q_blocks = (g.max_new + block - 1) / block;
+    const long long units = (long long)g.sequences * g.kv * g.q_blocks;
     if (units > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "paged attention: more than 2^31 - 1 thread blocks");
-    const long long steps = (((long long)g.width << g.page_log2) + Cf::BK - 1) / Cf::BK;
-    g.split = 1;
-    // (the workspace holds the partial rows of num_sms CTAs a sample)
-    if (c->attn_part && 2 * units <= c->num_sms) {
-        long long sp = c->num_sms / units;
-        if (sp > steps / 2) sp = steps / 2;
-        g.split = sp > 1 ? (int)sp : 1;
+    // (the workspace holds the partial rows of a few rounds of CTAs)
+    g.rows_unit = (g.max_new < block ? g.max_new : block) * g.G;
+    g.wave = Cf::CTAS * c->num_sms;
+    const long long room = (long long)c->num_sms * 256 * c->attn_part_rounds / g.rows_unit;
+    // rounds of parts: the fewest that like units would fill by nine tenths; two or
+    // more where sequences may differ
+    long long items = 0;
+    for (int k = g.sequences > 1 ? 2 : 1; k <= kRounds; ++k) {
+        items = (long long)k * g.wave;
+        if (units > 0 && 10 * (items / units * units) >= 9 * items) break;
     }
+    if (items > room) items = room / g.wave * g.wave;
+    const long long steps = (((long long)g.width << g.page_log2) + Cf::BK - 1) / Cf::BK;
+    g.items = c->attn_part && g.sequences <= 32 * kPlanned && steps > Cf::MIN_STEPS && units < items ? (int)items : 0;
+    g.counter = c->attn_counters;
+    g.record = reinterpret_cast<int4*>(c->attn_records);
     g.part_o = c->attn_part;
     g.part_ml = reinterpret_cast<float2*>(c->attn_ml);
+    const long long grid = g.items > units ? g.items : units;      // (parts, or whole units)
     OverlapScope ov(c, s);
     {
         LaunchScope ls(c, WDC_K_ATTN, s);
-        launch_kernel(attn_paged_kernel<D>, dim3((unsigned)(units * g.split)), Cf::THREADS, Cf::SMEM, s, 1, tq, tk, tv, g);
+        launch_kernel(attn_paged_kernel<D, NT>, dim3((unsigned)grid), Cf::THREADS, Cf::SMEM, s, 1, tq, tk, tv, g);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention launch: ") + cudaGetErrorString(e));
-    if (g.split > 1) {
-        const int tokens = g.max_new < 2 * g.tpt ? g.max_new : 2 * g.tpt;
-        const long long rows = units * tokens * g.G;
+    if (NT == 2 && g.items > 0) {
         LaunchScope ls(c, WDC_K_OTHER, s);
-        launch_kernel(paged_combine_kernel<D>, dim3((unsigned)((rows + 7) / 8)), 256, 0, s, 1, g, tokens * g.G, (int)units);
+        launch_kernel(paged_merge_kernel<D>, dim3((unsigned)g.items, 16), 256, 0, s, 1, g);
         e = cudaGetLastError();
         if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention merge launch: ") + cudaGetErrorString(e));
     }
@@ -592,7 +809,9 @@ wdc_status op_attention_paged(Ctx* c, const void* q, const wdc_paged_cache* p, c
     g.table = p->table; g.length = p->length; g.start = q_start;
     g.o = reinterpret_cast<__nv_bfloat16*>(o);
     g.err = c->err;
-    return p->head_dim == 64 ? launch<64>(c, q, p, g, s) : launch<128>(c, q, p, g, s);
+    g.sequences = p->sequences;
+    if (g.max_new <= g.tpt) return p->head_dim == 64 ? launch<64, 1>(c, q, p, g, s) : launch<128, 1>(c, q, p, g, s);
+    return p->head_dim == 64 ? launch<64, 2>(c, q, p, g, s) : launch<128, 2>(c, q, p, g, s);
 }
 
 }  // namespace wdc

@@ -1024,9 +1024,14 @@ wdc_status dit_create(Ctx* c) {
     if ((s = dalloc(c, (void**)&t->temb, (size_t)t->E * sizeof(float)))) return s;
     if ((s = dalloc(c, (void**)&t->mods, t->mod_rows * sizeof(float)))) return s;
     if (t->dtype == WDC_BF16) {
-        const size_t rows = (size_t)t->B * c->num_sms * 256;
+        c->attn_part_rounds = t->B > 3 ? t->B : 3;           // (a paged attention's parts run in up to three)
+        const size_t rows = (size_t)c->attn_part_rounds * c->num_sms * 256;
         if ((s = dalloc(c, (void**)&c->attn_part, rows * 128 * sizeof(float)))) return s;
         if ((s = dalloc(c, (void**)&c->attn_ml, rows * 2 * sizeof(float)))) return s;
+        const size_t counters = 3 * 2 * (size_t)c->num_sms * sizeof(unsigned);   // (three rounds of two CTAs an SM)
+        if ((s = dalloc(c, (void**)&c->attn_counters, counters))) return s;
+        if ((s = dalloc(c, &c->attn_records, 3 * (size_t)c->num_sms * 16))) return s;
+        if (cudaMemset(c->attn_counters, 0, counters) != cudaSuccess) return fail(c, WDC_ERR_CUDA, "DiT init: attention counters");
         c->attn_part_samples = t->B;
     }
     const long long npe = (long long)t->Lv * t->D;
@@ -1048,6 +1053,9 @@ void dit_destroy(Ctx* c) {
     c->attn_part = nullptr;
     c->attn_ml = nullptr;
     c->attn_part_samples = 0;
+    c->attn_part_rounds = 0;
+    c->attn_counters = nullptr;
+    c->attn_records = nullptr;
 }
 
 static uint16_t f32_to_bf16_bits(float f) {

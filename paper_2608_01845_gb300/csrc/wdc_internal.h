@@ -170,12 +170,14 @@ struct Ctx {
 
     // denoiser
     struct DiT* dit = nullptr;
-    // split-key attention partials of a sample's last round (bf16 models):
-    // per sample of the batch, unnormalised O rows [num_sms x 256][128] and
-    // (base, row sum) pairs
+    // split-key attention partials (bf16 models): unnormalised O rows
+    // [num_sms x 256][128] and (base, row sum) pairs, of attn_part_rounds rounds of
+    // CTAs (the dense attention uses one a sample of the batch)
     float* attn_part = nullptr;
     float* attn_ml = nullptr;
-    int attn_part_samples = 0;
+    int attn_part_samples = 0, attn_part_rounds = 0;
+    unsigned* attn_counters = nullptr; // a paged attention's units: parts done, 0 between launches
+    void* attn_records = nullptr;      // and, of two tiles, which of its parts are a split unit's first
 
     // graph rollout (device-side control flow), built on first use
     GraphRollout* grollout = nullptr;
