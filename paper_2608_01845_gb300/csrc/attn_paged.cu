@@ -32,6 +32,7 @@
 #include "ptx.cuh"
 
 #include <climits>
+#include <type_traits>
 
 namespace wdc {
 
@@ -57,8 +58,8 @@ struct PagedCfg {
     static constexpr int MIN_STEPS = 8;                        // of a part of a split unit
     // two tiles: registers a thread, 168 at launch (65536 / 384, a multiple of 8),
     // of which the control warpgroup hands most to the softmax warpgroups
-    static constexpr uint32_t REGS_CONTROL = 40;
-    static constexpr uint32_t REGS_SOFTMAX = 232;
+    static constexpr uint32_t REGS_CONTROL = D == 64 ? 40 : 88;
+    static constexpr uint32_t REGS_SOFTMAX = D == 64 ? 232 : 208;
     static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= 384 * 168, "register split exceeds the launch");
     static_assert(NT * (BK + BK / 2 + D) <= (int)TMEM_COLS, "S, P and O exceed tensor memory");
     static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
     if (threadIdx.x == 64) {
         mbar_init(q_full, 1);
         for (int s = 0; s < C::STAGES; ++s) {
-            mbar_init(&kv_full[s], 1);
+            mbar_init(&kv_full[s], 2);         // K's producer and V's
             mbar_init(&kv_empty[s], NT);       // each MMA issuer's, or the one's and the producer's
         }
         for (int w = 0; w < 2; ++w) {
@@ -336,6 +337,15 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
     if (warp == 1 && early) {
         tmem_alloc(tmem_slot, C::TMEM_COLS);
         tmem_relinquish();
+    }
+    if (warp >= 4) {                                          // rows of a tile that no box fills
+        const int row = threadIdx.x & 127;
+        if (row >= g.tpt * g.G) {
+            uint4* q = reinterpret_cast<uint4*>(sq + ((warp >> 2) - 1) * C::Q_TILE + row * 128);
+            for (int a = 0; a < C::ATOMS; ++a)
+                for (int i = 0; i < 8; ++i) q[a * (BQ * 8) + i] = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
     }
     chain_wait();
     if (warp == 0) {
@@ -383,13 +393,16 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
 
     if (wg == 0) {
         if constexpr (NT == 2) setmaxnreg_dec<C::REGS_CONTROL>();
-        if (warp == 0) {
-            if (un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
+        if (warp == 0 || warp == 3) {
+            // producers: warp 0 of Q and K, warp 3 of V (one for all three is behind
+            // with pages of 16: 16 boxes a step at d = 128)
+            const bool of_v = warp == 3;
+            if (!of_v && un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
                 const int given = g.length[un.b];
                 if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
             }
             if (nj > 0) {
-                if (elect_one()) {
+                if (!of_v && elect_one()) {
                     mbar_arrive_expect_tx(q_full, (uint32_t)(nt * C::ATOMS * g.G * g.tpt) * 128u);
                     for (int t = 0; t < nt; ++t)
                         for (int a = 0; a < C::ATOMS; ++a)
@@ -397,6 +410,8 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                                         un.row0 + tok0 + t * g.tpt);
                 }
                 __syncwarp();
+                const CUtensorMap* map = of_v ? &tv : &tk;
+                uint8_t* tile0 = skv + (of_v ? C::K_TILE : 0);
                 const int rows = min(page, BKV), boxes = BKV / rows;
                 // page of this lane's box of step j
                 auto lookup = [&](int j) {
@@ -421,25 +436,22 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                     if (j + 1 < j0 + nj) next = lookup(j + 1);
                     if (!mbar_wait_warp(&kv_empty[stage], phase ^ 1u, abort_flag, g.err)) { ok = false; break; }
                     if (elect_one()) {
-                        mbar_arrive_expect_tx(&kv_full[stage], C::STAGE);
-                        if (NT == 2 && nt == 1) mbar_arrive(&kv_empty[stage]);
+                        mbar_arrive_expect_tx(&kv_full[stage], C::K_TILE);
+                        if (NT == 2 && nt == 1 && !of_v) mbar_arrive(&kv_empty[stage]);
                     }
                     __syncwarp();
                     if (lane < boxes) {
-                        uint8_t* sk = skv + stage * C::STAGE + lane * rows * 128;
-                        const int y = (j * BKV) & (page - 1);
+                        uint8_t* dst = tile0 + stage * C::STAGE + lane * rows * 128;
+                        const int y = boxes > 1 ? 0 : (j * BKV) & (page - 1);
                         for (int a = 0; a < C::ATOMS; ++a)
-                            tma_load_4d(sk + a * (BKV * 128), &tk, &kv_full[stage], 64 * a, boxes > 1 ? 0 : y, un.h, p);
-                        for (int a = 0; a < C::ATOMS; ++a)
-                            tma_load_4d(sk + C::K_TILE + a * (BKV * 128), &tv, &kv_full[stage], 64 * a, boxes > 1 ? 0 : y,
-                                        un.h, p);
+                            tma_load_4d(dst + a * (BKV * 128), map, &kv_full[stage], 64 * a, y, un.h, p);
                     }
                     __syncwarp();
                     armed |= 1u << stage;
                     parity = (parity & ~(1u << stage)) | (phase << stage);
                     if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                 }
-                if (ok && clear) {
+                if (ok && clear && of_v) {
                     const int st = (nj - 1) % C::STAGES;
                     if (mbar_wait_warp(&kv_full[st], (parity >> st) & 1, abort_flag, g.err)) {
                         for (int a = 0; a < C::ATOMS; ++a) {
@@ -451,7 +463,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                         if (lane == 0) mbar_arrive(v_ready);
                     }
                 }
-                {
+                if (!of_v) {
                     const unsigned long long t0 = globaltimer();
                     while (!mbar_try_wait(q_full, 0) && globaltimer() - t0 < kWaitLimitNs) {
                     }
@@ -558,18 +570,18 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
         const uint64_t scale2 = pair(g.scale_log2, g.scale_log2);
         bool ok = true, s_ready = false;
         const int mine = t < nt ? nj : 0;
-        for (int j = 0; j < mine; ++j) {                     // j counts this CTA's steps
-            if (!s_ready && !mbar_wait_warp(&s_full[t], j & 1, abort_flag, g.err)) { ok = false; break; }
-            tc_fence_after();
-            if (!work) {
-                if (lane == 0) mbar_arrive(&s_free[t]);
-                if (j > 0 && !mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) { ok = false; break; }
-                if (lane == 0) {
-                    mbar_arrive(&p_full[t]);
-                    if (NT == 2 && j == 0 && t == 0) mbar_arrive(stagger);
-                }
-                continue;
+        auto hand_over = [&](int j) {
+            if (lane == 0) {
+                mbar_arrive(&p_full[t]);
+                if (NT == 2 && j == 0 && t == 0) mbar_arrive(stagger);
             }
+        };
+        // one step (j counts this CTA's) of a warp with rows; `masked`: some row's
+        // limit lies within it.  (The masked steps, the last few, are code of their
+        // own: as a branch in every step they cost 5% at d = 128.)
+        auto step = [&](int j, auto masked) {
+            if (!s_ready && !mbar_wait_warp(&s_full[t], j & 1, abort_flag, g.err)) return false;
+            tc_fence_after();
             float s[BKV];
 #pragma unroll
             for (int c = 0; c < BKV / 32; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
@@ -579,8 +591,8 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
             __syncwarp();
             if (lane == 0) mbar_arrive(&s_free[t]);
             const int k0 = (j0 + j) * BKV;
-            if (min_lim - k0 < BKV) {
-                asm volatile("");                            // a branch, not a select for each score of every step
+            (void)k0;
+            if constexpr (decltype(masked)::value) {
                 const int left = lim - k0;
 #pragma unroll
                 for (int c = 0; c < BKV; ++c)
@@ -608,7 +620,8 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                 return (lo[0] + lo[1]) + (hi[0] + hi[1]);
             };
             float base = m_run;
-            if (__any_sync(0xffffffffu, l_run == 0.f)) {     // a row that has seen nothing yet
+            // a row that has seen nothing yet (in a masked step, or the first)
+            if (decltype(masked)::value ? __any_sync(0xffffffffu, l_run == 0.f) : j == 0) {
                 const float top = tile_max() * g.scale_log2;
                 if (l_run == 0.f) base = top == -INFINITY ? 0.f : top;
             }
@@ -619,7 +632,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
 #pragma unroll 1
             for (int pass = 0;; ++pass) {
                 sum = numerators(base);
-                const bool redo = pass == 0 && valid && !(sum <= 256.0f);
+                const bool redo = pass == 0 && !(sum <= 256.0f);
                 if (!__any_sync(0xffffffffu, redo)) break;
                 if (redo) base = fmaxf(base, tile_max() * g.scale_log2);
             }
@@ -629,7 +642,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
             m_run = base;
             // PV(t, j-1) must be done before P(t) is overwritten and O(t) rescaled
             if (j > 0) {
-                if (!mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) { ok = false; break; }
+                if (!mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err)) return false;
                 tc_fence_after();
             }
             if (j > 0 && moved) {
@@ -656,11 +669,24 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&p_full[t]);
-                if (NT == 2 && j == 0 && t == 0) mbar_arrive(stagger);
-            }
+            hand_over(j);
             if (D == 64) s_ready = __all_sync(0xffffffffu, next);
+            return true;
+        };
+        if (work) {
+            const int open = max(0, min(mine, (min_lim - j0 * BKV) / BKV));
+            int j = 0;
+#pragma unroll 1
+            for (; ok && j < open; ++j) ok = step(j, std::false_type{});
+#pragma unroll 1
+            for (; ok && j < mine; ++j) ok = step(j, std::true_type{});
+        } else {                                             // a warp without rows only keeps step
+            for (int j = 0; ok && j < mine; ++j) {
+                ok = mbar_wait_warp(&s_full[t], j & 1, abort_flag, g.err);
+                if (ok && lane == 0) mbar_arrive(&s_free[t]);
+                if (ok && j > 0) ok = mbar_wait_warp(&p_free[t], (j - 1) & 1, abort_flag, g.err);
+                if (ok) hand_over(j);
+            }
         }
         if (ok && mine > 0) ok = mbar_wait_warp(&o_final[t], 0, abort_flag, g.err);
         if (ok && work) {
