@@ -8,6 +8,8 @@
 // sum over K is fp32 beyond a block, whatever the scales.
 #include "gemm_fp8.cuh"
 
+#include <cmath>
+
 namespace wdc {
 
 namespace {
@@ -24,18 +26,28 @@ __device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 1
 // A cluster of `split` CTAs shares a tile's K: each sums its blocks, sends the
 // others their share of the tile's tokens through distributed shared memory and
 // adds what it receives in rank order.
+// A round of the issuer (two waits, four MMAs, two commits) takes about 500 cycles
+// however narrow the MMAs are, so a stage of the ring, and a TMEM buffer, holds two
+// blocks, and one lane runs the issuer's loop (4 x 3072 x 12288 in one piece: 31 us,
+// with one lane 26, with both 18).  Ring and buffers are as many as one CTA an SM may
+// have where no SM needs two.
+constexpr int kMaxStages = 11;
 template <int BN>
 struct NarrowCfg {
-    static constexpr uint32_t W_BYTES = 128 * kBlock, A_BYTES = BN * kBlock, STAGE = W_BYTES + A_BYTES;
-    static constexpr int STAGES = BN <= 32 ? 5 : (BN == 64 ? 4 : 3);
-    static constexpr int BUFS = BN == 128 ? 2 : 4;
-    static constexpr uint32_t TMEM_COLS = BUFS * BN;
+    static constexpr int KB = 2;                           // blocks a stage
+    static constexpr uint32_t W_BYTES = 128 * kBlock, A_BYTES = BN * kBlock, BLOCK = W_BYTES + A_BYTES, STAGE = KB * BLOCK;
+    static constexpr int BUFS = 256 / (KB * BN);           // (twice as many alone)
     static constexpr uint32_t IDESC = idesc_e4m3(128, BN);
-    static constexpr int WINDOW = BN == 128 ? 8 : 16;      // blocks whose scales are in shared memory at a time
+    static constexpr int WINDOW = 16;                      // blocks whose scales are in shared memory at a time
     static constexpr uint32_t WINDOW_BYTES = 2 * WINDOW * BN * 4;
-    static constexpr size_t SMEM = STAGES * STAGE + WINDOW_BYTES + 1024 + 256;
-    static_assert(BN * 128 * 4 <= STAGES * STAGE, "partial sums fit the ring");
-    static_assert(TMEM_COLS >= 32 && 2 * TMEM_COLS <= 512 && 2 * (SMEM + 1024) <= 227 * 1024, "two CTAs an SM");
+    static constexpr size_t FIXED = WINDOW_BYTES + 1024 + 512;
+    static constexpr size_t smem(int stages) { return (size_t)stages * STAGE + FIXED; }
+    static constexpr int fit(size_t bytes) {
+        return (int)((bytes - FIXED) / STAGE) < kMaxStages ? (int)((bytes - FIXED) / STAGE) : kMaxStages;
+    }
+    static constexpr int DEEP = fit(227 * 1024), SHARED = fit(113 * 1024);   // one CTA an SM, two
+    static_assert(BN * 128 * 4 <= SHARED * STAGE, "partial sums fit the ring");
+    static_assert(WINDOW % KB == 0, "whole stages a window");
 };
 
 template <typename T, int BN>
@@ -45,12 +57,13 @@ __global__ void __launch_bounds__(kThreads, 2)
     using C = NarrowCfg<BN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float* window = reinterpret_cast<float*>(smem + C::STAGES * C::STAGE);     // [2][WINDOW][BN]
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE + C::WINDOW_BYTES);
-    uint64_t* empty = full + C::STAGES;
-    uint64_t* tfull = empty + C::STAGES;
-    uint64_t* tempty = tfull + C::BUFS;
-    uint64_t* mma_done = tempty + C::BUFS;
+    const int stages = g.stages, bufs = g.bufs;
+    float* window = reinterpret_cast<float*>(smem + stages * C::STAGE);     // [2][WINDOW][BN]
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + stages * C::STAGE + C::WINDOW_BYTES);
+    uint64_t* empty = full + stages;
+    uint64_t* tfull = empty + stages;
+    uint64_t* tempty = tfull + bufs;
+    uint64_t* mma_done = tempty + bufs;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -58,13 +71,15 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int S = g.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
     const int tile = blockIdx.x / S;
     const int m0 = (tile % g.m_tiles) * BN, nb = tile / g.m_tiles;             // neighbouring tiles share W
-    const int kb0 = (int)((long long)rank * g.kb / S), kb1 = (int)((long long)(rank + 1) * g.kb / S);
+    const int units = (g.kb + C::KB - 1) / C::KB;          // stages' worth of blocks
+    const int kb0 = (int)((long long)rank * units / S) * C::KB;
+    const int kb1 = min((int)((long long)(rank + 1) * units / S) * C::KB, g.kb);
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::STAGES; ++s) {
+        for (int s = 0; s < stages; ++s) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        for (int b = 0; b < C::BUFS; ++b) {
+        for (int b = 0; b < bufs; ++b) {
             mbar_init(&tfull[b], 1);
             mbar_init(&tempty[b], 4);
         }
@@ -77,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         prefetch_tmap(&tmA);
     }
     if (warp == 1) {
-        tmem_alloc(tmem_slot, C::TMEM_COLS);
+        tmem_alloc(tmem_slot, (uint32_t)(bufs * C::KB * BN));
         tmem_relinquish();
     }
     __syncthreads();
@@ -89,53 +104,57 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (warp == 0) {
         int stage = 0;
         uint32_t phase = 0, armed = 0, parity = 0;         // per stage: a copy was issued; its phase
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int kb = kb0; kb < kb1; kb += C::KB) {        // (columns past K are filled with zeros)
             if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_flag, g.err)) break;
             if (elect_one()) {
                 mbar_arrive_expect_tx(&full[stage], C::STAGE);
-                uint8_t* sw = smem + stage * C::STAGE;
-                tma_load_2d(sw, &tmW, &full[stage], kb * kBlock, nb * 128);
-                tma_load_2d(sw + C::W_BYTES, &tmA, &full[stage], kb * kBlock, m0);
+#pragma unroll
+                for (int i = 0; i < C::KB; ++i) {
+                    uint8_t* sw = smem + stage * C::STAGE + i * C::BLOCK;
+                    tma_load_2d(sw, &tmW, &full[stage], (kb + i) * kBlock, nb * 128);
+                    tma_load_2d(sw + C::W_BYTES, &tmA, &full[stage], (kb + i) * kBlock, m0);
+                }
             }
             __syncwarp();
             armed |= 1u << stage;
             parity = (parity & ~(1u << stage)) | (phase << stage);
-            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
         // every issued copy has landed before the ring is reused or the CTA exits
-        for (int s = 0; s < C::STAGES; ++s) {
+        for (int s = 0; s < stages; ++s) {
             if (!((armed >> s) & 1)) continue;
             const unsigned long long t0 = globaltimer();
             while (!mbar_try_wait(&full[s], (parity >> s) & 1) && globaltimer() - t0 < kWaitLimitNs) {
             }
         }
     } else if (warp == 1) {
-        const uint64_t dw = sdesc_sw128(smem_u32(smem)), da = sdesc_sw128(smem_u32(smem) + C::W_BYTES);
-        int stage = 0, buf = 0;
-        uint32_t phase = 0, bphase = 0;
-        bool ok = true;                                    // this lane's waits (elect_one)
-        for (int kb = kb0; kb < kb1; ++kb) {
-            ok = ok && mbar_wait(&tempty[buf], bphase ^ 1u, abort_flag, g.err);
-            ok = ok && mbar_wait(&full[stage], phase, abort_flag, g.err);
-            tc_fence_after();
-            if (elect_one() && ok) {
+        if (elect_one()) {
+            const uint64_t dw = sdesc_sw128(smem_u32(smem)), da = sdesc_sw128(smem_u32(smem) + C::W_BYTES);
+            int stage = 0, buf = 0;
+            uint32_t phase = 0, bphase = 0;
+            for (int kb = kb0; kb < kb1; kb += C::KB) {
+                if (!mbar_wait(&tempty[buf], bphase ^ 1u, abort_flag, g.err)) break;
+                if (!mbar_wait(&full[stage], phase, abort_flag, g.err)) break;
+                tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    tc_mma8(tmem + (uint32_t)(buf * BN), sdesc_at(dw, stage * C::STAGE + k * 32),
-                            sdesc_at(da, stage * C::STAGE + k * 32), C::IDESC, k != 0);
+                for (int i = 0; i < C::KB; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma8(tmem + (uint32_t)((buf * C::KB + i) * BN),
+                                sdesc_at(dw, stage * C::STAGE + i * C::BLOCK + k * 32),
+                                sdesc_at(da, stage * C::STAGE + i * C::BLOCK + k * 32), C::IDESC, k != 0);
                 tc_commit(&empty[stage]);
                 tc_commit(&tfull[buf]);
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+                if (++buf == bufs) { buf = 0; bphase ^= 1u; }
             }
-            __syncwarp();
-            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
-            if (++buf == C::BUFS) { buf = 0; bphase ^= 1u; }
+            // all MMAs issued by this lane have completed before TMEM is freed
+            tc_commit(mma_done);
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(mma_done, 0) && globaltimer() - t0 < kWaitLimitNs) {
+            }
         }
-        // all MMAs issued by this warp have completed before TMEM is freed
-        if (elect_one()) tc_commit(mma_done);
         __syncwarp();
-        const unsigned long long t0 = globaltimer();
-        while (!mbar_try_wait(mma_done, 0) && globaltimer() - t0 < kWaitLimitNs) {
-        }
     }
 
     float acc[BN];
@@ -159,8 +178,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         for (int c = 0; c < BN; ++c) acc[c] = 0.f;
         int buf = 0;
         uint32_t bphase = 0;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int at = (kb - kb0) % C::WINDOW, w = (kb - kb0) / C::WINDOW;
+        int at = 0, w = 0;                                 // the stage's first block in its window; the window
+        for (int kb = kb0; kb < kb1; kb += C::KB) {
             if (at == 0) {
                 float* own = window + (w & 1) * C::WINDOW * BN;
                 cp_async_wait();
@@ -174,14 +193,14 @@ __global__ void __launch_bounds__(kThreads, 2)
             const float4* s4 = reinterpret_cast<const float4*>(window + ((w & 1) * C::WINDOW + at) * BN);
             ok = ok && mbar_wait_warp(&tfull[buf], bphase, abort_flag, g.err);
             tc_fence_after();
-            constexpr int CH = BN < 32 ? BN : 32;          // columns a load
+            constexpr int CH = BN < 32 ? BN : 32, COLS = C::KB * BN;        // columns a load; of the buffer
 #pragma unroll
-            for (int c0 = 0; c0 < BN; c0 += CH) {
+            for (int c0 = 0; c0 < COLS; c0 += CH) {
                 uint32_t p[CH];
-                if constexpr (CH == 16) tmem_ld16(lanes + (uint32_t)(buf * BN), p);
-                else tmem_ld32(lanes + (uint32_t)(buf * BN + c0), p);
+                if constexpr (CH == 16) tmem_ld16(lanes + (uint32_t)(buf * COLS + c0), p);
+                else tmem_ld32(lanes + (uint32_t)(buf * COLS + c0), p);
                 tmem_ld_wait();
-                if (c0 + CH == BN) {
+                if (c0 + CH == COLS) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&tempty[buf]);
@@ -189,13 +208,15 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
                 for (int c = 0; c < CH; c += 4) {
                     const float4 s = s4[(c0 + c) / 4];
-                    acc[c0 + c] = fmaf(__uint_as_float(p[c]), s.x, acc[c0 + c]);
-                    acc[c0 + c + 1] = fmaf(__uint_as_float(p[c + 1]), s.y, acc[c0 + c + 1]);
-                    acc[c0 + c + 2] = fmaf(__uint_as_float(p[c + 2]), s.z, acc[c0 + c + 2]);
-                    acc[c0 + c + 3] = fmaf(__uint_as_float(p[c + 3]), s.w, acc[c0 + c + 3]);
+                    const int a = (c0 + c) % BN;
+                    acc[a] = fmaf(__uint_as_float(p[c]), s.x, acc[a]);
+                    acc[a + 1] = fmaf(__uint_as_float(p[c + 1]), s.y, acc[a + 1]);
+                    acc[a + 2] = fmaf(__uint_as_float(p[c + 2]), s.z, acc[a + 2]);
+                    acc[a + 3] = fmaf(__uint_as_float(p[c + 3]), s.w, acc[a + 3]);
                 }
             }
-            if (++buf == C::BUFS) { buf = 0; bphase ^= 1u; }
+            if (++buf == bufs) { buf = 0; bphase ^= 1u; }
+            if ((at += C::KB) == C::WINDOW) { at = 0; ++w; }
         }
     }
     // this CTA's copies have landed and its MMAs are done
@@ -203,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, C::TMEM_COLS);
+        tmem_dealloc(tmem, (uint32_t)(bufs * C::KB * BN));
     }
     const int row = lg * 32 + lane, n = nb * 128 + row;
     const bool mine = warp >= 2 && ok && n < g.N;
@@ -255,33 +276,36 @@ __global__ void __launch_bounds__(kThreads, 2)
 using NarrowKernel = void (*)(const CUtensorMap, const CUtensorMap, const Gemm8Args);
 struct Narrow {
     NarrowKernel kernel;
-    size_t smem;
+    int deep, shared;                                      // stages of the ring, of one CTA an SM and of two
+    int bufs;                                              // TMEM buffers of two
+    size_t (*smem)(int stages);
 };
+template <typename T, int BN>
+Narrow narrow_of() {
+    using C = NarrowCfg<BN>;
+    return {gemm8_narrow_kernel<T, BN>, C::DEEP, C::SHARED, C::BUFS, [](int stages) { return C::smem(stages); }};
+}
 template <typename T>
 Narrow narrow(int bn) {
     switch (bn) {
-        case 16: return {gemm8_narrow_kernel<T, 16>, NarrowCfg<16>::SMEM};
-        case 32: return {gemm8_narrow_kernel<T, 32>, NarrowCfg<32>::SMEM};
-        case 64: return {gemm8_narrow_kernel<T, 64>, NarrowCfg<64>::SMEM};
-        default: return {gemm8_narrow_kernel<T, 128>, NarrowCfg<128>::SMEM};
+        case 16: return narrow_of<T, 16>();
+        case 32: return narrow_of<T, 32>();
+        default: return narrow_of<T, 64>();
     }
 }
 
 template <typename T>
-wdc_status launch(Ctx* c, const void* A, const void* W, Gemm8Args g, cudaStream_t s) {
+wdc_status launch(Ctx* c, const void* A, const void* W, Gemm8Args g, int bn, int split, cudaStream_t s) {
     static PerDevice<bool> attr;
     attr.get(c->device, [](bool& ok) {
         ok = true;
-        for (int bn : {16, 32, 64, 128}) ok &= allow_smem(narrow<T>(bn).kernel, narrow<T>(bn).smem);
+        for (int bn : {16, 32, 64}) ok &= allow_smem(narrow<T>(bn).kernel, narrow<T>(bn).smem(narrow<T>(bn).deep));
         return ok;
     });
-    int bn = 16;
-    while (bn < 128 && bn < g.M) bn *= 2;
-    g.m_tiles = (g.M + bn - 1) / bn;
-    g.n_tiles = (g.N + 127) / 128;
+    g.m_tiles = (g.M - 1) / bn + 1;
+    g.n_tiles = (g.N - 1) / 128 + 1;
     const long long tiles = (long long)g.m_tiles * g.n_tiles;
-    g.split = 1;
-    while (g.split < 8 && 2 * g.split <= g.kb && tiles * g.split * 2 <= c->num_sms) g.split *= 2;
+    g.split = split;
     if (tiles * g.split > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp8 GEMM: more than 2^31 - 1 thread blocks");
     CUtensorMap tw, ta;
     std::string why;
@@ -292,11 +316,61 @@ wdc_status launch(Ctx* c, const void* A, const void* W, Gemm8Args g, cudaStream_
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_GEMM, s);
         const Narrow k = narrow<T>(bn);
-        launch_kernel(k.kernel, dim3((unsigned)(tiles * g.split)), kThreads, k.smem, s, g.split, tw, ta, g);
+        const bool alone = tiles * g.split <= c->num_sms;
+        g.stages = alone ? k.deep : k.shared;
+        g.bufs = alone ? 2 * k.bufs : k.bufs;
+        launch_kernel(k.kernel, dim3((unsigned)(tiles * g.split)), kThreads, k.smem(g.stages), s, g.split, tw, ta, g);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp8 GEMM launch: ") + cudaGetErrorString(e));
     return WDC_OK;
+}
+
+// The kernel for a shape is the one with the least estimated time, by fits to a
+// sweep (us, bf16, no residual; narrow kernel n<tokens a tile>,<CTAs a tile>; pair
+// kernel p<columns a tile>):
+//                          n16,1  n32,1  n64,1  n16,4   p128   p256
+//   4 x 3072 x 3072          7.7                  8.9
+//   4 x 3072 x 12288        18.2                 11.9
+//   33 x 9216 x 3072        10.3    9.3   12.6
+//   100 x 12288 x 3072      23.7   19.9   19.6
+//   226 x 1024 x 1024        5.5    5.8    8.2           7.6    8.8
+//   226 x 9216 x 3072       33.3   24.2   19.7          12.5   15.3
+//   512 x 3072 x 12288             65.5   57.3          29.9   41.7
+//   512 x 9216 x 3072              44.7   36.5          19.4   16.3
+//   1350 x 3072 x 12288                                 66.6   43.1
+//   4276 x 9216 x 3072                                   129    104
+// A narrow CTA takes kStage us for two blocks of K; more CTAs than SMs take turns
+// (two on an SM are each about half as fast); a cluster's launch, barriers and
+// exchange cost kSplit.  A pair takes kBlock us a block of K and kTile a tile.
+struct Choice {
+    int bn, split;                     // split 0: the pair kernel
+};
+Choice choose(const Ctx* c, int M, int N, int kb) {
+    constexpr double kStart[3] = {4.2, 4.3, 5.8}, kStage[3] = {0.29, 0.375, 0.56};
+    Choice best{16, 1};
+    double least = 1e30;
+    auto offer = [&](int bn, int split, double est) {
+        if (est < least) {
+            least = est;
+            best = {bn, split};
+        }
+    };
+    for (int i = 0; i < 3; ++i) {
+        const int bn = 16 << i;
+        const double tiles = (double)((M - 1) / bn + 1) * ((N - 1) / 128 + 1);
+        for (int split = 1; split <= 8 && (split == 1 || 4 * split <= kb); split *= 2) {
+            const double kSplit = split == 1 ? 0.0 : (split == 8 ? 6.0 : 4.2);
+            const int stages = (kb + 2 * split - 1) / (2 * split);
+            offer(bn, split, kStart[i] + ceil(tiles * split / c->num_sms) * stages * kStage[i] + kSplit);
+        }
+    }
+    if (c->num_sms >= 2) {
+        const double rows = (M - 1) / 256 + 1, pairs = c->num_sms / 2;
+        offer(128, 0, 5.0 + ceil(rows * ((N - 1) / 128 + 1) / pairs) * (kb * 0.25 + 1.0));
+        offer(256, 0, 5.0 + ceil(rows * ((N - 1) / 256 + 1) / pairs) * (kb * 0.37 + 1.5));
+    }
+    return best;
 }
 
 }  // namespace
@@ -315,8 +389,10 @@ wdc_status op_gemm_fp8(Ctx* c, const void* A, const float* a_scale, const void* 
     g.M = M; g.N = N; g.K = K; g.kb = (K + kBlock - 1) / kBlock; g.sw_rows = (N + 127) / 128;
     g.sa = a_scale; g.sw = w_scale; g.bias = bias; g.gate = res ? gate : nullptr; g.res = res; g.out = C; g.gelu = gelu;
     g.err = c->err;
-    if (M >= 512) return launch_gemm8_pair(c, A, W, g, 256, s);
-    return c->cfg.dtype == WDC_BF16 ? launch<__nv_bfloat16>(c, A, W, g, s) : launch<float>(c, A, W, g, s);
+    const Choice ch = choose(c, M, N, g.kb);
+    if (ch.split == 0) return launch_gemm8_pair(c, A, W, g, ch.bn, s);
+    return c->cfg.dtype == WDC_BF16 ? launch<__nv_bfloat16>(c, A, W, g, ch.bn, ch.split, s)
+                                    : launch<float>(c, A, W, g, ch.bn, ch.split, s);
 }
 
 }  // namespace wdc

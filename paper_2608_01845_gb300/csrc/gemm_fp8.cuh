@@ -11,7 +11,7 @@ constexpr int kBlock8 = 128;            // of K: a scale's columns, the bytes of
 struct Gemm8Args {
     int M, N, K, kb;                    // kb: blocks of K
     int m_tiles, n_tiles;
-    int split;                          // narrow kernel: CTAs a tile
+    int split, stages, bufs;            // narrow kernel: CTAs a tile, tiles of its ring, TMEM buffers
     int group_n;                        // pair kernel: column blocks of a raster group
     int sw_rows;                        // rows of w_scale
     const float *sa, *sw, *bias, *gate;

@@ -115,7 +115,9 @@ def test_gemm(contexts, M, N, K, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", [(3, 264, 528), (140, 264, 528), (700, 1152, 400)])
+# (in this order: one narrow tile; several, K over a cluster; the pair kernel's tiles
+# of 128 and of 256 columns, several a pair in the last)
+@pytest.mark.parametrize("M,N,K", [(3, 264, 528), (40, 392, 8208), (520, 2312, 2064), (1030, 2056, 1040), (2309, 3080, 528)])
 @pytest.mark.parametrize("mode", ["bias", "gelu", "resid", "resid_gelu", "gateless"])
 def test_gemm_epilogues(contexts, M, N, K, mode, kind):
     """The epilogue's own error: 1.13 (GELU's steepest slope) of the sum's, 2^-18 of
