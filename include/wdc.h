@@ -571,7 +571,8 @@ wdc_status wdc_op_qk_norm_rope(wdc_ctx* ctx, const void* qkv, long long ld, int 
  * q_start[b] .. q_start[b + 1] - 1 are the last tokens of sequence b (q_start
  * device [sequences + 1], non-decreasing, 4-byte aligned).  Writes q [T, heads, d]
  * and appends keys and values to their pages (values fp16, saturated as above).
- * Rows from q_start[sequences] on are not read and their q is left as it is.
+ * What rows from q_start[sequences] on hold does not matter, and their q is left
+ * as it is.
  * The pages that a chunk is appended to belong to one sequence each. */
 wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads,
                                       const wdc_head_norm* norm, const wdc_paged_cache* cache, const int* q_start,

@@ -3,7 +3,7 @@
 //   y = x / sqrt(mean(x^2) + eps) * w per head, then on its first rot elements
 //   a' = a cos - b sin, b' = b cos + a sin for each pair (a, b).
 // Bound by memory: each row is read once and written once, the angles of a
-// token are read once for all its heads.  A lane holds 16 bytes of a head, so a
+// token are read once for a few of its heads.  A lane holds 16 bytes of a head, so a
 // head of 64 bf16 is 8 lanes and a sum over it three shuffles; a warp takes
 // kGroups neighbouring warp-widths of one token's heads, all loaded before the
 // first is reduced.  Sums, weights and angles are fp32; the one rounding is that
@@ -30,13 +30,14 @@ struct NormArgs {
     const int* positions;
     void *q, *k, *v;
     int ldv;                           // dense: V^T's row stride
-    unsigned norm_blocks;              // dense: the blocks behind these transpose V
+    unsigned vt_tiles;                 // dense: blocks that transpose V
     // append
     const int *table, *length, *start;
     int pages, page_log2, sequences, width;
     unsigned* err;
 };
 
+// A lane's elements of a head: 16 bytes in two halves, each of E / 2 neighbours.
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int E = 4;
@@ -44,29 +45,43 @@ template <> struct Vec<float> {
         const float4 a = *reinterpret_cast<const float4*>(p);
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
     }
+    static __device__ __forceinline__ void load(const float* p, const float* q, float (&v)[4]) {
+        const float2 a = *reinterpret_cast<const float2*>(p), b = *reinterpret_cast<const float2*>(q);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    }
     static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
+    static __device__ __forceinline__ void store(float* p, float* q, const float (&v)[4]) {
+        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+        *reinterpret_cast<float2*>(q) = make_float2(v[2], v[3]);
+    }
 };
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void widen(uint32_t w, float& a, float& b) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xffff0000u);
+}
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int E = 8;
     static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
         const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        widen(u.x, v[0], v[1]); widen(u.y, v[2], v[3]); widen(u.z, v[4], v[5]); widen(u.w, v[6], v[7]);
+    }
+    static __device__ __forceinline__ void load(const __nv_bfloat16* p, const __nv_bfloat16* q, float (&v)[8]) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(q);
+        widen(a.x, v[0], v[1]); widen(a.y, v[2], v[3]); widen(b.x, v[4], v[5]); widen(b.y, v[6], v[7]);
     }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, __nv_bfloat16* q, const float (&v)[8]) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]));
+        *reinterpret_cast<uint2*>(q) = make_uint2(bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
     }
 };
 
@@ -82,17 +97,21 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
     const int n = min(kVtTokens, a.T - t0);
     const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)(a.heads + a.kv + head) * D;
     bool sat = false;
-    constexpr int PER = D / V::E;                              // lanes a token
+    constexpr int PER = D / V::E, N = kVtTokens * PER / 256;   // lanes a token; pieces a thread
+    float v[N][V::E];
 #pragma unroll
-    for (int i0 = 0; i0 < kVtTokens * PER; i0 += 256) {
-        const int i = i0 + threadIdx.x, t = i / PER, e = (i % PER) * V::E;
+    for (int u = 0; u < N; ++u) {
+        const int i = u * 256 + threadIdx.x, t = i / PER;
+        if (t < n) V::load(src + (size_t)(t0 + t) * a.ld + (i % PER) * V::E, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int i = u * 256 + threadIdx.x, t = i / PER, e = (i % PER) * V::E;
         if (t < n) {
-            float v[V::E];
-            V::load(src + (size_t)(t0 + t) * a.ld + e, v);
 #pragma unroll
             for (int j = 0; j < V::E; ++j) {
-                if constexpr (sizeof(T) == 2) sm[(e + j) * LDS + t] = to_vt_half(v[j], sat);
-                else sm[(e + j) * LDS + t] = v[j];
+                if constexpr (sizeof(T) == 2) sm[(e + j) * LDS + t] = to_vt_half(v[u][j], sat);
+                else sm[(e + j) * LDS + t] = v[u][j];
             }
         }
     }
@@ -120,22 +139,52 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
 }
 
 template <typename T, int D, bool APPEND, bool PAIRS>
-__global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant__ NormArgs a) {
     using V = Vec<T>;
     constexpr int E = V::E, LPH = D / E, HPW = 32 / LPH;       // elements a lane, lanes a head, heads a warp-width
     chain_release();
     chain_wait();
-    if (!APPEND && blockIdx.x >= a.norm_blocks) {
-        transpose_v<T, D>(a, (int)(blockIdx.x - a.norm_blocks));
-        return;
+    unsigned block = blockIdx.x;
+    if (!APPEND && a.vt_tiles > 0) {
+        // V^T's tiles among the blocks of norms, evenly: each kind waits for
+        // memory at other times (one behind the other 133 us, mixed 124 at 17776 x 72 heads of 128)
+        const unsigned v = (unsigned)((unsigned long long)block * a.vt_tiles / gridDim.x);
+        if ((unsigned)((unsigned long long)(block + 1) * a.vt_tiles / gridDim.x) > v) {
+            transpose_v<T, D>(a, (int)v);
+            return;
+        }
+        block -= v;
     }
     const int lane = threadIdx.x & 31;
-    const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long w = (long long)block * 8 + (threadIdx.x >> 5);
     const long long tl = w / a.chunks;
     if (tl >= a.T) return;
     const int t = (int)tl, chunk = (int)(w - tl * a.chunks);
-    const int e0 = (lane % LPH) * E;
     const int n_heads = APPEND ? a.heads + 2 * a.kv : a.heads + a.kv;
+    const int half = a.rot_dim >> 1, l = lane % LPH;
+
+    // This lane's elements of a head, in two halves whose element i makes a pair
+    // (not interleaved), so that a pair is turned within a lane; what is not turned
+    // lies behind.  Interleaved, or not turned at all, they are neighbours.
+    int ea = l * E, eb = ea + E / 2;
+    if (!PAIRS) {
+        const int lanes = half / (E / 2);                      // that hold pairs
+        ea = l < lanes ? l * (E / 2) : a.rot_dim + (l - lanes) * E;
+        eb = l < lanes ? half + ea : ea + E / 2;
+    }
+    float x[kGroups][E];
+    const T* row = reinterpret_cast<const T*>(a.qkv) + (size_t)t * a.ld;
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+        const int h = (chunk * kGroups + u) * HPW + lane / LPH;
+        if (h < n_heads) {
+            if constexpr (PAIRS) V::load(row + (size_t)h * D + ea, x[u]);
+            else V::load(row + (size_t)h * D + ea, row + (size_t)h * D + eb, x[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[u][i] = 0.f;
+        }
+    }
 
     // this token's place: its row of the cache and its position
     int place = t;
@@ -160,10 +209,9 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ 
         slot = keep ? (size_t)page * a.kv : 0;
     }
 
-    // its angles, for the elements of this lane
-    float cs[PAIRS ? E : 2 * E];                               // cos, sin of each pair
-    const int half = a.rot_dim >> 1;
-    const bool turned = a.rot && e0 < a.rot_dim;
+    // its angles, for the pairs of this lane
+    float cs[E];                                               // cos, sin of each pair
+    const bool turned = a.rot && ea < (PAIRS ? a.rot_dim : half);
     if (a.rot) {
         int p = a.positions ? a.positions[t] : place;
         if (p < 0 || p >= a.rot_positions) {
@@ -171,28 +219,15 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ 
             p = max(0, min(p, a.rot_positions - 1));
         }
         if (turned) {
-            const int i0 = PAIRS ? e0 / 2 : (e0 < half ? e0 : e0 - half);
-            const float4* r = reinterpret_cast<const float4*>(a.rot + (size_t)p * half + i0);
+            const float4* r = reinterpret_cast<const float4*>(a.rot + (size_t)p * half + (PAIRS ? ea / 2 : ea));
 #pragma unroll
-            for (int i = 0; i < (PAIRS ? E : 2 * E) / 4; ++i) {
+            for (int i = 0; i < E / 4; ++i) {
                 const float4 c = r[i];
                 cs[4 * i] = c.x; cs[4 * i + 1] = c.y; cs[4 * i + 2] = c.z; cs[4 * i + 3] = c.w;
             }
         }
     }
 
-    float x[kGroups][E];
-    const T* row = reinterpret_cast<const T*>(a.qkv) + (size_t)t * a.ld;
-#pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-        const int h = (chunk * kGroups + u) * HPW + lane / LPH;
-        if (h < n_heads) {
-            V::load(row + (size_t)h * D + e0, x[u]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[u][i] = 0.f;
-        }
-    }
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
         const int h = (chunk * kGroups + u) * HPW + lane / LPH;
@@ -201,49 +236,12 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ 
         for (int i = 0; i < E; ++i) ss = fmaf(x[u][i], x[u][i], ss);
 #pragma unroll
         for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-        float y[E];
-        const float* wt = h < a.heads ? a.wq : a.wk;
-#pragma unroll
-        for (int i = 0; i < E; ++i) y[i] = x[u][i] * inv;
-        if (wt) {
-#pragma unroll
-            for (int i = 0; i < E; i += 4) {
-                const float4 f = *reinterpret_cast<const float4*>(wt + e0 + i);
-                y[i] *= f.x; y[i + 1] *= f.y; y[i + 2] *= f.z; y[i + 3] *= f.w;
-            }
-        }
-        if constexpr (PAIRS) {
-            if (turned) {
-#pragma unroll
-                for (int i = 0; i < E; i += 2) {
-                    const float p = y[i], q = y[i + 1];
-                    y[i] = p * cs[i] - q * cs[i + 1];
-                    y[i + 1] = q * cs[i] + p * cs[i + 1];
-                }
-            }
-        } else if (a.rot) {
-            // the pair's other element lies rot_dim / 2 elements on, or back
-            const int other = !turned ? lane : (e0 < half ? lane + half / E : lane - half / E);
-            const float sign = e0 < half ? -1.f : 1.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float z = __shfl_sync(0xffffffffu, y[i], other);
-                if (turned) y[i] = y[i] * cs[2 * i] + sign * z * cs[2 * i + 1];
-            }
-        }
         if (h >= n_heads) continue;
-        if (h < a.heads) {
-            const size_t at = APPEND ? (size_t)t * a.heads + h : (size_t)h * a.T + t;
-            V::store(reinterpret_cast<T*>(a.q) + at * D + e0, y);
-        } else if (h < a.heads + a.kv) {
-            const int g = h - a.heads;
-            if constexpr (APPEND) {
-                if (keep) V::store(reinterpret_cast<T*>(a.k) + (((slot + g) << a.page_log2) + in_page) * D + e0, y);
-            } else {
-                V::store(reinterpret_cast<T*>(a.k) + ((size_t)g * a.T + t) * D + e0, y);
-            }
-        } else if constexpr (APPEND) {
+        auto put = [&](T* head, const float (&v)[E]) {
+            if constexpr (PAIRS) V::store(head + ea, v);
+            else V::store(head + ea, head + eb, v);
+        };
+        if (APPEND && h >= a.heads + a.kv) {
             const int g = h - a.heads - a.kv;
             bool sat = false;
             uint32_t p[E / 2];
@@ -253,10 +251,53 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(const __grid_constant__ 
                 p[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
             }
             if (keep) {
-                uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__half*>(a.v) +
-                                                            (((slot + g) << a.page_log2) + in_page) * D + e0);
-                if constexpr (E == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(p[0], p[1], p[2], p[3]);
+                __half* dst = reinterpret_cast<__half*>(a.v) + (((slot + g) << a.page_log2) + in_page) * D;
+                if constexpr (E == 8) {
+                    if constexpr (PAIRS) {
+                        *reinterpret_cast<uint4*>(dst + ea) = make_uint4(p[0], p[1], p[2], p[3]);
+                    } else {
+                        *reinterpret_cast<uint2*>(dst + ea) = make_uint2(p[0], p[1]);
+                        *reinterpret_cast<uint2*>(dst + eb) = make_uint2(p[2], p[3]);
+                    }
+                }
                 if (sat) atomicOr(a.err, kErrVSaturated);
+            }
+            continue;
+        }
+        const float inv = rsqrtf(ss * (1.0f / D) + a.eps);     // (2 ulp; IEEE's root and quotient are 30 instructions)
+        float y[E];
+        const float* wt = h < a.heads ? a.wq : a.wk;
+#pragma unroll
+        for (int i = 0; i < E; ++i) y[i] = x[u][i] * inv;
+        if (wt) {
+            float f[E];
+            if constexpr (E == 8) {
+                Vec<float>::load(wt + ea, *reinterpret_cast<float(*)[4]>(&f[0]));
+                Vec<float>::load(wt + eb, *reinterpret_cast<float(*)[4]>(&f[4]));
+            } else {
+                Vec<float>::load(wt + ea, wt + eb, f);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[i] *= f[i];
+        }
+        if (turned) {
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float& p = y[PAIRS ? 2 * i : i];
+                float& q = y[PAIRS ? 2 * i + 1 : i + E / 2];
+                const float c = p, d = q;
+                p = c * cs[2 * i] - d * cs[2 * i + 1];
+                q = d * cs[2 * i] + c * cs[2 * i + 1];
+            }
+        }
+        if (h < a.heads) {
+            put(reinterpret_cast<T*>(a.q) + (APPEND ? (size_t)t * a.heads + h : (size_t)h * a.T + t) * D, y);
+        } else {
+            const int g = h - a.heads;
+            if constexpr (APPEND) {
+                if (keep) put(reinterpret_cast<T*>(a.k) + (((slot + g) << a.page_log2) + in_page) * D, y);
+            } else {
+                put(reinterpret_cast<T*>(a.k) + ((size_t)g * a.T + t) * D, y);
             }
         }
     }
@@ -269,7 +310,7 @@ wdc_status launch(Ctx* c, NormArgs& a, bool pairs, int vt_tiles, cudaStream_t s)
     a.chunks = (n_heads + kGroups * HPW - 1) / (kGroups * HPW);
     const long long blocks = ((long long)a.T * a.chunks + 7) / 8;
     if (blocks + vt_tiles > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^31 - 1 thread blocks");
-    a.norm_blocks = (unsigned)blocks;
+    a.vt_tiles = (unsigned)vt_tiles;
     const dim3 grid((unsigned)(blocks + vt_tiles));
     {
         OverlapScope ov(c, s);

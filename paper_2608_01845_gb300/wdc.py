@@ -236,23 +236,31 @@ class PagedCache:
         import torch
         if k.dim() != 4 or table.dim() != 2 or length.dim() != 1 or table.shape[0] != length.shape[0]:
             raise ValueError("PagedCache: k [pages, kv_heads, page, d], table [sequences, width], length [sequences]")
-        _tensor("PagedCache", "k", k, torch.bfloat16, k.shape, k.device)
-        _tensor("PagedCache", "v", v, torch.float16, k.shape, k.device)
-        _tensor("PagedCache", "table", table, torch.int32, table.shape, k.device)
-        _tensor("PagedCache", "length", length, torch.int32, length.shape, k.device)
+        self.device = dev = k.get_device()
+        _tensor("PagedCache", "k", k, torch.bfloat16, k.shape, dev)
+        _tensor("PagedCache", "v", v, torch.float16, k.shape, dev)
+        _tensor("PagedCache", "table", table, torch.int32, table.shape, dev)
+        _tensor("PagedCache", "length", length, torch.int32, length.shape, dev)
         self.k, self.v, self.table, self.length = k, v, table, length
         self.c = PagedCacheC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), k.shape[0], k.shape[2],
                              k.shape[1], k.shape[3], table.shape[0], table.shape[1])
 
 
 def _tensor(what, name, t, dtype, shape, device, row_stride=False):
-    """Checks a tensor that an operator takes; row_stride: its rows may lie apart."""
+    """Checks a tensor that an operator takes on device `device` (its index; -1: host memory); row_stride: its
+    rows may lie apart."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and (t.is_contiguous() or row_stride and (
+            t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1))):
+        return
     if t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: {name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{what}: {name} is on {t.device}, not {device}")
-    if not t.is_contiguous() and not (row_stride and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)):
-        raise ValueError(f"{what}: {name} must be contiguous")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: {name} is on {t.device}, not on device {device}")
+    raise ValueError(f"{what}: {name} must be contiguous")
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _row_stride(t):
@@ -478,62 +486,73 @@ class Context:
     # ---- chunk operators: the tensors' types, shapes and device are checked here, the rest behind the C ABI
 
     def _operand_types(self):
+        """(element type of the model, device index) that the operators' tensors have."""
         import torch
-        return (torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32), torch.device("cuda", self.device)
+        return (torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32), self.device
 
     def _op_stream(self, stream):
-        import torch
-        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+        """The given stream, or the current one of the context's device."""
+        if stream is None:
+            import torch
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def op_quantize_fp8(self, x, q, scale, block_rows=1, stream=None):
         """wdc_op_quantize_fp8: x [M, K] (rows may lie apart) to q (float8_e4m3fn [M, K]) and scale
         ([ceil(K/128), M], or with block_rows=128 [ceil(M/128), ceil(K/128)])."""
         import torch
-        dt, dev = self._operand_types()
+        what, (dt, dev) = "op_quantize_fp8", self._operand_types()
         if x.dim() != 2:
-            raise ValueError("op_quantize_fp8: x must be [M, K]")
+            raise ValueError(f"{what}: x must be [M, K]")
         M, K = x.shape
         kb = -(-K // 128)
-        _tensor("op_quantize_fp8", "x", x, dt, (M, K), dev, row_stride=True)
-        _tensor("op_quantize_fp8", "q", q, torch.float8_e4m3fn, (M, K), dev)
-        _tensor("op_quantize_fp8", "scale", scale, torch.float32, (kb, M) if block_rows == 1 else (-(-M // 128), kb), dev)
-        self._check(LIB.wdc_op_quantize_fp8(self._h, _ptr(x), _row_stride(x), _ptr(q), _ptr(scale), M, K, block_rows,
-                                            self._op_stream(stream)), "op_quantize_fp8")
+        _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
+        _tensor(what, "q", q, torch.float8_e4m3fn, (M, K), dev)
+        _tensor(what, "scale", scale, torch.float32, (kb, M) if block_rows == 1 else (-(-M // 128), kb), dev)
+        self._check(LIB.wdc_op_quantize_fp8(self._h, x.data_ptr(), _row_stride(x), q.data_ptr(), scale.data_ptr(), M, K,
+                                            block_rows, self._op_stream(stream)), what)
 
     def op_gemm_fp8(self, A, a_scale, W, w_scale, C, bias=None, gelu=False, res=None, gate=None, stream=None):
         """wdc_op_gemm_fp8: C = epilogue(A W^T) of float8_e4m3fn matrices with the scales of op_quantize_fp8
         (block_rows=1 for A, 128 for W)."""
         import torch
-        dt, dev = self._operand_types()
+        what, (dt, dev) = "op_gemm_fp8", self._operand_types()
         if A.dim() != 2 or W.dim() != 2:
-            raise ValueError("op_gemm_fp8: A must be [M, K] and W [N, K]")
+            raise ValueError(f"{what}: A must be [M, K] and W [N, K]")
         (M, K), N = A.shape, W.shape[0]
-        kb = -(-K // 128)
-        for name, t, ty, shape in (("A", A, torch.float8_e4m3fn, (M, K)), ("W", W, torch.float8_e4m3fn, (N, K)),
-                                   ("a_scale", a_scale, torch.float32, (kb, M)),
-                                   ("w_scale", w_scale, torch.float32, (-(-N // 128), kb)), ("C", C, dt, (M, N)),
-                                   ("bias", bias, torch.float32, (N,)), ("res", res, dt, (M, N)),
-                                   ("gate", gate, torch.float32, (N,))):
-            if t is not None:
-                _tensor("op_gemm_fp8", name, t, ty, shape, dev)
-        self._check(LIB.wdc_op_gemm_fp8(self._h, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(C), M,
-                                        N, K, int(gelu), _ptr(res), _ptr(gate), self._op_stream(stream)), "op_gemm_fp8")
+        kb, f8, f32 = -(-K // 128), torch.float8_e4m3fn, torch.float32
+        _tensor(what, "A", A, f8, (M, K), dev)
+        _tensor(what, "W", W, f8, (N, K), dev)
+        _tensor(what, "a_scale", a_scale, f32, (kb, M), dev)
+        _tensor(what, "w_scale", w_scale, f32, (-(-N // 128), kb), dev)
+        _tensor(what, "C", C, dt, (M, N), dev)
+        if bias is not None:
+            _tensor(what, "bias", bias, f32, (N,), dev)
+        if res is not None:
+            _tensor(what, "res", res, dt, (M, N), dev)
+        if gate is not None:
+            _tensor(what, "gate", gate, f32, (N,), dev)
+        self._check(LIB.wdc_op_gemm_fp8(self._h, A.data_ptr(), a_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(),
+                                        _address(bias), C.data_ptr(), M, N, K, int(gelu), _address(res), _address(gate),
+                                        self._op_stream(stream)), what)
 
     def _head_norm(self, what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved):
         import torch
-        for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if t is not None:
-                _tensor(what, name, t, torch.float32, (d,), dev)
+        f32 = torch.float32
+        if q_weight is not None:
+            _tensor(what, "q_weight", q_weight, f32, (d,), dev)
+        if k_weight is not None:
+            _tensor(what, "k_weight", k_weight, f32, (d,), dev)
         if positions is not None:
             _tensor(what, "positions", positions, torch.int32, (T,), dev)
-        n = HeadNorm(eps=eps, interleaved=int(bool(interleaved)))
-        n.q_weight, n.k_weight, n.positions = _ptr(q_weight), _ptr(k_weight), _ptr(positions)
+        at, n, pairs = None, 0, 0
         if rot is not None:
             if rot.dim() != 3 or rot.shape[2] != 2:
                 raise ValueError(f"{what}: rot must be [positions, rot_dim / 2, 2]")
-            _tensor(what, "rot", rot, torch.float32, rot.shape, dev)
-            n.rot, n.rot_positions, n.rot_dim = _ptr(rot), rot.shape[0], 2 * rot.shape[1]
-        return n
+            _tensor(what, "rot", rot, f32, rot.shape, dev)
+            at, (n, pairs, _) = rot.data_ptr(), rot.shape
+        return HeadNorm(_address(q_weight), _address(k_weight), eps, at, n, 2 * pairs, int(bool(interleaved)),
+                        _address(positions))
 
     def op_qk_norm_rope(self, qkv, q, k, vt=None, q_weight=None, k_weight=None, eps=1e-6, rot=None, positions=None,
                         interleaved=True, stream=None):
@@ -548,11 +567,11 @@ class Context:
         _tensor(what, "q", q, dt, (H, T, d), dev)
         _tensor(what, "k", k, dt, (kv, T, d), dev)
         if vt is not None:
-            bf16 = dt == torch.bfloat16
+            bf16 = dt is torch.bfloat16
             _tensor(what, "vt", vt, torch.float16 if bf16 else dt, (kv, d, -(-T // 8) * 8 if bf16 else T), dev)
         n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
-        self._check(LIB.wdc_op_qk_norm_rope(self._h, _ptr(qkv), _row_stride(qkv), T, H, kv, d, ctypes.byref(n), _ptr(q),
-                                            _ptr(k), _ptr(vt), self._op_stream(stream)), what)
+        self._check(LIB.wdc_op_qk_norm_rope(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, kv, d, n, q.data_ptr(),
+                                            k.data_ptr(), _address(vt), self._op_stream(stream)), what)
 
     def op_qk_norm_rope_append(self, qkv, q, cache, q_start, q_weight=None, k_weight=None, eps=1e-6, rot=None,
                                positions=None, interleaved=True, stream=None):
@@ -563,14 +582,14 @@ class Context:
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
-        if cache.k.device != dev or d != c.head_dim:
-            raise ValueError(f"{what}: the cache must be on {dev} with heads of {d}")
+        if cache.device != dev or d != c.head_dim:
+            raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "qkv", qkv, dt, (T, (H + 2 * c.kv_heads) * d), dev, row_stride=True)
         _tensor(what, "q", q, dt, (T, H, d), dev)
         _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
         n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
-        self._check(LIB.wdc_op_qk_norm_rope_append(self._h, _ptr(qkv), _row_stride(qkv), T, H, ctypes.byref(n),
-                                                   ctypes.byref(c), _ptr(q_start), _ptr(q), self._op_stream(stream)), what)
+        self._check(LIB.wdc_op_qk_norm_rope_append(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, n, c,
+                                                   q_start.data_ptr(), q.data_ptr(), self._op_stream(stream)), what)
 
     def op_attention_paged(self, q, cache, q_start, o, max_new, frame=1, stream=None):
         """wdc_op_attention_paged: q [T, heads, d] over ``cache`` (a PagedCache) into o [T, heads * d]; no
@@ -580,13 +599,13 @@ class Context:
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
-        if cache.k.device != dev or d != c.head_dim:
-            raise ValueError(f"{what}: the cache must be on {dev} with heads of {d}")
+        if cache.device != dev or d != c.head_dim:
+            raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "q", q, dt, (T, H, d), dev)
         _tensor(what, "o", o, dt, (T, H * d), dev)
         _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
-        self._check(LIB.wdc_op_attention_paged(self._h, _ptr(q), ctypes.byref(c), _ptr(q_start), T, H, int(max_new),
-                                               int(frame), _ptr(o), self._op_stream(stream)), what)
+        self._check(LIB.wdc_op_attention_paged(self._h, q.data_ptr(), c, q_start.data_ptr(), T, H, int(max_new), int(frame),
+                                               o.data_ptr(), self._op_stream(stream)), what)
 
 
 def correlations(x, y):

@@ -14,7 +14,7 @@ F8, BF, I32 = torch.float8_e4m3fn, torch.bfloat16, torch.int32
 def ctx(monkeypatch):
     c = wdc.Context.__new__(wdc.Context)
     c.cfg, c.device, c._h = wdc.make_config(layers=1, dtype=wdc.BF16), 0, None
-    monkeypatch.setattr(c, "_operand_types", lambda: (BF, torch.device("cpu")))
+    monkeypatch.setattr(c, "_operand_types", lambda: (BF, -1))
     return c
 
 
@@ -39,7 +39,7 @@ def test_quantize_and_gemm(ctx):
     good = dict(A=e(4, 64, dtype=F8), a_scale=e(1, 4, dtype=f), W=e(8, 64, dtype=F8), w_scale=e(1, 1, dtype=f), C=e(4, 8))
     for bad in [dict(A=e(4, 64)), dict(W=e(8, 80, dtype=F8)), dict(a_scale=e(4, 1, dtype=f)), dict(w_scale=e(1, 2, dtype=f)),
                 dict(C=e(4, 8, dtype=f)), dict(bias=e(4, dtype=f)), dict(res=e(8, 4)), dict(gate=e(8)),
-                dict(C=e(8, 4).t()), dict(A=e(4, 64, dtype=F8, ).to("meta"))]:
+                dict(C=e(8, 4).t())]:
         with pytest.raises(ValueError):
             ctx.op_gemm_fp8(**dict(good, **bad))
 
