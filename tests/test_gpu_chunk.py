@@ -57,6 +57,21 @@ def test_quantize(contexts, M, K, rows, kind):
     assert bool((buf[M:].float() == 3.0).all()) and bool((scale[ws.size:] == 7.0).all())
 
 
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_quotients_are_ieee(contexts, rows):
+    """Scales of every size, from subnormal to the largest, and values of every size below them: bit for bit."""
+    g = np.random.default_rng(5)
+    M, K = 256 * rows // (2 if rows > 1 else 1), 256
+    top = np.exp2(g.integers(-149, 127, (M // rows, K // 128))).repeat(rows, 0).repeat(128, 1)
+    with np.errstate(over="ignore", under="ignore"):
+        x = (top * (1 + g.random((M, K))) * np.exp2(-g.integers(0, 20, (M, K))) * g.choice([-1, 1], (M, K))).astype(np.float32)
+    x = np.clip(x, -3e38, 3e38)
+    want, ws = chunk.quantize(x, rows)
+    q, s = torch.empty(M, K, device="cuda", dtype=torch.float8_e4m3fn), torch.empty(ws.shape, device="cuda")
+    contexts["f32"].op_quantize_fp8(dev(x), q, s, block_rows=rows)
+    assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(host(q), want)
+
+
 def test_quantize_rows_that_lie_apart(contexts):
     x = rows_of(12, 20, 400, "bf16")
     t = dev(x, torch.bfloat16)
