@@ -107,6 +107,7 @@ constexpr int kPlanned = 2;            // sequences a lane; more than 32 of thes
 // come first within a head.
 struct Item : PagedSeq {
     int b, h, qb, part, parts, chunk;
+    int j0, nj;                        // its steps
     int slot;                          // of the unit's first part in the plan: where its workspace rows begin
 };
 
@@ -351,6 +352,12 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
     if (warp == 0) {
         Item it{};
         const bool has = find_item<D, NT>(g, blockIdx.x, lane, it);
+        if (has) {
+            const int keys = paged_limit(it, g.frame, min((it.qb + 1) * NT * g.tpt, it.n) - 1);
+            const int steps = (keys + BKV - 1) / BKV;
+            it.j0 = it.parts > 1 ? min(it.part * it.chunk, steps) : 0;
+            it.nj = (it.parts > 1 ? min(it.j0 + it.chunk, steps) : steps) - it.j0;
+        }
         if (lane == 0) {
             s_item = it;
             s_has = has;
@@ -380,10 +387,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
 
     const int tok0 = un.qb * NT * g.tpt;                      // the chunk's first token here
     const int nt = NT == 2 && tok0 + g.tpt < un.n ? 2 : 1;    // tiles with rows
-    const int keys = paged_limit(un, g.frame, min(tok0 + NT * g.tpt, un.n) - 1);
-    const int steps = (keys + BKV - 1) / BKV;
-    const int j0 = un.parts > 1 ? min(un.part * un.chunk, steps) : 0;
-    const int nj = (un.parts > 1 ? min(j0 + un.chunk, steps) : steps) - j0;
+    const int j0 = un.j0, nj = un.nj;
     const int page = 1 << g.page_log2;
     const int used = (un.len + page - 1) >> g.page_log2;      // pages of the sequence
     // rows of the last step's V that lie behind the sequence, in its last page
@@ -394,15 +398,11 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
     if (wg == 0) {
         if constexpr (NT == 2) setmaxnreg_dec<C::REGS_CONTROL>();
         if (warp == 0 || warp == 3) {
-            // producers: warp 0 of Q and K, warp 3 of V (one for all three is behind
+            // producers: warp 0 of K, warp 3 of Q and V (one for all three is behind
             // with pages of 16: 16 boxes a step at d = 128)
             const bool of_v = warp == 3;
-            if (!of_v && un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
-                const int given = g.length[un.b];
-                if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
-            }
             if (nj > 0) {
-                if (!of_v && elect_one()) {
+                if (of_v && elect_one()) {
                     mbar_arrive_expect_tx(q_full, (uint32_t)(nt * C::ATOMS * g.G * g.tpt) * 128u);
                     for (int t = 0; t < nt; ++t)
                         for (int a = 0; a < C::ATOMS; ++a)
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                         if (lane == 0) mbar_arrive(v_ready);
                     }
                 }
-                if (!of_v) {
+                if (of_v) {
                     const unsigned long long t0 = globaltimer();
                     while (!mbar_try_wait(q_full, 0) && globaltimer() - t0 < kWaitLimitNs) {
                     }
@@ -474,6 +474,10 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                     while (!mbar_try_wait(&kv_full[s], (parity >> s) & 1) && globaltimer() - t0 < kWaitLimitNs) {
                     }
                 }
+            }
+            if (!of_v && un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
+                const int given = g.length[un.b];
+                if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
             }
         } else if (((NT == 1 && warp == 1) || (NT == 2 && warp - 1 < nt && warp <= 2)) && nj > 0) {
             constexpr uint32_t idesc_s = idesc_bf16(BQ, BKV);

@@ -233,42 +233,69 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (g.bias) bias = ld_chain(g.bias + n);
         if (g.gate) gate = ld_chain(g.gate + n);
     }
-    auto put = [&](int c, float v) {
+    // residuals are fetched before the first result is stored (C may be where they lie,
+    // so the compiler leaves each load behind the store before it)
+    const T* res = reinterpret_cast<const T*>(g.res);
+    auto fetch_res = [&](int c) {
+        const int m = m0 + c;
+        return g.res && mine && m < g.M ? ld_act<T>(res + (size_t)m * g.N + n) : 0.f;
+    };
+    auto put = [&](int c, float v, float r) {
         const int m = m0 + c;
         if (!mine || m >= g.M) return;
         v += bias;
         if (g.gelu) v = gelu_tanh_f(v);
-        const size_t at = (size_t)m * g.N + n;
-        if (g.res) v = fmaf(gate, v, ld_act<T>(reinterpret_cast<const T*>(g.res) + at));
-        reinterpret_cast<T*>(g.out)[at] = to_act<T>(v);
+        if (g.res) v = fmaf(gate, v, r);
+        reinterpret_cast<T*>(g.out)[(size_t)m * g.N + n] = to_act<T>(v);
     };
     if (S == 1) {
-        if (warp >= 2) {
+        if (warp >= 2 && g.res) {
+            constexpr int CH = BN < 32 ? BN : 32;
 #pragma unroll
-            for (int c = 0; c < BN; ++c) put(c, acc[c]);
+            for (int c0 = 0; c0 < BN; c0 += CH) {
+                float r[CH];
+#pragma unroll
+                for (int c = 0; c < CH; ++c) r[c] = fetch_res(c0 + c);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) put(c0 + c, acc[c0 + c], r[c]);
+            }
+        } else if (warp >= 2) {
+#pragma unroll
+            for (int c = 0; c < BN; ++c) put(c, acc[c], 0.f);
         }
         return;
     }
-    // partial sums lie as [source][token of the share][row of W]
+    // partial sums lie as [source][4 tokens of the share][row of W]: a warp sends
+    // one 512-byte run
     cluster_sync_all();                                    // every ring is free
+    const int share = BN / 4 / S;                          // groups of 4 tokens a CTA finishes
     if (warp >= 2) {
-        int to = 0;
 #pragma unroll
-        for (int c = 0; c < BN; ++c) {
-            while (c >= (to + 1) * BN / S) ++to;
-            const int first = to * BN / S, width = (to + 1) * BN / S - first;
-            const uint32_t off = (uint32_t)((rank * width + c - first) * 128 + row) * 4u;
-            st_shared_cluster_f32(mapa_shared(smem_u32(smem) + off, to), acc[c]);
+        for (int c4 = 0; c4 < BN / 4; ++c4) {
+            const int to = c4 / share;
+            const uint32_t off = (uint32_t)((rank * share + c4 - to * share) * 128 + row) * 16u;
+            st_shared_cluster_v4(mapa_shared(smem_u32(smem) + off, to), __float_as_uint(acc[4 * c4]),
+                                 __float_as_uint(acc[4 * c4 + 1]), __float_as_uint(acc[4 * c4 + 2]),
+                                 __float_as_uint(acc[4 * c4 + 3]));
         }
     }
     cluster_sync_all();
     if (warp >= 2) {
-        const int first = rank * BN / S, width = (rank + 1) * BN / S - first;
-        const float* part = reinterpret_cast<const float*>(smem);
-        for (int c = 0; c < width; ++c) {
-            float v = part[c * 128 + row];
-            for (int p = 1; p < S; ++p) v += part[(p * width + c) * 128 + row];
-            put(first + c, v);
+        const float4* part = reinterpret_cast<const float4*>(smem);
+        for (int i = 0; i < share; ++i) {
+            const int c = 4 * (rank * share + i);
+            float r[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[k] = fetch_res(c + k);
+            float4 v = part[i * 128 + row];
+            for (int p = 1; p < S; ++p) {
+                const float4 x = part[(p * share + i) * 128 + row];
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            put(c, v.x, r[0]);
+            put(c + 1, v.y, r[1]);
+            put(c + 2, v.z, r[2]);
+            put(c + 3, v.w, r[3]);
         }
     }
 }
@@ -329,25 +356,28 @@ wdc_status launch(Ctx* c, const void* A, const void* W, Gemm8Args g, int bn, int
 // The kernel for a shape is the one with the least estimated time, by fits to a
 // sweep (us, bf16, no residual; narrow kernel n<tokens a tile>,<CTAs a tile>; pair
 // kernel p<columns a tile>):
-//                          n16,1  n32,1  n64,1  n16,4   p128   p256
-//   4 x 3072 x 3072          7.7                  8.9
-//   4 x 3072 x 12288        18.2                 11.9
-//   33 x 9216 x 3072        10.3    9.3   12.6
-//   100 x 12288 x 3072      23.7   19.9   19.6
-//   226 x 1024 x 1024        5.5    5.8    8.2           7.6    8.8
-//   226 x 9216 x 3072       33.3   24.2   19.7          12.5   15.3
-//   512 x 3072 x 12288             65.5   57.3          29.9   41.7
-//   512 x 9216 x 3072              44.7   36.5          19.4   16.3
-//   1350 x 3072 x 12288                                 66.6   43.1
-//   4276 x 9216 x 3072                                   129    104
+//                          n16,1  n32,1  n64,1  n16,4  n32,4  n64,4   p128   p256
+//   4 x 3072 x 3072          7.6                  6.1
+//   4 x 3072 x 12288        18.4                  8.9
+//   33 x 9216 x 3072        10.5    9.9   14.0   18.3   16.9   13.0
+//   64 x 1536 x 6144        11.6   14.0   21.4    8.9    8.3   11.4   17.2
+//   100 x 3072 x 12288      26.1   23.2   36.6   28.9   24.0   22.4   29.4
+//   226 x 1024 x 1024        5.8    6.8    9.6   11.3    8.1    8.7    7.6    8.6
+//   226 x 9216 x 3072       34.8   25.7   21.6   82.1   56.9   44.2   12.5   15.2
+//   512 x 3072 x 12288             63.9   59.7          72.8   62.9   29.7   41.7
+//   512 x 9216 x 3072              48.2   40.6         110.4   86.1   19.5   16.0
+//   1350 x 3072 x 12288                                               66.6   43.1
+//   4276 x 9216 x 3072                                                 129    104
 // A narrow CTA takes kStage us for two blocks of K; more CTAs than SMs take turns
-// (two on an SM are each about half as fast); a cluster's launch, barriers and
-// exchange cost kSplit.  A pair takes kBlock us a block of K and kTile a tile.
+// (two on an SM are each about half as fast), each turn with its own end, kEnd; a
+// cluster's launch, barriers and exchange cost kSplit.  A pair takes 0.25 or 0.37 us
+// a block of K and 1 or 1.5 a tile.
 struct Choice {
     int bn, split;                     // split 0: the pair kernel
 };
 Choice choose(const Ctx* c, int M, int N, int kb) {
-    constexpr double kStart[3] = {4.2, 4.3, 5.8}, kStage[3] = {0.29, 0.375, 0.56};
+    constexpr double kStart[3] = {4.2, 4.3, 5.8}, kStage[3] = {0.29, 0.375, 0.56}, kEnd[3] = {0.8, 1.4, 2.3};
+    constexpr double kSplit[3] = {1.2, 1.8, 2.2};
     Choice best{16, 1};
     double least = 1e30;
     auto offer = [&](int bn, int split, double est) {
@@ -359,10 +389,11 @@ Choice choose(const Ctx* c, int M, int N, int kb) {
     for (int i = 0; i < 3; ++i) {
         const int bn = 16 << i;
         const double tiles = (double)((M - 1) / bn + 1) * ((N - 1) / 128 + 1);
-        for (int split = 1; split <= 8 && (split == 1 || 4 * split <= kb); split *= 2) {
-            const double kSplit = split == 1 ? 0.0 : (split == 8 ? 6.0 : 4.2);
+        for (int split = 1; split <= bn / 4 && split <= 8 && (split == 1 || 4 * split <= kb); split *= 2) {
             const int stages = (kb + 2 * split - 1) / (2 * split);
-            offer(bn, split, kStart[i] + ceil(tiles * split / c->num_sms) * stages * kStage[i] + kSplit);
+            const double again = ceil(tiles * split / c->num_sms) - 1.0;
+            offer(bn, split, kStart[i] + stages * kStage[i] + again * (stages * kStage[i] + kEnd[i]) +
+                                 (split > 1 ? kSplit[i] : 0.0));
         }
     }
     if (c->num_sms >= 2) {
