@@ -498,7 +498,7 @@ wdc_status wdc_op_attention(wdc_ctx* ctx, const void* q, const void* k, const vo
  * asynchronous on `stream`, need a context with a denoiser (layers > 0: it gives
  * the model dtype), check their arguments before any launch (pointers 16-byte
  * aligned unless said) and may be captured into a graph.  A call with no rows
- * (M == 0, T == 0 or no sequences) returns WDC_OK and launches nothing.  What
+ * (M, T, max_new or the number of sequences 0) returns WDC_OK and launches nothing.  What
  * only the device knows (page numbers, lengths, starts, positions) cannot be
  * refused: a value out of range sets bit 2 (wdc_device_errors), and nothing is
  * read or written outside the arrays given here. */
@@ -589,10 +589,11 @@ wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* ctx, const void* qkv, long long l
  * A row that sees nothing is zero.  Whatever a page holds behind its sequence's
  * last token is not used, infinities and NaN included; a non-finite value V of a
  * token within the sequence may reach every row of the chunk.  Rows from
- * q_start[sequences] on are left as they are.  A bf16 model may split a
- * sequence's keys over several CTAs and merge them with a second kernel through
- * the workspace wdc_op_attention uses: two attention calls of one context must
- * not run concurrently on different streams. */
+ * q_start[sequences] on are left as they are.  A sequence's keys may be split over
+ * several CTAs and merged, through the workspace wdc_op_attention uses: two
+ * attention calls of one context, and graphs that hold some, must not run
+ * concurrently.  How they are split follows from the lengths of all sequences of
+ * the call (the results of equal calls are equal bit for bit). */
 wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_cache* cache, const int* q_start,
                                   int T, int heads, int max_new, int frame, void* o, wdc_stream stream);
 

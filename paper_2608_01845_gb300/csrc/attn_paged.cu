@@ -624,8 +624,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                 return (lo[0] + lo[1]) + (hi[0] + hi[1]);
             };
             float base = m_run;
-            // a row that has seen nothing yet (in a masked step, or the first)
-            if (decltype(masked)::value ? __any_sync(0xffffffffu, l_run == 0.f) : j == 0) {
+            if (__any_sync(0xffffffffu, l_run == 0.f)) {     // a row that has seen nothing yet
                 const float top = tile_max() * g.scale_log2;
                 if (l_run == 0.f) base = top == -INFINITY ? 0.f : top;
             }

@@ -438,6 +438,67 @@ def test_attention_more_new_rows_than_promised(contexts):
     assert bool((o[256:] == 5.0).all())
 
 
+def test_attention_shared_pages(contexts):
+    """Two sequences with the same first pages, and a page that a sequence's table names twice."""
+    ctx = contexts["bf16"]
+    P = Paged(84, [150, 170], 32, 2, 64)
+    P.table[1, :3] = P.table[0, :3]
+    P.table[1, 4] = P.table[1, 3]
+    P.k[P.table[1, 3]], P.v[P.table[1, 3]] = 0.25, 0.5             # (both its places are filled)
+    P.dtable.copy_(dev(P.table, torch.int32))
+    P.dk.copy_(dev(P.k, torch.bfloat16))
+    P.dv.copy_(dev(P.v, torch.half))
+    q = synth.bf16_round(synth.normal(85, (12, 4, 64)))
+    o = attend(ctx, q, P, [5, 7], 1)
+    want, mag = chunk.attention_paged(q, P.k, P.v, P.table, [150, 170], starts([5, 7]), 1)
+    assert (np.abs(host(o).reshape(want.shape) - want) <= attention_bound(want, mag, 170)).all()
+
+
+def test_attention_scores_of_minus_infinity(contexts):
+    """Keys whose scores are -infinity (visible ones) have no weight, however many come first; a row of nothing else is zero."""
+    ctx = contexts["bf16"]
+    for d, H in ((64, 2), (128, 1)):
+        P = Paged(86, [300], 16, 1, d)
+        for i in range(256):
+            P.k[P.table[0, i // 16], 0, i % 16, 0] = -np.inf
+        P.dk.copy_(dev(P.k, torch.bfloat16))
+        q = synth.bf16_round(synth.normal(87, (300, H, d)))
+        q[:, :, 0] = np.abs(q[:, :, 0]) + 0.5
+        q[:, :, 1:] *= 8                                           # finite scores far below 0 among them
+        o = attend(ctx, q, P, [300], 1)
+        with np.errstate(invalid="ignore"):
+            want, mag = chunk.attention_paged(q, P.k, P.v, P.table, [300], starts([300]), 1)
+        got = host(o).reshape(want.shape)
+        assert (got[:256] == 0).all()
+        assert (np.abs(got - want) <= attention_bound(want, mag, 300)).all()
+
+
+def test_two_contexts_at_once_on_streams_of_their_own(contexts):
+    """Calls of two contexts overlap on two streams (given and current); each gives what it gives alone."""
+    other = wdc.Context(wdc.make_config(dtype=wdc.BF16, **MODEL), 2)
+    jobs = []
+    for i, (ctx, lens, H) in enumerate(((contexts["bf16"], [3000, 1, 77], 8), (other, [900, 2500], 6))):
+        P = Paged(88 + i, lens, 64, 2, 128)
+        new = [1] * len(lens)
+        q = dev(synth.normal(90 + i, (len(lens), H, 128)), torch.bfloat16)
+        o = torch.zeros(len(lens), H * 128, device="cuda", dtype=torch.bfloat16)
+        jobs.append((ctx, q, P, dev(starts(new), torch.int32), o))
+    want = []
+    for ctx, q, P, s, o in jobs:
+        ctx.op_attention_paged(q, P.cache, s, o, 1)
+        want.append(o.clone())
+        o.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        jobs[0][0].op_attention_paged(*jobs[0][1:2], jobs[0][2].cache, jobs[0][3], jobs[0][4], 1, stream=streams[0])
+        with torch.cuda.stream(streams[1]):
+            jobs[1][0].op_attention_paged(*jobs[1][1:2], jobs[1][2].cache, jobs[1][3], jobs[1][4], 1)
+    torch.cuda.synchronize()
+    for w, j in zip(want, jobs):
+        assert torch.equal(w, j[4])
+
+
 # ---------------------------------------------------------------- together
 def chunk_path(ctx, t, P, start, new, frame):
     """A block's attention half on a chunk: fp8 QKV projection, norms and rotation into the cache, attention, fp8 output
