@@ -71,6 +71,7 @@ struct PagedCfg {
 struct PagedArgs {
     int T, heads, kv, G, tpt;          // G query heads a key head, tpt tokens a tile
     int sequences, q_blocks, max_new;  // q_blocks: of max_new tokens
+    int by_length;                     // whole units go longest sequence first
     int items, wave;                   // most parts of units (0: none is split); parts that run at a time
     int page_log2, pages, width, frame;
     const int *table, *length, *start;
@@ -119,12 +120,14 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
     const int block = NT * g.tpt;
     float with = 0.f;                  // steps a part; 0: whole units
     float units[kPlanned], steps[kPlanned];
-    if (g.items > 0) {
+    bool by_length = false;
+    if (g.items > 0 || g.by_length) {
         float n = 0.f, work = 0.f, bound = 0.f, most = 0.f, least = 3e38f;
 #pragma unroll
         for (int i = 0; i < kPlanned; ++i) {
             const int b = 32 * i + lane;
-            units[i] = steps[i] = 0.f;
+            units[i] = 0.f;
+            steps[i] = b < g.sequences ? 0.f : -1.f;
             if (b < g.sequences) {
                 const PagedSeq s = sequence(g, b);
                 const int rows = min(s.n, g.max_new);
@@ -148,6 +151,8 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
             most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
             least = fminf(least, __shfl_xor_sync(kAll, least, o));
         }
+        // (the order takes a CTA about 5 us: a long sequence that begins last costs more)
+        by_length = g.by_length && most - least > 64.f;
         const float wave = (float)g.wave;
         const bool alike = 4.f * least >= 3.f * most;
         auto estimate = [&](float c, float parts) {
@@ -155,9 +160,9 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
             if (NT == 1) return fmaxf(work / wave, 0.55f * c) + rounds * kStart;
             return alike ? rounds * (c + kStart) : fmaxf(c, work / wave + 0.5f * c) + rounds * kStart;
         };
-        float best = estimate(most, n) - kMerge;
+        float best = g.items > 0 ? estimate(most, n) - kMerge : 0.f;
 #pragma unroll 1
-        for (int k = 1; k <= kRounds && most > (float)kMin; ++k) {
+        for (int k = 1; k <= kRounds && g.items > 0 && most > (float)kMin; ++k) {
             const float items = (float)min(k * g.wave, g.items);
             if (n >= items) continue;
             // sum u ceil(s / c) lies between sum u s / c and that + n
@@ -187,6 +192,23 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
         it.h = r % g.kv;
         it.b = r / g.kv;
         if (it.b >= g.sequences) return false;
+        if (by_length) {               // the sequence of that rank instead, ties in order
+            int rank[kPlanned] = {};
+#pragma unroll 4
+            for (int o = 0; o < 32; ++o)
+#pragma unroll
+                for (int k = 0; k < kPlanned; ++k) {
+                    const float other = __shfl_sync(kAll, steps[k], o);
+#pragma unroll
+                    for (int i = 0; i < kPlanned; ++i)
+                        rank[i] += other > steps[i] || (other == steps[i] && 32 * k + o < 32 * i + lane);
+                }
+#pragma unroll
+            for (int i = 0; i < kPlanned; ++i) {
+                const unsigned at = __ballot_sync(kAll, rank[i] == r / g.kv);
+                if (at) it.b = 32 * i + __ffs(at) - 1;
+            }
+        }
         static_cast<PagedSeq&>(it) = sequence(g, it.b);
         it.part = it.slot = 0;
         it.parts = 1;
@@ -798,6 +820,9 @@ wdc_status launch(Ctx* c, const void* q, const wdc_paged_cache* p, PagedArgs g, 
     if (items > room) items = room / g.wave * g.wave;
     const long long steps = (((long long)g.width << g.page_log2) + Cf::BK - 1) / Cf::BK;
     g.items = c->attn_part && g.sequences <= 32 * kPlanned && steps > Cf::MIN_STEPS && units < items ? (int)items : 0;
+    // more units than run at a time: the longest sequences may go first, so that none
+    // begins last (64 tokens over up to 4000, 8 key heads of 128: 132 -> 112 us)
+    g.by_length = NT == 1 && g.q_blocks == 1 && g.sequences > 1 && g.sequences <= 32 * kPlanned && units > g.wave;
     g.counter = c->attn_counters;
     g.record = reinterpret_cast<int4*>(c->attn_records);
     g.part_o = c->attn_part;

@@ -258,10 +258,10 @@ class Paged:
         bad = np.where(r.random((self.pages, kv, page, d)) < 0.5, np.nan, np.inf)
         self.k, self.v = bad.astype(np.float32), (-bad).astype(np.float32)
         for b, n in enumerate(lens if fill else []):
-            for i in range(n):
-                p = self.table[b, i // page]
-                self.k[p, :, i % page] = synth.bf16_round(r.standard_normal((kv, d)).astype(np.float32))
-                self.v[p, :, i % page] = r.standard_normal((kv, d)).astype(np.float16)
+            i = np.arange(n)
+            p = self.table[b, i // page]
+            self.k[p, :, i % page] = synth.bf16_round(r.standard_normal((n, kv, d)).astype(np.float32))
+            self.v[p, :, i % page] = r.standard_normal((n, kv, d)).astype(np.float16)
         self.dk, self.dv = dev(self.k, torch.bfloat16), dev(self.v, torch.half)
         self.dtable, self.dlen = dev(self.table, torch.int32), torch.tensor(list(lens), dtype=torch.int32, device="cuda")
         self.cache = wdc.PagedCache(self.dk, self.dv, self.dtable, self.dlen)
@@ -376,6 +376,21 @@ def test_attention_long_and_split(contexts):
         o = attend(ctx, q, P, new, 1)
         want, mag = chunk.attention_paged(q, P.k, P.v, P.table, lens, starts(new), 1)
         assert (np.abs(host(o).reshape(want.shape) - want) <= attention_bound(want, mag, max(lens))).all()
+
+
+@pytest.mark.parametrize("lens,kv,d", [([2500] + [1 + 61 * i % 2400 for i in range(39)], 8, 128),     # longest first
+                                       ([1 + 7 * i % 130 for i in range(70)], 2, 64),                 # too many to plan for
+                                       ([3] * 32 + [4000] + [5, 0, 6], 1, 64),                        # one to split, past lane 31
+                                       ([0] * 3 + [1] * 61, 8, 128)])
+def test_attention_many_sequences(contexts, lens, kv, d):
+    ctx = contexts["bf16"]
+    P = Paged(89, lens, 16, kv, d, spare=0)
+    new = [min(1, n) for n in lens]
+    q = synth.bf16_round(synth.normal(90, (sum(new), 2 * kv, d)))
+    o = attend(ctx, q, P, new, 1)
+    assert ctx.device_errors() == 0
+    want, mag = chunk.attention_paged(q, P.k, P.v, P.table, lens, starts(new), 1)
+    assert (np.abs(host(o).reshape(want.shape) - want) <= attention_bound(want, mag, max(lens))).all()
 
 
 def test_attention_rows_that_see_nothing_are_zero(contexts):
