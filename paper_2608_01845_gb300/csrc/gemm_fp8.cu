@@ -377,7 +377,7 @@ struct Choice {
 };
 Choice choose(const Ctx* c, int M, int N, int kb) {
     constexpr double kStart[3] = {4.2, 4.3, 5.8}, kStage[3] = {0.29, 0.375, 0.56}, kEnd[3] = {0.8, 1.4, 2.3};
-    constexpr double kSplit[3] = {1.2, 1.8, 2.2};
+    constexpr double kSplit[3] = {1.9, 1.9, 2.2};
     Choice best{16, 1};
     double least = 1e30;
     auto offer = [&](int bn, int split, double est) {

@@ -259,6 +259,19 @@ def _tensor(what, name, t, dtype, shape, device, row_stride=False):
     raise ValueError(f"{what}: {name} must be contiguous")
 
 
+_raw_stream = None
+
+
+def _current_stream():
+    """device index -> address of the current stream, without a Stream object where torch offers that."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -280,7 +293,7 @@ class Context:
                             ctypes.byref(self._h))
         if st != 0:
             raise WdcError(st, "wdc_create failed")
-        self.device = device
+        self.device, self._types = device, None
 
     def close(self):
         if self._h:
@@ -486,41 +499,41 @@ class Context:
     # ---- chunk operators: the tensors' types, shapes and device are checked here, the rest behind the C ABI
 
     def _operand_types(self):
-        """(element type of the model, device index) that the operators' tensors have."""
-        import torch
-        return (torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32), self.device
+        """(element type of the model, device index, e4m3, fp32, int32) of the operators' tensors."""
+        if self._types is None:
+            import torch
+            self._types = (torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32, self.device, torch.float8_e4m3fn,
+                           torch.float32, torch.int32)
+        return self._types
 
     def _op_stream(self, stream):
         """The given stream, or the current one of the context's device."""
         if stream is None:
-            import torch
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return _current_stream()(self.device)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def op_quantize_fp8(self, x, q, scale, block_rows=1, stream=None):
         """wdc_op_quantize_fp8: x [M, K] (rows may lie apart) to q (float8_e4m3fn [M, K]) and scale
         ([ceil(K/128), M], or with block_rows=128 [ceil(M/128), ceil(K/128)])."""
-        import torch
-        what, (dt, dev) = "op_quantize_fp8", self._operand_types()
+        what, (dt, dev, f8, f32, _) = "op_quantize_fp8", self._operand_types()
         if x.dim() != 2:
             raise ValueError(f"{what}: x must be [M, K]")
         M, K = x.shape
         kb = -(-K // 128)
         _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
-        _tensor(what, "q", q, torch.float8_e4m3fn, (M, K), dev)
-        _tensor(what, "scale", scale, torch.float32, (kb, M) if block_rows == 1 else (-(-M // 128), kb), dev)
+        _tensor(what, "q", q, f8, (M, K), dev)
+        _tensor(what, "scale", scale, f32, (kb, M) if block_rows == 1 else (-(-M // 128), kb), dev)
         self._check(LIB.wdc_op_quantize_fp8(self._h, x.data_ptr(), _row_stride(x), q.data_ptr(), scale.data_ptr(), M, K,
                                             block_rows, self._op_stream(stream)), what)
 
     def op_gemm_fp8(self, A, a_scale, W, w_scale, C, bias=None, gelu=False, res=None, gate=None, stream=None):
         """wdc_op_gemm_fp8: C = epilogue(A W^T) of float8_e4m3fn matrices with the scales of op_quantize_fp8
         (block_rows=1 for A, 128 for W)."""
-        import torch
-        what, (dt, dev) = "op_gemm_fp8", self._operand_types()
+        what, (dt, dev, f8, f32, _) = "op_gemm_fp8", self._operand_types()
         if A.dim() != 2 or W.dim() != 2:
             raise ValueError(f"{what}: A must be [M, K] and W [N, K]")
         (M, K), N = A.shape, W.shape[0]
-        kb, f8, f32 = -(-K // 128), torch.float8_e4m3fn, torch.float32
+        kb = -(-K // 128)
         _tensor(what, "A", A, f8, (M, K), dev)
         _tensor(what, "W", W, f8, (N, K), dev)
         _tensor(what, "a_scale", a_scale, f32, (kb, M), dev)
@@ -536,15 +549,14 @@ class Context:
                                         _address(bias), C.data_ptr(), M, N, K, int(gelu), _address(res), _address(gate),
                                         self._op_stream(stream)), what)
 
-    def _head_norm(self, what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved):
-        import torch
-        f32 = torch.float32
+    def _head_norm(self, what, d, T, q_weight, k_weight, eps, rot, positions, interleaved):
+        _, dev, _, f32, i32 = self._operand_types()
         if q_weight is not None:
             _tensor(what, "q_weight", q_weight, f32, (d,), dev)
         if k_weight is not None:
             _tensor(what, "k_weight", k_weight, f32, (d,), dev)
         if positions is not None:
-            _tensor(what, "positions", positions, torch.int32, (T,), dev)
+            _tensor(what, "positions", positions, i32, (T,), dev)
         at, n, pairs = None, 0, 0
         if rot is not None:
             if rot.dim() != 3 or rot.shape[2] != 2:
@@ -558,8 +570,7 @@ class Context:
                         interleaved=True, stream=None):
         """wdc_op_qk_norm_rope: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) to q [heads, T, d],
         k [kv_heads, T, d] and vt [kv_heads, d, T rounded up to 8] (fp16; fp32 and T for an fp32 model)."""
-        import torch
-        what, (dt, dev) = "op_qk_norm_rope", self._operand_types()
+        what, (dt, dev, _, f32, _) = "op_qk_norm_rope", self._operand_types()
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError(f"{what}: q must be [heads, T, d] and k [kv_heads, T, d]")
         (H, T, d), kv = q.shape, k.shape[0]
@@ -567,9 +578,10 @@ class Context:
         _tensor(what, "q", q, dt, (H, T, d), dev)
         _tensor(what, "k", k, dt, (kv, T, d), dev)
         if vt is not None:
-            bf16 = dt is torch.bfloat16
+            import torch
+            bf16 = dt is not f32
             _tensor(what, "vt", vt, torch.float16 if bf16 else dt, (kv, d, -(-T // 8) * 8 if bf16 else T), dev)
-        n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        n = self._head_norm(what, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
         self._check(LIB.wdc_op_qk_norm_rope(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, kv, d, n, q.data_ptr(),
                                             k.data_ptr(), _address(vt), self._op_stream(stream)), what)
 
@@ -577,8 +589,7 @@ class Context:
                                positions=None, interleaved=True, stream=None):
         """wdc_op_qk_norm_rope_append: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) of new tokens to
         q [T, heads, d], their keys and values into ``cache`` (a PagedCache); q_start int32 [sequences + 1]."""
-        import torch
-        what, (dt, dev) = "op_qk_norm_rope_append", self._operand_types()
+        what, (dt, dev, _, _, i32) = "op_qk_norm_rope_append", self._operand_types()
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
@@ -586,16 +597,15 @@ class Context:
             raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "qkv", qkv, dt, (T, (H + 2 * c.kv_heads) * d), dev, row_stride=True)
         _tensor(what, "q", q, dt, (T, H, d), dev)
-        _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
-        n = self._head_norm(what, dev, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        _tensor(what, "q_start", q_start, i32, (c.sequences + 1,), dev)
+        n = self._head_norm(what, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
         self._check(LIB.wdc_op_qk_norm_rope_append(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, n, c,
                                                    q_start.data_ptr(), q.data_ptr(), self._op_stream(stream)), what)
 
     def op_attention_paged(self, q, cache, q_start, o, max_new, frame=1, stream=None):
         """wdc_op_attention_paged: q [T, heads, d] over ``cache`` (a PagedCache) into o [T, heads * d]; no
         sequence has more than max_new new tokens."""
-        import torch
-        what, (dt, dev) = "op_attention_paged", self._operand_types()
+        what, (dt, dev, _, _, i32) = "op_attention_paged", self._operand_types()
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
@@ -603,7 +613,7 @@ class Context:
             raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "q", q, dt, (T, H, d), dev)
         _tensor(what, "o", o, dt, (T, H * d), dev)
-        _tensor(what, "q_start", q_start, torch.int32, (c.sequences + 1,), dev)
+        _tensor(what, "q_start", q_start, i32, (c.sequences + 1,), dev)
         self._check(LIB.wdc_op_attention_paged(self._h, q.data_ptr(), c, q_start.data_ptr(), T, H, int(max_new), int(frame),
                                                o.data_ptr(), self._op_stream(stream)), what)
 

@@ -14,7 +14,7 @@ F8, BF, I32 = torch.float8_e4m3fn, torch.bfloat16, torch.int32
 def ctx(monkeypatch):
     c = wdc.Context.__new__(wdc.Context)
     c.cfg, c.device, c._h = wdc.make_config(layers=1, dtype=wdc.BF16), 0, None
-    monkeypatch.setattr(c, "_operand_types", lambda: (BF, -1))
+    monkeypatch.setattr(c, "_operand_types", lambda: (BF, -1, F8, torch.float32, I32))
     return c
 
 
