@@ -165,20 +165,26 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
         for (int k = 1; k <= kRounds && g.items > 0 && most > (float)kMin; ++k) {
             const float items = (float)min(k * g.wave, g.items);
             if (n >= items) continue;
-            // sum u ceil(s / c) lies between sum u s / c and that + n
-            float lo = fminf(most, fmaxf((float)kMin, floorf(bound / items)));
-            float hi = fminf(most, fmaxf(lo, ceilf(bound / (items - n)) + 1.f)), c, parts;
+            float c, parts;
+            if (g.sequences == 1) {    // as many parts a unit as there are places
+                c = fmaxf((float)kMin, ceilf(most / floorf(items / n)));
+                parts = n * ceilf(most / c);
+            } else {
+                // sum u ceil(s / c) lies between sum u s / c and that + n
+                float lo = fminf(most, fmaxf((float)kMin, floorf(bound / items)));
+                float hi = fminf(most, fmaxf(lo, ceilf(bound / (items - n)) + 1.f));
 #pragma unroll 1
-            do {
-                c = lo < hi ? floorf(0.5f * (lo + hi)) : lo;
-                parts = 0.f;
+                do {
+                    c = lo < hi ? floorf(0.5f * (lo + hi)) : lo;
+                    parts = 0.f;
 #pragma unroll
-                for (int i = 0; i < kPlanned; ++i) parts += units[i] * fmaxf(1.f, ceilf(steps[i] / c));
-                parts = (float)__reduce_add_sync(kAll, (unsigned)parts);
-                if (lo == hi) break;
-                if (parts <= items) hi = c;
-                else lo = c + 1.f;
-            } while (true);
+                    for (int i = 0; i < kPlanned; ++i) parts += units[i] * fmaxf(1.f, ceilf(steps[i] / c));
+                    parts = (float)__reduce_add_sync(kAll, (unsigned)parts);
+                    if (lo == hi) break;
+                    if (parts <= items) hi = c;
+                    else lo = c + 1.f;
+                } while (true);
+            }
             const float est = estimate(c, parts);
             if (c < most && parts <= items && est < best) {
                 best = est;
