@@ -552,7 +552,8 @@ typedef struct wdc_head_norm {
     const float* k_weight;
     float eps;                  /* >= 0                                           */
     const float* rot;           /* device [rot_positions][rot_dim / 2][cos, sin], or NULL: no rotation */
-    int rot_positions, rot_dim; /* rot_dim a multiple of 16, at most head_dim     */
+    int rot_positions, rot_dim; /* rot_dim a multiple of 16, at most head_dim (not looked at
+                                   without rot)                                   */
     int interleaved;            /* 1: pairs (2 i, 2 i + 1); 0: pairs (i, i + rot_dim / 2) */
     const int* positions;       /* device [T] (4-byte aligned), or NULL: the token's place in its
                                    sequence.  A position outside the table sets bit 2, and the

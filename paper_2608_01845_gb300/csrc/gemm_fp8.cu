@@ -2,10 +2,11 @@
 // (tcgen05 kind::f8f6f4, sm_103a):
 //   C[m, n] = epilogue( sum_b sa[b][m] sw[n / 128][b] sum_{k in block b} A[m, k] W[n, k] ),
 // blocks of 128 columns of K.  A block is one 128-byte row of the swizzled
-// shared-memory tiles and four MMAs (32 of K each) into a TMEM buffer of its
-// own; the epilogue warps then add the buffer, times its scales, to sums in
+// shared-memory tiles and four MMAs (32 of K each) into tensor memory, started
+// from zero; the epilogue warps then add that product, times its scales, to sums in
 // their registers, while the next blocks' MMAs fill the other buffers.  So a
-// sum over K is fp32 beyond a block, whatever the scales.
+// sum over K is fp32 beyond a block, whatever the scales.  This file: the entry, the
+// choice of the kernel, and the kernel for few rows; gemm_fp8_pair.cu: many rows.
 #include "gemm_fp8.cuh"
 
 #include <cmath>

@@ -203,9 +203,6 @@ __device__ __forceinline__ void st_shared_cluster_v4(uint32_t cluster_addr, uint
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(a), "r"(b), "r"(c), "r"(d)
                  : "memory");
 }
-__device__ __forceinline__ void st_shared_cluster_f32(uint32_t cluster_addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
-}
 // tcgen05 operations of a CTA pair (.cta_group::2): every tcgen05 instruction
 // of a kernel must use the same cta_group.
 __device__ __forceinline__ void tmem_alloc2(uint32_t* smem_result, uint32_t ncols) {

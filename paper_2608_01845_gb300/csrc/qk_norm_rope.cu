@@ -341,7 +341,7 @@ wdc_status take(Ctx* c, NormArgs& a, const void* qkv, long long ld, int T, int h
     a.qkv = qkv; a.ld = ld; a.T = T; a.heads = heads; a.kv = kv;
     a.wq = n->q_weight; a.wk = n->k_weight; a.eps = n->eps;
     a.rot = n->rot_dim > 0 ? reinterpret_cast<const float2*>(n->rot) : nullptr;
-    a.rot_positions = n->rot_positions; a.rot_dim = n->rot_dim; a.positions = n->positions;
+    a.rot_positions = n->rot_positions; a.rot_dim = a.rot ? n->rot_dim : 0; a.positions = n->positions;
     a.err = c->err;
     return WDC_OK;
 }

@@ -235,6 +235,20 @@ def test_norm_of_zeros_and_without_eps(contexts):
     assert bool(q[0, 0].isnan().all()) and np.allclose(host(k[0, 1]), 1.0, atol=1e-6)
 
 
+def test_rot_dim_without_angles_is_not_looked_at(contexts):
+    x = synth.normal(4, (5, 3 * 64)).astype(np.float32)
+    q, k = torch.empty(1, 5, 64, device="cuda"), torch.empty(1, 5, 64, device="cuda")
+    ctx, dx = contexts["f32"], dev(x)
+    for pairs in (0, 1):
+        n = wdc.HeadNorm(None, None, 1e-5, None, 0, 1 << 20, pairs, None)
+        q.fill_(9)
+        assert wdc.LIB.wdc_op_qk_norm_rope(ctx._h, dx.data_ptr(), 3 * 64, 5, 1, 1, 64, n, q.data_ptr(), k.data_ptr(), None,
+                                           torch.cuda.current_stream().cuda_stream) == 0
+        h = x.reshape(5, 3, 64)
+        want = chunk.norm_rotate(h[:, :1], None, 1e-5, None, np.arange(5), bool(pairs)).transpose(1, 0, 2)
+        assert (np.abs(host(q) - want) <= norm_bound(h, None, want, "f32")).all()
+
+
 def test_positions_outside_the_table_are_reported(contexts):
     ctx = contexts["f32"]
     x, cs = synth.normal(3, (3, 3 * 64)), rotations(4, 64)
