@@ -175,7 +175,7 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
                 float hi = fminf(most, fmaxf(lo, ceilf(bound / (items - n)) + 1.f));
 #pragma unroll 1
                 do {
-                    c = lo < hi ? floorf(0.5f * (lo + hi)) : lo;
+                    c = plan_middle(lo, hi);
                     parts = 0.f;
 #pragma unroll
                     for (int i = 0; i < kPlanned; ++i) parts += units[i] * fmaxf(1.f, ceilf(steps[i] / c));

@@ -3,6 +3,8 @@
 // the results stay within the arrays.
 #pragma once
 
+#include <math.h>
+
 #ifdef __CUDACC__
 #define WDC_INDEX __host__ __device__ __forceinline__
 #else
@@ -37,5 +39,8 @@ WDC_INDEX int paged_limit(const PagedSeq& s, int frame, int i) {
 }
 // A page number that the pool has, or -1.
 WDC_INDEX int paged_page(int p, int pages) { return p >= 0 && p < pages ? p : -1; }
+// The middle of whole numbers lo <= hi <= 2^24, rounded down.  (Their sum may not be
+// a float; with a middle rounded up to hi a bisection would not end.)
+WDC_INDEX float plan_middle(float lo, float hi) { return lo + floorf(0.5f * (hi - lo)); }
 
 }  // namespace wdc

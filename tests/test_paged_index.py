@@ -13,6 +13,16 @@ from oracle import chunk
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2608_01845_gb300", "csrc")
 
+MIDDLE = r"""
+#include "paged_index.h"
+#include <cstdio>
+
+int main() {
+    float lo, hi;
+    while (std::scanf("%f %f", &lo, &hi) == 2) std::printf("%.0f\n", wdc::plan_middle(lo, hi));
+}
+"""
+
 PROGRAM = r"""
 #include "paged_index.h"
 #include <cstdio>
@@ -30,15 +40,19 @@ int main() {
 """
 
 
-@pytest.fixture(scope="module")
-def program(tmp_path_factory):
+def compiled(source, d):
     cxx = shutil.which("g++")
     if cxx is None:
         pytest.skip("no C++ compiler")
-    d = tmp_path_factory.mktemp("paged")
     src, exe = d / "paged.cpp", d / "paged"
-    src.write_text(PROGRAM)
+    src.write_text(source)
     subprocess.run([cxx, "-std=c++17", "-O1", "-ftrapv", "-I", CSRC, str(src), "-o", str(exe)], check=True)
+    return exe
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    exe = compiled(PROGRAM, tmp_path_factory.mktemp("paged"))
 
     def run(cases):
         r = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True,
@@ -73,3 +87,11 @@ def test_bad_values_stay_within_the_arrays(program):
         if n:
             for place, lim in np.array(got[4:]).reshape(-1, 2):
                 assert place < L and 0 <= lim <= L
+
+
+def test_middle_of_a_bisection_up_to_the_longest_sequence(tmp_path):
+    exe = compiled(MIDDLE, tmp_path)
+    top = 2 ** 24                      # steps of 64 keys of 2^30
+    cases = [(lo, hi) for hi in (1, 2, 9, 2 ** 23, 2 ** 23 + 2, top - 1, top) for lo in (0, 1, hi - 3, hi - 2, hi - 1, hi) if 0 <= lo <= hi]
+    r = subprocess.run([str(exe)], input="\n".join(f"{lo} {hi}" for lo, hi in cases), capture_output=True, text=True, check=True)
+    assert [int(x) for x in r.stdout.split()] == [(lo + hi) // 2 for lo, hi in cases]
