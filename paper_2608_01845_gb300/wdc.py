@@ -237,6 +237,7 @@ class PagedCache:
         if k.dim() != 4 or table.dim() != 2 or length.dim() != 1 or table.shape[0] != length.shape[0]:
             raise ValueError("PagedCache: k [pages, kv_heads, page, d], table [sequences, width], length [sequences]")
         self.device = dev = k.get_device()
+        _sizes("PagedCache", *k.shape, *table.shape)
         _tensor("PagedCache", "k", k, torch.bfloat16, k.shape, dev)
         _tensor("PagedCache", "v", v, torch.float16, k.shape, dev)
         _tensor("PagedCache", "table", table, torch.int32, table.shape, dev)
@@ -257,6 +258,16 @@ def _tensor(what, name, t, dtype, shape, device, row_stride=False):
     if t.get_device() != device:
         raise ValueError(f"{what}: {name} is on {t.device}, not on device {device}")
     raise ValueError(f"{what}: {name} must be contiguous")
+
+
+_INT_MAX = 0x7fffffff
+
+
+def _sizes(what, *n):
+    """Sizes that the C ABI takes as ints."""
+    for v in n:
+        if v > _INT_MAX:
+            raise ValueError(f"{what}: a size of {v} (at most {_INT_MAX})")
 
 
 _raw_stream = None
@@ -519,6 +530,7 @@ class Context:
         if x.dim() != 2:
             raise ValueError(f"{what}: x must be [M, K]")
         M, K = x.shape
+        _sizes(what, M, K)
         kb = -(-K // 128)
         _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
         _tensor(what, "q", q, f8, (M, K), dev)
@@ -533,6 +545,7 @@ class Context:
         if A.dim() != 2 or W.dim() != 2:
             raise ValueError(f"{what}: A must be [M, K] and W [N, K]")
         (M, K), N = A.shape, W.shape[0]
+        _sizes(what, M, N, K)
         kb = -(-K // 128)
         _tensor(what, "A", A, f8, (M, K), dev)
         _tensor(what, "W", W, f8, (N, K), dev)
@@ -574,6 +587,7 @@ class Context:
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError(f"{what}: q must be [heads, T, d] and k [kv_heads, T, d]")
         (H, T, d), kv = q.shape, k.shape[0]
+        _sizes(what, T, H, kv)
         _tensor(what, "qkv", qkv, dt, (T, (H + 2 * kv) * d), dev, row_stride=True)
         _tensor(what, "q", q, dt, (H, T, d), dev)
         _tensor(what, "k", k, dt, (kv, T, d), dev)
@@ -593,6 +607,7 @@ class Context:
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
+        _sizes(what, T, H)
         if cache.device != dev or d != c.head_dim:
             raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "qkv", qkv, dt, (T, (H + 2 * c.kv_heads) * d), dev, row_stride=True)
@@ -609,12 +624,14 @@ class Context:
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
         (T, H, d), c = q.shape, cache.c
+        _sizes(what, T, H)
         if cache.device != dev or d != c.head_dim:
             raise ValueError(f"{what}: the cache must be on device {dev} with heads of {d}")
         _tensor(what, "q", q, dt, (T, H, d), dev)
         _tensor(what, "o", o, dt, (T, H * d), dev)
         _tensor(what, "q_start", q_start, i32, (c.sequences + 1,), dev)
-        self._check(LIB.wdc_op_attention_paged(self._h, q.data_ptr(), c, q_start.data_ptr(), T, H, int(max_new), int(frame),
+        self._check(LIB.wdc_op_attention_paged(self._h, q.data_ptr(), c, q_start.data_ptr(), T, H,
+                                               max(-1, min(int(max_new), T)), max(-1, min(int(frame), _INT_MAX)),
                                                o.data_ptr(), self._op_stream(stream)), what)
 
 

@@ -73,6 +73,50 @@ def test_cache_tensors():
     assert (c.pages, c.page, c.kv_heads, c.head_dim, c.sequences, c.table_width) == (3, 16, 1, 64, 2, 4)
 
 
+def test_sizes_beyond_an_int(ctx, monkeypatch):
+    """What the C ABI's ints would cut off is refused, or (max_new, frame) means what a smaller one does."""
+    f, m = torch.float32, lambda *s, dtype=BF: torch.empty(*s, dtype=dtype, device="meta")
+    big = 2 ** 32 + 1
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_quantize_fp8(m(big, 16), m(big, 16, dtype=F8), m(1, big, dtype=f))
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_gemm_fp8(m(big, 16, dtype=F8), m(1, big, dtype=f), m(8, 16, dtype=F8), m(1, 1, dtype=f), m(big, 8))
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_qk_norm_rope(m(big, 3 * 64), m(1, big, 64), m(1, big, 64))
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_qk_norm_rope_append(m(big, 3 * 64), m(big, 1, 64), cache(), e(2, dtype=I32))
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_attention_paged(m(big, 1, 64), cache(), e(2, dtype=I32), m(big, 64), 1)
+    with pytest.raises(ValueError, match="a size of"):
+        wdc.PagedCache(m(3, 1, 16, 64), m(3, 1, 16, 64, dtype=torch.half), m(1, big, dtype=I32), m(1, dtype=I32))
+    seen = []
+    monkeypatch.setattr(wdc.LIB, "wdc_op_attention_paged", lambda *a: seen.append(a[6:8]) or 0)
+    monkeypatch.setattr(ctx, "_op_stream", lambda s: 0)
+    for new, frame in [(2 ** 32 + 2, 2 ** 32), (-2 ** 32, 2 ** 31), (3, -2 ** 32)]:
+        ctx.op_attention_paged(e(5, 2, 64), cache(), e(2, dtype=I32), e(5, 128), new, frame=frame)
+    assert seen == [(5, 2 ** 31 - 1), (-1, 2 ** 31 - 1), (3, -1)]
+
+
+@pytest.mark.parametrize("cname,struct", [("wdc_paged_cache", "PagedCacheC"), ("wdc_head_norm", "HeadNorm")])
+def test_struct_layout_matches_a_c_compiler(tmp_path, cname, struct):
+    import ctypes
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("gcc") is None:
+        pytest.skip("no C compiler")
+    s = getattr(wdc, struct)
+    names = [n for n, _ in s._fields_]
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src, exe = tmp_path / "s.c", tmp_path / "s"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "wdc.h"\nint main(void) {'
+                   + "".join(f'printf("%zu ", offsetof({cname}, {n}));' for n in names)
+                   + f'printf("%zu", sizeof({cname})); return 0; }}')
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [getattr(s, n).offset for n in names] + [ctypes.sizeof(s)]
+
+
 def test_null_context_is_refused():
     n, c = wdc.HeadNorm(), wdc.PagedCacheC()
     import ctypes
