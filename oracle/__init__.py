@@ -28,6 +28,8 @@ Modules (each function cites the passage it follows):
                    Fig. 3a.
 * ``batch``     -- batched and guided rollouts (serving extensions: a batch of
                    independent trajectories; classifier-free guidance).
+* ``chunk``     -- the chunk operators: e4m3 blocks and their product, head
+                   norms with rotation, attention over a paged cache.
 
 Parity status: the controller constants and the lift's normalisation details
 are not printed in the paper (it defers them to supplementary material that is
