@@ -81,7 +81,7 @@ struct PagedArgs {
     float2* part_ml;                   // [item][rows_unit] base, row sum
     int rows_unit;                     // rows of a unit (host's bound)
     unsigned* counter;                 // one tile: [item] parts of a split unit that are done; 0 between launches
-    int4* record;                      // two tiles: [item] sequence, head, query block and parts of a split unit at its first part's
+    int4* record;                      // two tiles: [item] sequence, head, query block; parts of the unit (high half) and which it is
     unsigned* err;
 };
 
@@ -200,10 +200,10 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
         if (it.b >= g.sequences) return false;
         if (by_length) {               // the sequence of that rank instead, ties in order
             int rank[kPlanned] = {};
-#pragma unroll 4
-            for (int o = 0; o < 32; ++o)
 #pragma unroll
-                for (int k = 0; k < kPlanned; ++k) {
+            for (int k = 0; k < kPlanned; ++k)
+#pragma unroll 4
+                for (int o = 0; o < min(32, g.sequences - 32 * k); ++o) {
                     const float other = __shfl_sync(kAll, steps[k], o);
 #pragma unroll
                     for (int i = 0; i < kPlanned; ++i)
@@ -295,20 +295,25 @@ __device__ __forceinline__ void merge_parts(const PagedArgs& g, const Item& un, 
     }
 }
 
-// Two tiles: the merging of a split unit's rows is work for more than one CTA.
+// Two tiles: the merging of a split unit's rows is work for more than one CTA, so
+// kMergeCtas for each of its parts.  (300 rows of 8 heads on one over 6000 31.5 -> 26.7
+// us against sixteen for each part's place, of which a unit's first did the work; one or
+// two for each part are slower where there are few parts, eight where there are many.)
+constexpr int kMergeCtas = 4;
 template <int D>
 __global__ void __launch_bounds__(256) paged_merge_kernel(const __grid_constant__ PagedArgs g) {
     chain_release();
     chain_wait();
     const int4 rec = g.record[blockIdx.x];
-    if (rec.w < 2) return;
+    const int parts = rec.w >> 16, part = rec.w & 0xffff;
+    if (parts < 2) return;
     Item un;
     static_cast<PagedSeq&>(un) = sequence(g, rec.x);
     un.h = rec.y;
     un.qb = rec.z;
-    un.parts = rec.w;
-    un.slot = blockIdx.x;
-    merge_parts<D, 2>(g, un, blockIdx.y * 8 + (threadIdx.x >> 5), gridDim.y * 8, threadIdx.x & 31);
+    un.parts = parts;
+    un.slot = blockIdx.x - part;
+    merge_parts<D, 2>(g, un, (part * kMergeCtas + blockIdx.y) * 8 + (threadIdx.x >> 5), parts * kMergeCtas * 8, threadIdx.x & 31);
 }
 
 template <int D, int NT>
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
             s_item = it;
             s_has = has;
             if (NT == 2 && (int)blockIdx.x < g.items)
-                g.record[blockIdx.x] = make_int4(it.b, it.h, it.qb, has && it.part == 0 ? it.parts : 0);
+                g.record[blockIdx.x] = make_int4(it.b, it.h, it.qb, has ? it.parts << 16 | it.part : 0);
         }
     }
     __syncthreads();
@@ -843,7 +848,7 @@ wdc_status launch(Ctx* c, const void* q, const wdc_paged_cache* p, PagedArgs g, 
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention launch: ") + cudaGetErrorString(e));
     if (NT == 2 && g.items > 0) {
         LaunchScope ls(c, WDC_K_OTHER, s);
-        launch_kernel(paged_merge_kernel<D>, dim3((unsigned)g.items, 16), 256, 0, s, 1, g);
+        launch_kernel(paged_merge_kernel<D>, dim3((unsigned)g.items, kMergeCtas), 256, 0, s, 1, g);
         e = cudaGetLastError();
         if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("paged attention merge launch: ") + cudaGetErrorString(e));
     }

@@ -177,7 +177,7 @@ struct Ctx {
     float* attn_ml = nullptr;
     int attn_part_samples = 0, attn_part_rounds = 0;
     unsigned* attn_counters = nullptr; // a paged attention's units: parts done, 0 between launches
-    void* attn_records = nullptr;      // and, of two tiles, which of its parts are a split unit's first
+    void* attn_records = nullptr;      // and, of two tiles, the unit that each part is of
 
     // graph rollout (device-side control flow), built on first use
     GraphRollout* grollout = nullptr;
