@@ -99,10 +99,14 @@ __device__ __forceinline__ PagedSeq sequence(const PagedArgs& g, int b) {
 // lengths, each is split into parts of `chunk` steps: the fewest for which all
 // parts run in k rounds of the SMs, with the k = 1 .. kRounds of the least
 // estimated time, if that is less than the whole units'.  Estimates are in steps:
-// kStart a part for its start and end, kMerge for merging parts.  One tile is bound
-// by memory, whose bandwidth few CTAs fill too (0.55: one step's time of a lone
-// CTA); of two tiles, units of like length take whole rounds, others fill the gaps
-// that the longest leave.  The lengths are the device's, so the first warp of each CTA works the plan out, two
+// kStart a unit for its start and end, kPart a part (whose sums go out in fp32), kMerge
+// for merging.  One tile is bound by memory, whose bandwidth few CTAs fill too (0.55:
+// one step's time of a lone CTA); of two tiles, units of like length take whole rounds,
+// others fill the gaps that the longest leave, up to a share of the last.  Both sides
+// (us, whole, split): 300 tokens onto 3000, 32 heads of 128, 46 and 38; 1024 onto 2048,
+// 16 of 64, 35 and 30; four sequences of up to 900 onto 3000, 16 of 128, 54 and 64;
+// 4096 onto none, 8 of 128, 56 and 59.
+// The lengths are the device's, so the first warp of each CTA works the plan out, two
 // sequences a lane, in whole numbers as floats (exact below 2^24).  (A kernel of
 // its own for the plan and one for the merging cost 10 of 48 us at one token of 32
 // heads over 32000.)
@@ -110,7 +114,10 @@ constexpr int kRounds = 3;
 constexpr int kPlanned = 2;            // sequences a lane; more than 32 of these are not split
 
 // What a CTA does: part `part` of `parts` of a unit.  The blocks with the most keys
-// come first within a head.
+// come first in a sequence.  Where its blocks differ, over all heads, so that what
+// begins last is short (head by head: causal over 3000 tokens of 16 heads of 128 58 us,
+// 42 so; over 13568 of 24 746 and 705); where they do not, head by head, so that a
+// head's keys stay in L2 (17776 tokens of 48 heads of 64 onto themselves 3235 us, over all heads 3416).
 struct Item : PagedSeq {
     int b, h, qb, part, parts, chunk;
     int j0, nj;                        // its steps
@@ -120,7 +127,7 @@ struct Item : PagedSeq {
 template <int D, int NT>
 __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
     constexpr int BK = PagedCfg<D, NT>::BK, kMin = PagedCfg<D, NT>::MIN_STEPS;
-    constexpr float kStart = NT == 2 ? 8.f : 6.f, kMerge = NT == 2 ? 12.f : 8.f;
+    constexpr float kStart = NT == 2 ? 8.f : 6.f, kPart = NT == 2 ? 11.f : 6.f, kMerge = NT == 1 ? 8.f : D == 64 ? 6.f : 10.f;
     constexpr unsigned kAll = 0xffffffffu;
     const int block = NT * g.tpt;
     float with = 0.f;                  // steps a part; 0: whole units
@@ -160,12 +167,12 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
         by_length = g.by_length && most - least > 64.f;
         const float wave = (float)g.wave;
         const bool alike = 4.f * least >= 3.f * most;
-        auto estimate = [&](float c, float parts) {
+        auto estimate = [&](float c, float parts, float start, float late) {
             const float rounds = ceilf(parts / wave);
-            if (NT == 1) return fmaxf(work / wave, 0.55f * c) + rounds * kStart;
-            return alike ? rounds * (c + kStart) : fmaxf(c, work / wave + 0.5f * c) + rounds * kStart;
+            if (NT == 1) return fmaxf(work / wave, 0.55f * c) + rounds * start;
+            return (alike ? rounds * c : fmaxf(c, work / wave + late * c)) + rounds * start;
         };
-        float best = g.items > 0 ? estimate(most, n) - kMerge : 0.f;
+        float best = g.items > 0 ? estimate(most, n, kStart, 0.3f) - kMerge : 0.f;
 #pragma unroll 1
         for (int k = 1; k <= kRounds && g.items > 0 && most > (float)kMin; ++k) {
             const float items = (float)min(k * g.wave, g.items);
@@ -190,7 +197,7 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
                     else lo = c + 1.f;
                 } while (true);
             }
-            const float est = estimate(c, parts);
+            const float est = estimate(c, parts, kPart, 0.6f);
             if (c < most && parts <= items && est < best) {
                 best = est;
                 with = c;
@@ -199,8 +206,6 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
     }
     if (with == 0.f) {                 // whole units in order, some of them empty
         const int r = index / g.q_blocks;
-        it.qb = g.q_blocks - 1 - index % g.q_blocks;
-        it.h = r % g.kv;
         it.b = r / g.kv;
         if (it.b >= g.sequences) return false;
         if (by_length) {               // the sequence of that rank instead, ties in order
@@ -221,6 +226,10 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
             }
         }
         static_cast<PagedSeq&>(it) = sequence(g, it.b);
+        const bool even = 4ll * paged_limit(it, g.frame, min(it.n, block) - 1) >= 3ll * paged_limit(it, g.frame, it.n - 1);
+        const int unit = index % (g.kv * g.q_blocks);
+        it.h = even ? unit / g.q_blocks : unit % g.kv;
+        it.qb = g.q_blocks - 1 - (even ? unit % g.q_blocks : unit / g.kv);
         it.part = it.slot = 0;
         it.parts = 1;
         it.chunk = INT_MAX;
@@ -245,8 +254,8 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
             static_cast<PagedSeq&>(it) = sequence(g, it.b);
             const int nq = (min(it.n, g.max_new) + block - 1) / block, unit = r / it.parts;
             it.part = r - unit * it.parts;
-            it.h = unit / nq;
-            it.qb = nq - 1 - (unit - it.h * nq);
+            it.h = unit % g.kv;
+            it.qb = max(0, nq - 1 - unit / g.kv);
             it.chunk = (int)with;
             it.slot = index - it.part;
             return true;
