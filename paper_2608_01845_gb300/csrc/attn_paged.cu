@@ -60,7 +60,7 @@ struct PagedCfg {
     static constexpr uint32_t SMEM = NT * Q_TILE + STAGES * STAGE + 1024 + 256;
     static constexpr uint32_t TMEM_COLS = NT == 2 ? 512 : 256;
     static constexpr int CTAS = 3 - NT;                        // an SM
-    static constexpr int MIN_STEPS = 8;                        // of a part of a split unit
+    static constexpr int MIN_STEPS = NT == 1 ? 6 : 8;          // of a part of a split unit
     // two tiles: registers a thread, 168 at launch (65536 / 384, a multiple of 8),
     // of which the control warpgroup hands most to the softmax warpgroups
     static constexpr uint32_t REGS_CONTROL = D == 64 ? 40 : 88;
@@ -99,8 +99,8 @@ __device__ __forceinline__ PagedSeq sequence(const PagedArgs& g, int b) {
 // lengths, each is split into parts of `chunk` steps: the fewest for which all
 // parts run in k rounds of the SMs, with the k = 1 .. kRounds of the least
 // estimated time, if that is less than the whole units'.  Estimates are in steps:
-// kStart a unit for its start and end, kPart a part (whose sums go out in fp32), kMerge
-// for merging.  One tile is bound by memory, whose bandwidth few CTAs fill too (0.55:
+// kStart a unit for its start and end, kPart a part (whose sums go out in fp32), and
+// what merging takes.  One tile is bound by memory, whose bandwidth few CTAs fill too (0.55:
 // one step's time of a lone CTA); of two tiles, units of like length take whole rounds,
 // others fill the gaps that the longest leave, up to a share of the last.  Both sides
 // (us, whole, split): 300 tokens onto 3000, 32 heads of 128, 46 and 38; 1024 onto 2048,
@@ -127,7 +127,10 @@ struct Item : PagedSeq {
 template <int D, int NT>
 __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
     constexpr int BK = PagedCfg<D, NT>::BK, kMin = PagedCfg<D, NT>::MIN_STEPS;
-    constexpr float kStart = NT == 2 ? 8.f : 6.f, kPart = NT == 2 ? 11.f : 6.f, kMerge = NT == 1 ? 8.f : D == 64 ? 6.f : 10.f;
+    constexpr float kStart = NT == 2 ? 8.f : 6.f, kPart = NT == 2 ? 11.f : 6.f;
+    // merging: one tile's by four warps, eight parts of a row of D / 4 lanes at a time
+    const float turns = ceilf((float)(g.rows_unit * D) / 512.f);
+    auto merging = [&](float parts) { return NT == 2 ? (D == 64 ? 6.f : 10.f) : 2.f + turns * ceilf(parts / 8.f); };
     constexpr unsigned kAll = 0xffffffffu;
     const int block = NT * g.tpt;
     float with = 0.f;                  // steps a part; 0: whole units
@@ -172,11 +175,12 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
             if (NT == 1) return fmaxf(work / wave, 0.55f * c) + rounds * start;
             return (alike ? rounds * c : fmaxf(c, work / wave + late * c)) + rounds * start;
         };
-        float best = g.items > 0 ? estimate(most, n, kStart, 0.3f) - kMerge : 0.f;
+        float best = g.items > 0 ? estimate(most, n, kStart, 0.3f) : 0.f;
 #pragma unroll 1
         for (int k = 1; k <= kRounds && g.items > 0 && most > (float)kMin; ++k) {
             const float items = (float)min(k * g.wave, g.items);
-            if (n >= items) continue;
+            // (with the places all full, and no part short: no less than that)
+            if (n >= items || estimate(bound / items, items, kPart, 0.6f) + merging(2.f) >= best) continue;
             float c, parts;
             if (g.sequences == 1) {    // as many parts a unit as there are places
                 c = fmaxf((float)kMin, ceilf(most / floorf(items / n)));
@@ -197,10 +201,19 @@ __device__ bool find_item(const PagedArgs& g, int index, int lane, Item& it) {
                     else lo = c + 1.f;
                 } while (true);
             }
-            const float est = estimate(c, parts, kPart, 0.6f);
-            if (c < most && parts <= items && est < best) {
-                best = est;
-                with = c;
+            auto offer = [&](float c, float parts) {
+                const float est = estimate(c, parts, kPart, 0.6f) + merging(ceilf(most / c));
+                if (c < most && est < best) {
+                    best = est;
+                    with = c;
+                }
+            };
+            if (parts <= items) {
+                offer(c, parts);
+                // fewer parts, as many as merge at a time (60 tokens onto 3000, 24 heads
+                // of 128: 45 us, 27 so, 59 whole)
+                const float eighth = ceilf(most / 8.f);
+                if (NT == 1 && eighth > c) offer(eighth, fminf(parts, ceilf(bound / eighth) + n));
             }
         }
     }
@@ -290,17 +303,26 @@ __device__ __forceinline__ void merge_parts(const PagedArgs& g, const Item& un, 
                 ml[k] = __ldcg(g.part_ml + row);
                 v[k] = __ldcg(reinterpret_cast<const float4*>(g.part_o + row * D + col));
             }
+            float top = m;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                if (p + k >= un.parts || ml[k].x == -INFINITY) continue;     // (saw nothing)
-                const float top = fmaxf(m, ml[k].x), a = ex2(m - top), b = ex2(ml[k].x - top);
-                l = l * a + ml[k].y * b;
-                acc.x = acc.x * a + v[k].x * b;
-                acc.y = acc.y * a + v[k].y * b;
-                acc.z = acc.z * a + v[k].z * b;
-                acc.w = acc.w * a + v[k].w * b;
-                m = top;
+                if (p + k >= un.parts) ml[k].x = -INFINITY;
+                top = fmaxf(top, ml[k].x);
             }
+            const float a = m == -INFINITY ? 0.f : ex2(m - top);
+            l *= a;
+            acc.x *= a; acc.y *= a; acc.z *= a; acc.w *= a;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (ml[k].x == -INFINITY) continue;          // (saw nothing)
+                const float b = ex2(ml[k].x - top);
+                l = fmaf(ml[k].y, b, l);
+                acc.x = fmaf(v[k].x, b, acc.x);
+                acc.y = fmaf(v[k].y, b, acc.y);
+                acc.z = fmaf(v[k].z, b, acc.z);
+                acc.w = fmaf(v[k].w, b, acc.w);
+            }
+            m = top;
         }
         const float inv = l != 0.f ? 1.0f / l : 0.f;
         const size_t t = (size_t)un.row0 + tok0 + r / g.G;
