@@ -23,10 +23,10 @@
 //  * Each row has a limit of its own.  A row that has seen nothing yet takes the
 //    next tile's maximum as its exponent base, as at the first step.
 //  * Row sums add the fp16 probabilities in fp32 (mixed-precision adds).
-// Measured: one token of 32 heads on 8 of 128 in 16 sequences of 16000 keys 5.8 TB/s,
-// 0.86 of a copy (one tile: bound by memory, what is missing are the parts' starts and
-// ends); 24 heads of 128, 13568 tokens onto themselves 1640 TFLOP/s, 48 of 64, 17776
-// 1200 (two tiles: bound by the chain S -> softmax -> P -> PV, whose S and P have one
+// Measured: one token of 32 heads on 8 of 128 in 16 sequences of 16000 keys 5.9 TB/s,
+// 0.87 of a copy (one tile: bound by memory, what is missing are the parts' starts and
+// ends); 24 heads of 128, 13568 tokens onto themselves 1720 TFLOP/s, 48 of 64, 17776
+// 1220 (two tiles: bound by the chain S -> softmax -> P -> PV, whose S and P have one
 // buffer a tile, 0.77 us a step of 64 keys of 128 or 1.0 of 128 keys of 64).
 // Where there are few units, each is split over its keys into parts of equal
 // numbers of steps (find_item), which the last of them to be done (one tile) or a second kernel

@@ -392,6 +392,26 @@ def test_attention_long_and_split(contexts):
         assert (np.abs(host(o).reshape(want.shape) - want) <= attention_bound(want, mag, max(lens))).all()
 
 
+@pytest.mark.parametrize("d,H,kv,new,past,frame", [(128, 2, 2, [60], [3000], 1), (64, 4, 1, [30, 7, 0], [2500, 40, 9], 16),     # one tile
+                                                   (128, 24, 1, [5], [4000], 1), (64, 8, 4, [1, 16], [1900, 2100], 0),
+                                                   (128, 3, 1, [200], [2600], 1), (64, 2, 2, [400, 90, 300], [1500, 700, 0], 50),
+                                                   (128, 2, 2, [700], [0], 1), (64, 3, 3, [515, 257], [0, 300], 0)])
+def test_attention_chunks_split_and_in_order(contexts, d, H, kv, new, past, frame):
+    """Chunks whose keys are split, rows of one tile and of several blocks, some of them short; the longest
+    blocks first, or head by head; equal calls give equal bits."""
+    ctx = contexts["bf16"]
+    lens = [n + p for n, p in zip(new, past)]
+    P = Paged(95, lens, 32, kv, d)
+    q = synth.bf16_round(synth.normal(96, (sum(new), H, d), 1.5))
+    o = attend(ctx, q, P, new, frame, extra=3)
+    again = attend(ctx, q, P, new, frame, extra=3)
+    assert ctx.device_errors() == 0
+    assert torch.equal(o.view(torch.int16), again.view(torch.int16))
+    want, mag = chunk.attention_paged(q, P.k, P.v, P.table, lens, starts(new), frame)
+    assert (np.abs(host(o[:-3]).reshape(want.shape) - want) <= attention_bound(want, mag, max(lens))).all()
+    assert bool((o[-3:] == 5.0).all())
+
+
 @pytest.mark.parametrize("lens,kv,d", [([2500] + [1 + 61 * i % 2400 for i in range(39)], 8, 128),     # longest first
                                        ([1 + 7 * i % 130 for i in range(70)], 2, 64),                 # too many to plan for
                                        ([3] * 32 + [4000] + [5, 0, 6], 1, 64),                        # one to split, past lane 31
