@@ -20,8 +20,9 @@
 //    there are masked; a probability of 0 times an infinity or NaN of V would not
 //    be 0, so the producer zeroes those rows of the last step's V in shared
 //    memory before that step's PV products.
-//  * Each row has a limit of its own.  A row that has seen nothing yet takes the
-//    next tile's maximum as its exponent base, as at the first step.
+//  * Each row has a limit of its own.  A row that has seen nothing yet (masked, or
+//    scores of -infinity) takes the next tile's maximum as its exponent base, as at
+//    the first step, and nothing over from before it.
 //  * Row sums add the fp16 probabilities in fp32 (mixed-precision adds).
 // Measured: one token of 32 heads on 8 of 128 in 16 sequences of 16000 keys 5.9 TB/s,
 // 0.87 of a copy (one tile: bound by memory, what is missing are the parts' starts and
@@ -709,7 +710,9 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                 if (redo) base = fmaxf(base, tile_max() * g.scale_log2);
             }
             const bool moved = __any_sync(0xffffffffu, base != m_run);
-            const float corr = ex2(m_run - base);            // 1 when the base stays; 0 before the first tile
+            // 1 when the base stays; 0 before a row has seen something, when the base it
+            // leaves means nothing (and may lie above the new one by more than ex2 holds)
+            const float corr = l_run == 0.f ? 0.f : ex2(m_run - base);
             l_run = l_run * corr + sum;
             m_run = base;
             // PV(t, j-1) must be done before P(t) is overwritten and O(t) rescaled

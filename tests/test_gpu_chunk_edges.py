@@ -1,0 +1,47 @@
+"""The chunk operators where their numbers come to an edge: scores of -infinity
+before finite ones far below 0, sums far outside a GELU's range, tiles without
+rows among tiles with some, starts and lengths that no caller should give, sizes
+next to the C ABI's largest."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import chunk
+from paper_2608_01845_gb300 import synth, wdc
+from test_gpu_chunk import Paged, attend, attention_bound, contexts, dev, host, starts  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# (one tile, whole and split; two tiles, whole and split; a group; several sequences)
+@pytest.mark.parametrize("H,kv,new,past,frame", [(2, 2, [40], [260], 1), (4, 1, [1], [3100], 1), (2, 1, [300], [0], 1),
+                                                 (3, 3, [300], [2900], 0), (6, 2, [1, 20, 5], [900, 2000, 0], 7),
+                                                 (1, 1, [260, 140], [1100, 800], 50)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_finite_scores_far_below_0_after_minus_infinity(contexts, d, H, kv, new, past, frame):
+    """Scores of -infinity, however many steps of them, and then one near -160: the finite ones
+    alone have weight.  (Taken over from a base of 0, the first sum would be 0 * 2^231.)
+
+    The bound: a score is a sum of d products of which one is 160 sqrt(d), so each addition is off
+    by at most 2^-23 of that, and the score by d 160 2^-23 < 2^-8 after its division by sqrt(d);
+    a probability by as much, relatively, beside what attention_bound counts."""
+    ctx = contexts["bf16"]
+    lens = [n + p for n, p in zip(new, past)]
+    P = Paged(101, lens, 32, kv, d)
+    for b, n in enumerate(lens):
+        i = np.arange(n)
+        at = P.table[b, i // 32], slice(None), i % 32
+        k = P.k[at]
+        k[:, :, 0] = np.where(i % 197 == 150, 0, -np.inf)[:, None]
+        k[:, :, 1] = synth.bf16_round(np.float32(-10.0 * np.sqrt(d)))
+        P.k[at] = k
+    P.dk.copy_(dev(P.k, torch.bfloat16))
+    q = synth.bf16_round(synth.normal(102, (sum(new), H, d)))
+    q[:, :, 0], q[:, :, 1] = 1.0, 16.0
+    o = attend(ctx, q, P, new, frame)
+    assert ctx.device_errors() == 0
+    want, mag = chunk.attention_paged(q, P.k, P.v, P.table, lens, starts(new), frame)
+    assert np.isfinite(want).all()
+    got = host(o).reshape(want.shape)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= attention_bound(want, mag, max(lens)) + 2.0 ** -8 * (mag + np.abs(want))).all()
