@@ -781,6 +781,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                 const size_t prow = (size_t)(un.slot + un.part) * g.rows_unit + t * g.tpt * g.G + row;
                 const size_t at = split ? prow * D : ((size_t)(un.row0 + i) * g.heads + un.h * g.G + row % g.G) * D;
                 if (split && valid) g.part_ml[prow] = make_float2(seen ? m_run : -INFINITY, l_run);
+                __syncwarp();
                 auto put = [&](int piece, uint4 w) {
                     *reinterpret_cast<uint4*>(stage + lane * (D * 2) + ((piece ^ (lane & 7)) << 4)) = seen ? w : make_uint4(0, 0, 0, 0);
                 };
@@ -832,6 +833,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
+                    __syncwarp();                            // (lanes with a row come from its stores)
                     if (mine > 0) {
                         tmem_ld32(o_addr + c, o);
                         tmem_ld_wait();
@@ -872,6 +874,7 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                 __threadfence();
                 s_last = last;
             }
+            __syncwarp();
             softmax_barrier<NT * 128>();
             if (s_last) merge_parts<D, NT>(g, un, warp - 4, NT * 4, lane);
         }

@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(kThreads, 2)
             }
             const float4* s4 = reinterpret_cast<const float4*>(window + ((w & 1) * C::WINDOW + at) * BN);
             ok = ok && mbar_wait_warp(&tfull[buf], bphase, abort_flag, g.err);
+            __syncwarp();                                  // (after a wait that gave up nothing else does)
             tc_fence_after();
             constexpr int CH = BN < 32 ? BN : 32, COLS = C::KB * BN;        // columns a load; of the buffer
 #pragma unroll
