@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             const bool rows = m0 < g.M;
             if (RESID && rows && n0 < end) request(n0, m0);
             // bias and gate of the tile's columns, on their way to shared memory meanwhile
-            if (4 * lane < COLS && n0 + 4 * lane < g.N) {
+            // (not where no row waits for them: the next tile's would be under way too)
+            if (rows && 4 * lane < COLS && n0 + 4 * lane < g.N) {
                 if (g.bias) cp_async16(bias + 4 * lane, g.bias + n0 + 4 * lane);
                 if (RESID && g.gate) cp_async16(gate + 4 * lane, g.gate + n0 + 4 * lane);
             }

@@ -46,3 +46,17 @@ def test_lanes_are_together_at_tensor_memory(name):
 @pytest.mark.parametrize("name", KERNELS)
 def test_a_wait_that_gives_up_leaves_no_lane_behind(name):
     leaves_no_lane_behind(name)
+
+
+def test_copies_are_awaited_before_the_next_into_the_same_place():
+    """Two cp.async into one place are not ordered.  In the pair kernel a tile's bias and gate are fetched
+    only by warps that await them: those that do not leave the tile early."""
+    code = _code("gemm_fp8_pair.cu")
+    tile = next(code[a:b] for a, b in _blocks(code, r"for \(int tile = pair; tile < tiles && ok; tile \+= pairs\) \{")
+                if "cp_async16(" in code[a:b])
+    first, wait = tile.index("cp_async16("), tile.index("cp_async_wait()")
+    assert first < wait and tile.count("cp_async_wait()") == 1
+    leaves = re.findall(r"if \((\S+)\) (?:continue|break);", tile[first:wait])
+    assert leaves == ["!ok", "!rows"]                          # (!ok ends the loop)
+    head = tile[:first].rindex("if (rows && ")                 # the copies' own condition
+    assert tile[head:first].count("{") - tile[head:first].count("}") == 1

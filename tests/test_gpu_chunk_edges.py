@@ -8,7 +8,8 @@ import torch
 
 from oracle import chunk
 from paper_2608_01845_gb300 import synth, wdc
-from test_gpu_chunk import Paged, attend, attention_bound, contexts, dev, host, starts  # noqa: F401
+from test_gpu_chunk import (DTYPES, HALF, Paged, attend, attention_bound, contexts, dev, gemm_bound, gemm_case,  # noqa: F401
+                            host, run_gemm, starts)
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,23 @@ def test_finite_scores_far_below_0_after_minus_infinity(contexts, d, H, kv, new,
     got = host(o).reshape(want.shape)
     assert np.isfinite(got).all()
     assert (np.abs(got - want) <= attention_bound(want, mag, max(lens)) + 2.0 ** -8 * (mag + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("resid", [False, True])
+def test_warps_without_rows_among_tiles_with_some(contexts, resid, kind):
+    """One block of K, several tiles a pair, and in the last row block most warps without a row: each tile
+    gets its own columns' bias and gate."""
+    ctx, (M, N, K) = contexts[kind], (4 * 256 + 5, 8200, 128)
+    A, sa, W, sw = gemm_case(51, M, N, K, kind)
+    n = np.arange(N, dtype=np.float32)
+    b, g = 1000 + n, 2.0 - n / 4096                                # (a neighbour's would be far off)
+    y = chunk.dequantize(A, sa, 1) @ chunk.dequantize(W, sw, 128).T + b
+    err = gemm_bound(A, sa, W, sw, 0 * y, kind) + 2.0 ** -22 * np.abs(y)
+    C, kw = torch.zeros(M, N, dtype=DTYPES[kind], device="cuda"), dict(bias=dev(b))
+    if resid:
+        kw.update(res=C, gate=dev(g))
+        y, err = g * y, np.abs(g) * err + 2.0 ** -22 * np.abs(g * y)
+    run_gemm(ctx, A, sa, W, sw, C, **kw)
+    assert ctx.device_errors() == 0
+    assert (np.abs(host(C) - y) <= err + HALF[kind] * np.abs(y) + 2.0 ** -22 * np.abs(y)).all()
