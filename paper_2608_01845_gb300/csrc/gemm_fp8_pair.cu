@@ -65,8 +65,8 @@ __device__ __forceinline__ float2 unpack64(uint64_t v) {
 
 // gelu_tanh_f of two values with one reciprocal for both: 1 / a = b / (a b).  The
 // epilogue's exponentials and reciprocals (16 a clock) are what a GELU costs.  The
-// exponent is cut off at 60, where the result is below 2^-60 |x|, so that a b is
-// finite.
+// exponent is cut off at 60, so that a b is finite; beyond it (x < -7) the result,
+// below 2^-60 |x|, is 0, as gelu_tanh_f's is from 2^-126 on.
 __device__ __forceinline__ void gelu_pair(float& x, float& y) {
     const float k0 = 0.7978845608028654f, k1 = 0.044715f, m2log2e = -2.0f * 1.4426950408889634f;
     const float u = k0 * m2log2e * fmaf(k1 * x * x, x, x), v = k0 * m2log2e * fmaf(k1 * y * y, y, y);
@@ -76,8 +76,8 @@ __device__ __forceinline__ void gelu_pair(float& x, float& y) {
     a += 1.0f;
     b += 1.0f;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
-    x *= r * b;
-    y *= r * a;
+    x *= u > 60.f ? 0.f : r * b;
+    y *= v > 60.f ? 0.f : r * a;
 }
 
 // A 16-byte piece of a slab's row.

@@ -66,3 +66,21 @@ def test_warps_without_rows_among_tiles_with_some(contexts, resid, kind):
     run_gemm(ctx, A, sa, W, sw, C, **kw)
     assert ctx.device_errors() == 0
     assert (np.abs(host(C) - y) <= err + HALF[kind] * np.abs(y) + 2.0 ** -22 * np.abs(y)).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("resid", [False, True])
+@pytest.mark.parametrize("M,N", [(12, 264), (1029, 8200)])             # narrow kernel, pair kernel
+def test_gelu_far_from_0(contexts, M, N, resid, kind):
+    """GELU(x) is x, or 0, from 8 on: below -8 it is smaller than 8 * 2^-60 (tanh form: 2^-70 x), above 8
+    nearer to x than 2^-18.  Sums up to 1e20 in size, whichever kernel the number of rows brings."""
+    sizes = np.float32([8, 30, 1e3, 1e6, 1e10, 1e20])
+    x = sizes[np.arange(M) % len(sizes)]
+    A, W = np.ones((M, 128)), np.ones((N, 128)) * np.where(np.arange(N) % 3 == 0, 1, -1)[:, None]
+    C, kw = torch.zeros(M, N, dtype=DTYPES[kind], device="cuda"), {}
+    if resid:
+        kw["res"] = C
+    run_gemm(contexts[kind], A, (x / 128)[None], W, np.ones((-(-N // 128), 1)), C, gelu=True, **kw)
+    got, up = host(C), np.arange(N) % 3 == 0
+    assert (np.abs(got[:, ~up]) <= 2.0 ** -57).all()
+    assert (np.abs(got[:, up] - x[:, None]) <= (2.0 ** -18 + HALF[kind]) * x[:, None]).all()
