@@ -252,6 +252,7 @@ enum wdc_gemm_form {
 wdc_status wdc_gemm_launches(const wdc_ctx* ctx, unsigned long long* counts);
 /* Synchronises the device and returns (then clears) the bits the kernels have
  * set in the context's error word: 1 = a bounded device-side wait timed out,
+ * 2 = a chunk operator met a page number, length, start or position out of range,
  * 4 = the two CTAs of a tensor-core pair saw different tensor-memory bases,
  * 8 = a bf16 model's QKV projection produced a value of V beyond fp16's range
  * (|v| > 65504), which was saturated to +-65504 when V^T was stored for the
@@ -500,8 +501,9 @@ wdc_status wdc_op_attention(wdc_ctx* ctx, const void* q, const void* k, const vo
  * aligned unless said) and may be captured into a graph.  A call with no rows
  * (M, T, max_new or the number of sequences 0) returns WDC_OK and launches nothing.  What
  * only the device knows (page numbers, lengths, starts, positions) cannot be
- * refused: a value out of range sets bit 2 (wdc_device_errors), and nothing is
- * read or written outside the arrays given here. */
+ * refused: a value out of range sets bit 2 (wdc_device_errors), in a sequence
+ * without new tokens too (a page number where a token or key of the call lies in the
+ * page), and nothing is read or written outside the arrays given here. */
 
 /* q = e4m3(x / s) with a scale for each block of 128 columns of one row
  * (block_rows 1) or of 128 rows (block_rows 128): s = max |x| / 448 over the

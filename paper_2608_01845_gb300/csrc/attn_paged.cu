@@ -434,6 +434,11 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
             if (NT == 2 && (int)blockIdx.x < g.items)
                 g.record[blockIdx.x] = make_int4(it.b, it.h, it.qb, has ? it.parts << 16 | it.part : 0);
         }
+    } else if (warp == 3 && lane == 0 && blockIdx.x < (unsigned)g.sequences) {
+        // a sequence's numbers, whether it has new tokens or not (there are as many CTAs, or more)
+        const int b = blockIdx.x;
+        if (!paged_given(g.start[b], g.start[b + 1], g.length[b], g.T, g.width << g.page_log2, g.max_new))
+            atomicOr(g.err, kErrBounds);
     }
     __syncthreads();
     if (!s_has) {
@@ -544,10 +549,6 @@ __global__ void __launch_bounds__(PagedCfg<D, NT>::THREADS, PagedCfg<D, NT>::CTA
                     while (!mbar_try_wait(&kv_full[s], (parity >> s) & 1) && globaltimer() - t0 < kWaitLimitNs) {
                     }
                 }
-            }
-            if (!of_v && un.part == 0 && un.qb == 0 && un.h == 0 && lane == 0) {
-                const int given = g.length[un.b];
-                if (given != un.len || un.n > g.max_new || un.n > un.len) atomicOr(g.err, kErrBounds);
             }
         } else if (((NT == 1 && warp == 1) || (NT == 2 && warp - 1 < nt && warp <= 2)) && nj > 0) {
             constexpr uint32_t idesc_s = idesc_bf16(BQ, BKV);

@@ -25,6 +25,12 @@ WDC_INDEX PagedSeq paged_seq(int start, int end, int length, int T, int room) {
     s.len = index_clamp(length, 0, room);
     return s;
 }
+// Whether the numbers are as a caller should give them, `most` new tokens at most; if
+// not, paged_seq takes the nearest that are.
+WDC_INDEX bool paged_given(int start, int end, int length, int T, int room, int most) {
+    return start >= 0 && end >= start && end <= T && length >= 0 && length <= room && end - start <= length &&
+           end - start <= most;
+}
 // Place of the chunk's token i in its sequence; negative where the sequence is
 // shorter than its chunk.
 WDC_INDEX int paged_place(const PagedSeq& s, int i) { return s.len - s.n + i; }

@@ -194,17 +194,21 @@ __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant
     if constexpr (APPEND) {
         int b = 0;
         for (int i = 0; i < a.sequences; i += 32) {
-            const bool past = i + lane < a.sequences && a.start[i + lane + 1] <= t;
+            const bool mine = i + lane < a.sequences;
+            const int end = mine ? a.start[i + lane + 1] : 0;
+            const bool past = mine && end <= t;
+            // (the first warp: each sequence's numbers, whether it has new tokens or not)
+            if (w == 0 && mine && !paged_given(a.start[i + lane], end, a.length[i + lane], a.T, a.width << a.page_log2, a.T))
+                atomicOr(a.err, kErrBounds);
             b += __popc(__ballot_sync(0xffffffffu, past));
         }
         if (b >= a.sequences) return;
-        const int given = a.length[b];
-        const PagedSeq seq = paged_seq(a.start[b], a.start[b + 1], given, a.T, a.width << a.page_log2);
+        const PagedSeq seq = paged_seq(a.start[b], a.start[b + 1], a.length[b], a.T, a.width << a.page_log2);
         if (t < seq.row0 || t >= seq.row0 + seq.n) return;
         place = paged_place(seq, t - seq.row0);
         const int page = place < 0 ? -1 : paged_page(a.table[(size_t)b * a.width + (place >> a.page_log2)], a.pages);
         keep = page >= 0;
-        if ((!keep || given != seq.len) && lane == 0) atomicOr(a.err, kErrBounds);
+        if (!keep && lane == 0) atomicOr(a.err, kErrBounds);
         in_page = place & ((1 << a.page_log2) - 1);
         slot = keep ? (size_t)page * a.kv : 0;
     }

@@ -84,3 +84,45 @@ def test_gelu_far_from_0(contexts, M, N, resid, kind):
     got, up = host(C), np.arange(N) % 3 == 0
     assert (np.abs(got[:, ~up]) <= 2.0 ** -57).all()
     assert (np.abs(got[:, up] - x[:, None]) <= (2.0 ** -18 + HALF[kind]) * x[:, None]).all()
+
+
+@pytest.mark.parametrize("start,lens,ok", [([0, 2, 3], [40, 20], True), ([1, 1, 3], [40, 20], True), ([0, 0, 0], [0, 0], True),
+                                           ([-1, 2, 3], [40, 20], False), ([0, 2, 4], [40, 20], False), ([2, 1, 3], [40, 20], False),
+                                           ([0, 5, 3], [40, 20], False), ([2 ** 31 - 1] * 3, [40, 20], False),
+                                           ([0, 3, 2 ** 31 - 1], [40, 20], False), ([-2 ** 31, 0, 3], [40, 20], False),
+                                           ([0, 3, 3], [40, -1], False), ([0, 0, 3], [10 ** 6, 20], False), ([0, 0, 3], [40, 2], False)])
+def test_starts_and_lengths_out_of_range_are_reported(contexts, start, lens, ok):
+    """Those of a sequence without new tokens too; what lies behind the T rows stays as it is."""
+    ctx, T = contexts["bf16"], 3
+    P = Paged(103, [48, 48], 16, 2, 64, spare=0)
+    P.dlen.copy_(torch.tensor(lens, dtype=torch.int32))
+    s = torch.tensor(start, dtype=torch.int64).to(torch.int32).cuda()
+    q = dev(synth.normal(104, (T, 4, 64)), torch.bfloat16)
+    o = torch.full((T + 4, 4 * 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    ctx.op_attention_paged(q, P.cache, s, o[:T], T, frame=1)
+    assert ctx.device_errors() == (0 if ok else 2)
+    assert bool((o[T:] == 5.0).all())
+    x = dev(synth.normal(105, (T, 8 * 64)), torch.bfloat16)
+    out = torch.full((T + 4, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    ctx.op_qk_norm_rope_append(x, out[:T], P.cache, s)
+    assert ctx.device_errors() == (0 if ok else 2)
+    assert bool((out[T:] == 5.0).all())
+    spare = [p for p in range(P.pages) if p not in set(P.table.reshape(-1).tolist())]
+    assert torch.equal(P.dk[spare].view(torch.int16), dev(P.k, torch.bfloat16)[spare].view(torch.int16))
+
+
+def test_every_sequence_is_looked_at(contexts):
+    """One bad length among many sequences, most without new tokens, wherever it is."""
+    ctx, B = contexts["bf16"], 75
+    P = Paged(106, [16] * B, 16, 1, 64, spare=0)
+    q, x = dev(synth.normal(107, (1, 1, 64)), torch.bfloat16), dev(synth.normal(108, (1, 3 * 64)), torch.bfloat16)
+    o, s = torch.empty(1, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(B + 1, dtype=torch.int32, device="cuda")
+    s[0] = 0
+    for b in (None, 0, 1, 31, 32, 63, 64, 74):
+        P.dlen.fill_(16)
+        if b is not None:
+            P.dlen[b] = 17
+        ctx.op_attention_paged(q, P.cache, s, o, 1)
+        assert ctx.device_errors() == (0 if b is None else 2)
+        ctx.op_qk_norm_rope_append(x, q.clone(), P.cache, s)
+        assert ctx.device_errors() == (0 if b is None else 2)
