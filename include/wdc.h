@@ -515,7 +515,7 @@ wdc_status wdc_op_attention(wdc_ctx* ctx, const void* q, const void* k, const vo
  * for weights).  Division and rounding (to nearest even) are IEEE's; a block of
  * zeros has scale 0; an infinity makes its block's scale infinite (finite
  * values there become 0, infinities NaN), a NaN makes scale and block NaN.
- * K % 16 == 0, ldx % 8 == 0 (WDC_ERR_UNSUPPORTED otherwise). */
+ * K % 16 == 0, K <= 2^31 - 512 and ldx % 8 == 0 (WDC_ERR_UNSUPPORTED otherwise). */
 wdc_status wdc_op_quantize_fp8(wdc_ctx* ctx, const void* x, long long ldx, void* q, float* scale, int M, int K,
                                int block_rows, wdc_stream stream);
 
@@ -525,8 +525,8 @@ wdc_status wdc_op_quantize_fp8(wdc_ctx* ctx, const void* x, long long ldx, void*
  *   sum over blocks b of a_scale[b][m] w_scale[n/128][b] sum_{k in b} A[m,k] W[n,k].
  * A block's 128 products are summed by the tensor core, the scaled block sums
  * in fp32.  bias, gelu, res, gate and C as in wdc_op_gemm (C and res [M, N] in
- * the model dtype, res may equal C).  N % 8 == 0 and K % 16 == 0
- * (WDC_ERR_UNSUPPORTED otherwise). */
+ * the model dtype, res may equal C).  N % 8 == 0 and K % 16 == 0, both at most
+ * 2^31 - 512 (WDC_ERR_UNSUPPORTED otherwise). */
 wdc_status wdc_op_gemm_fp8(wdc_ctx* ctx, const void* A, const float* a_scale, const void* W, const float* w_scale,
                            const float* bias, void* C, int M, int N, int K, int gelu, const void* res,
                            const float* gate, wdc_stream stream);

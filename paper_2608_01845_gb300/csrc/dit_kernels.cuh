@@ -42,6 +42,10 @@ __device__ __forceinline__ float gelu_tanh_f(float x) {
     return __fdividef(x, 1.0f + e);
 }
 
+// The widest matrix of the e4m3 operators: rounded up to whole tiles (512 columns at
+// most) its width is still an int.
+constexpr int kMaxWidth8 = 0x7fffffff - 511;
+
 enum EpiMode { kEpiStore = 0, kEpiResid = 1, kEpiQKV = 2, kEpiUnpatch = 3 };
 
 // Token rows of a batch of nb samples (L tokens each, the first Lc of them

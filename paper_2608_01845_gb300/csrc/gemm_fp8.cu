@@ -412,6 +412,7 @@ wdc_status op_gemm_fp8(Ctx* c, const void* A, const float* a_scale, const void* 
                        const float* bias, void* C, int M, int N, int K, int gelu, const void* res, const float* gate,
                        cudaStream_t s) {
     if (M < 0 || N <= 0 || K <= 0) return fail(c, WDC_ERR_INVALID_ARG, "fp8 GEMM: M >= 0, N > 0 and K > 0 wanted");
+    if (N > kMaxWidth8 || K > kMaxWidth8) return fail(c, WDC_ERR_UNSUPPORTED, "fp8 GEMM: N or K above 2^31 - 512");
     if (N % 8 || K % 16) return fail(c, WDC_ERR_UNSUPPORTED, "fp8 GEMM needs N % 8 == 0 and K % 16 == 0");
     if (M == 0) return WDC_OK;
     if (!A || !a_scale || !W || !w_scale || !C) return fail(c, WDC_ERR_INVALID_ARG, "fp8 GEMM: null pointer");

@@ -187,6 +187,7 @@ wdc_status op_quantize_fp8(Ctx* c, const void* x, long long ldx, void* q, float*
     if (M < 0 || K <= 0) return fail(c, WDC_ERR_INVALID_ARG, "quantize: M >= 0 and K > 0 wanted");
     if (block_rows != 1 && block_rows != kBlock) return fail(c, WDC_ERR_INVALID_ARG, "quantize: block_rows must be 1 or 128");
     if (ldx < K) return fail(c, WDC_ERR_INVALID_ARG, "quantize: row stride below K");
+    if (K > kMaxWidth8) return fail(c, WDC_ERR_UNSUPPORTED, "quantize: more than 2^31 - 512 columns");
     if (K % 16 || ldx % 8) return fail(c, WDC_ERR_UNSUPPORTED, "quantize needs K % 16 == 0 and ldx % 8 == 0");
     if (M == 0) return WDC_OK;
     if (!x || !q || !scale) return fail(c, WDC_ERR_INVALID_ARG, "quantize: null pointer");

@@ -126,3 +126,17 @@ def test_every_sequence_is_looked_at(contexts):
         assert ctx.device_errors() == (0 if b is None else 2)
         ctx.op_qk_norm_rope_append(x, q.clone(), P.cache, s)
         assert ctx.device_errors() == (0 if b is None else 2)
+
+
+def test_widths_that_tiles_would_take_past_an_int(contexts):
+    """Refused before anything is launched: rounded up to whole blocks they are negative."""
+    ctx, f8 = contexts["bf16"], torch.float8_e4m3fn
+    x, q, s = (torch.empty(1, 256, device="cuda", dtype=t) for t in (torch.bfloat16, f8, torch.float32))
+    at, n0 = [t.data_ptr() for t in (x, q, s)], ctx.launches
+    stream = torch.cuda.current_stream().cuda_stream
+    for big in (2 ** 31 - 496, 2 ** 31 - 16):
+        for rows in (1, 128):
+            assert wdc.LIB.wdc_op_quantize_fp8(ctx._h, at[0], big, at[1], at[2], 1, big, rows, stream) == 3
+        for N, K in ((8, big), (big, 16), (big, big)):
+            assert wdc.LIB.wdc_op_gemm_fp8(ctx._h, at[1], at[2], at[1], at[2], None, at[0], 1, N, K, 0, None, None, stream) == 3
+    assert ctx.launches == n0
