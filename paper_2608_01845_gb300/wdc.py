@@ -530,6 +530,8 @@ class Context:
         what, (dt, dev, f8, f32, _) = "op_quantize_fp8", self._operand_types()
         if x.dim() != 2:
             raise ValueError(f"{what}: x must be [M, K]")
+        if block_rows not in (1, 128):
+            raise ValueError(f"{what}: block_rows must be 1 or 128, not {block_rows}")
         M, K = x.shape
         _sizes(what, M, K)
         kb = -(-K // 128)
@@ -575,6 +577,7 @@ class Context:
         if rot is not None:
             if rot.dim() != 3 or rot.shape[2] != 2:
                 raise ValueError(f"{what}: rot must be [positions, rot_dim / 2, 2]")
+            _sizes(what, rot.shape[0], 2 * rot.shape[1])
             _tensor(what, "rot", rot, f32, rot.shape, dev)
             at, (n, pairs, _) = rot.data_ptr(), rot.shape
         return HeadNorm(_address(q_weight), _address(k_weight), eps, at, n, 2 * pairs, int(bool(interleaved)),
@@ -588,7 +591,7 @@ class Context:
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError(f"{what}: q must be [heads, T, d] and k [kv_heads, T, d]")
         (H, T, d), kv = q.shape, k.shape[0]
-        _sizes(what, T, H, kv)
+        _sizes(what, T, H, kv, d)
         _tensor(what, "qkv", qkv, dt, (T, (H + 2 * kv) * d), dev, row_stride=True)
         _tensor(what, "q", q, dt, (H, T, d), dev)
         _tensor(what, "k", k, dt, (kv, T, d), dev)

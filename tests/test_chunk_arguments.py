@@ -146,3 +146,26 @@ def test_oracle_attention_of_a_dense_cache():
         assert np.allclose(o[:, h], p @ v[0, 0])
     assert list(chunk.limits(4, 6, 1)) == [3, 4, 5, 6] and list(chunk.limits(4, 6, 4)) == [4, 4, 6, 6]
     assert list(chunk.limits(4, 2, 1)) == [0, 0, 1, 2]
+
+
+def test_heads_and_angles_beyond_an_int(ctx, monkeypatch):
+    """A head's size, a block's rows, the positions and the pairs of the angles are ints of the C ABI as well."""
+    f, m = torch.float32, lambda *s, dtype=BF: torch.empty(*s, dtype=dtype, device="meta")
+    big = 2 ** 32 + 64
+    monkeypatch.setattr(wdc.LIB, "wdc_op_qk_norm_rope", lambda *a: pytest.fail("called"))
+    monkeypatch.setattr(wdc.LIB, "wdc_op_qk_norm_rope_append", lambda *a: pytest.fail("called"))
+    monkeypatch.setattr(ctx, "_op_stream", lambda s: 0)
+    monkeypatch.setattr(wdc.LIB, "wdc_op_quantize_fp8", lambda *a: pytest.fail("called"))
+    for rows in (2 ** 32 + 1, 1 - 2 ** 32, 2 ** 32 + 128):         # (1 or 128 once cut off)
+        for scale in (e(1, 1, dtype=f), e(1, 4, dtype=f)):
+            with pytest.raises(ValueError):
+                ctx.op_quantize_fp8(e(4, 64), e(4, 64, dtype=F8), scale, block_rows=rows)
+    good = dict(qkv=e(5, 4 * 64), q=e(2, 5, 64), k=e(1, 5, 64))
+    app = dict(qkv=e(5, 4 * 64), q=e(5, 2, 64), cache=cache(), q_start=e(2, dtype=I32))
+    with pytest.raises(ValueError, match="a size of"):
+        ctx.op_qk_norm_rope(m(1, 3 * big), m(1, 1, big), m(1, 1, big))
+    for rot in (m(big, 16, 2, dtype=f), m(1, 2 ** 31 + 8, 2, dtype=f), m(1, 2 ** 30 + 8, 2, dtype=f)):
+        with pytest.raises(ValueError, match="a size of"):
+            ctx.op_qk_norm_rope(**good, rot=rot)
+        with pytest.raises(ValueError, match="a size of"):
+            ctx.op_qk_norm_rope_append(**app, rot=rot)
