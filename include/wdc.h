@@ -524,8 +524,10 @@ wdc_status wdc_op_quantize_fp8(wdc_ctx* ctx, const void* x, long long ldx, void*
  * (wdc_op_quantize_fp8's layouts), any fp32 scales:
  *   sum over blocks b of a_scale[b][m] w_scale[n/128][b] sum_{k in b} A[m,k] W[n,k].
  * A block's 128 products are summed by the tensor core, the scaled block sums
- * in fp32.  bias, gelu, res, gate and C as in wdc_op_gemm (C and res [M, N] in
- * the model dtype, res may equal C).  N % 8 == 0 and K % 16 == 0, both at most
+ * in fp32 (the two scales are multiplied first, in fp32 too: their product is to
+ * be 0 or a normal number).  bias, gelu, res, gate and C as in wdc_op_gemm (C and res
+ * [M, N] in the model dtype, res may equal C); GELU's exponential and quotient
+ * are approximations, together within 2^-18 of its value for either dtype.  N % 8 == 0 and K % 16 == 0, both at most
  * 2^31 - 512 (WDC_ERR_UNSUPPORTED otherwise). */
 wdc_status wdc_op_gemm_fp8(wdc_ctx* ctx, const void* A, const float* a_scale, const void* W, const float* w_scale,
                            const float* bias, void* C, int M, int N, int K, int gelu, const void* res,
@@ -548,7 +550,9 @@ typedef struct wdc_paged_cache {
  * normalised to y = x / sqrt(mean(x^2) + eps) * weight and its first rot_dim
  * elements are turned by the angles of the token's position p: of each pair
  * (a, b), a' = a cos - b sin and b' = b cos + a sin.  Statistics, weights and
- * angles in fp32, one rounding to the model dtype. */
+ * angles in fp32, one rounding to the model dtype.  (The squares too: a head with
+ * elements above about 10^18 comes out zero; without eps, one below 10^-19 is
+ * imprecise, and below 10^-23 infinite or NaN.) */
 typedef struct wdc_head_norm {
     const float* q_weight;      /* device [head_dim], or NULL (= 1)               */
     const float* k_weight;
@@ -564,8 +568,9 @@ typedef struct wdc_head_norm {
 
 /* Norm and rotation of T rows qkv [T][(heads + 2 kv_heads) * d] (model dtype,
  * row stride ld elements, ld % 8 == 0: query heads, key heads, value heads) into
- * wdc_op_attention's operands: q [heads, T, d], k [kv_heads, T, d] and, unless
- * vt is NULL, V^T [kv_heads, d, ldv] (fp16 for a bf16 model, beyond whose range
+ * the layout of wdc_op_attention's operands (which has as many key heads as query
+ * heads: fewer of them are the caller's to repeat): q [heads, T, d], k [kv_heads,
+ * T, d] and, unless vt is NULL, V^T [kv_heads, d, ldv] (fp16 for a bf16 model, beyond whose range
  * values are saturated and set bit 8; ldv as there, its padding columns are left
  * as they are).  d 64 or 128. */
 wdc_status wdc_op_qk_norm_rope(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
@@ -589,9 +594,14 @@ wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* ctx, const void* qkv, long long l
  * and are left as they are).  The token at place p of a sequence of length L sees
  *   frame == 0: all L tokens;   frame == 1: tokens 0 .. p;
  *   frame >= 2: its frame and those before it, tokens 0 .. min(L, (p / frame + 1) frame) - 1.
- * A row that sees nothing is zero.  Whatever a page holds behind its sequence's
- * last token is not used, infinities and NaN included; a non-finite value V of a
- * token within the sequence may reach every row of the chunk.  Rows from
+ * A row that sees nothing is zero.  Scores, row sums and O are fp32; a
+ * probability is held in fp16, as is its exponent relative to its row's base (a
+ * maximum of the row's, up to 2^8 below it): those above 2^-8 of the base are off by
+ * less than 2^-8 of themselves, relatively, smaller ones by less than twice that
+ * down to 2^-14, and below 2^-25 they are 0.  Scores are to stay below 2^27 in
+ * size.  Whatever a page holds behind its sequence's last token is not used,
+ * infinities and NaN included; a non-finite value V of a token within the
+ * sequence may reach every row of the chunk.  Rows from
  * q_start[sequences] on are left as they are.  A sequence's keys may be split over
  * several CTAs and merged, through the workspace wdc_op_attention uses: two
  * attention calls of one context, and graphs that hold some, must not run

@@ -23,11 +23,14 @@
 //  * Each row has a limit of its own.  A row that has seen nothing yet (masked, or
 //    scores of -infinity) takes the next tile's maximum as its exponent base, as at
 //    the first step, and nothing over from before it.
-//  * Row sums add the fp16 probabilities in fp32 (mixed-precision adds).
+//  * P is fp16, as the PV product takes it, and so are the exponents (exp2_pair_f); row sums
+//    add these probabilities in fp32 (mixed-precision adds).
+//  * A base is a rounded product, off by up to 2^-24 of itself: 8 at scores of 2^27,
+//    still within what fp16 holds.
 // Measured: one token of 32 heads on 8 of 128 in 16 sequences of 16000 keys 5.9 TB/s,
 // 0.87 of a copy (one tile: bound by memory, what is missing are the parts' starts and
-// ends); 24 heads of 128, 13568 tokens onto themselves 1720 TFLOP/s, 48 of 64, 17776
-// 1220 (two tiles: bound by the chain S -> softmax -> P -> PV, whose S and P have one
+// ends); 24 heads of 128, 13568 tokens onto themselves 1640 to 1730 TFLOP/s, 48 of 64, 17776
+// 1180 to 1200 (two tiles: bound by the chain S -> softmax -> P -> PV, whose S and P have one
 // buffer a tile, 0.77 us a step of 64 keys of 128 or 1.0 of 128 keys of 64).
 // Where there are few units, each is split over its keys into parts of equal
 // numbers of steps (find_item), which the last of them to be done (one tile) or a second kernel

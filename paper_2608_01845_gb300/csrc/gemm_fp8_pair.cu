@@ -13,8 +13,9 @@
 // buffer's MMAs cover 512.  (Buffers of half a tile, four of them, were slower: 63 us
 // where these took 50, as each costs a round of its own.)
 //
-// Bound by that round: 17776 x 9216 x 3072 bf16 381 us, 2640 TFLOP/s, 0.68 of the fp8
-// rate; 1350 x 3072 x 12288 43 us, where 72 tiles of 76 pairs hold 12% rows past M.
+// Bound by that round: 17776 x 9216 x 3072 bf16 380 to 400 us, 2520 to 2650 TFLOP/s, 0.65
+// to 0.69 of the fp8 rate; 1350 x 3072 x 12288 43 to 46 us, where 72 tiles of 76 pairs hold
+// 12% rows past M; 1576 rows 80 us, as 84 tiles take two rounds.
 //
 // Once a tile's last block is added, the warps finish it (bias, GELU, gated
 // residual), a slab of 32 rows x 128 bytes at a time through swizzled shared

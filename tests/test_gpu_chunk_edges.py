@@ -140,3 +140,24 @@ def test_widths_that_tiles_would_take_past_an_int(contexts):
         for N, K in ((8, big), (big, 16), (big, big)):
             assert wdc.LIB.wdc_op_gemm_fp8(ctx._h, at[1], at[2], at[1], at[2], None, at[0], 1, N, K, 0, None, None, stream) == 3
     assert ctx.launches == n0
+
+
+@pytest.mark.parametrize("new,past", [([1], [1500]), ([200], [30]), ([300], [1700])])
+@pytest.mark.parametrize("d,key", [(64, 2.0 ** 16.5), (128, 2.0 ** 17)])
+def test_scores_near_the_largest(contexts, d, key, new, past):
+    """Two kinds of keys with scores of about 2^26.5 and minus that: the mean over the first kind's values,
+    of equal probabilities, so that an error of theirs drops out."""
+    ctx = contexts["bf16"]
+    lens = [n + p for n, p in zip(new, past)]
+    P = Paged(109, lens, 32, 2, d)
+    for b, n in enumerate(lens):
+        i = np.arange(n)
+        k = np.zeros((n, 2, d), np.float32)
+        k[:, :, 1] = synth.bf16_round(np.where(i % 3 == 0, key, -key).astype(np.float32))[:, None]
+        P.k[P.table[b, i // 32], :, i % 32] = k
+    P.dk.copy_(dev(P.k, torch.bfloat16))
+    q = np.zeros((sum(new), 4, d), np.float32)
+    q[:, :, 1] = 2.0 ** 13
+    o = attend(ctx, q, P, new, 1)
+    want, mag = chunk.attention_paged(q, P.k, P.v, P.table, lens, starts(new), 1)
+    assert (np.abs(host(o).reshape(want.shape) - want) <= attention_bound(want, mag, max(lens))).all()
