@@ -610,6 +610,104 @@ wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* ctx, const void* qkv, long long l
 wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_cache* cache, const int* q_start,
                                   int T, int heads, int max_new, int frame, void* o, wdc_stream stream);
 
+/* ------------------------------------------------------------------ a block in four bits
+ * What a chunk's block does between its attention and its projections, in few
+ * bits: the residual's sum with its norm and modulation, rows and weights in 4-bit
+ * floating point, their products, a gated MLP's among them, and the rotation of a
+ * video's heads by frame, row and column.  As the chunk operators: asynchronous on
+ * `stream`, checked before any launch, capturable, and nothing is launched where there
+ * are no rows.  A call of wdc_op_gemm_fp4 or wdc_op_gated_fp4 needs no workspace. */
+
+/* Positions of several axes (frame, row and column of a video's token, say): the
+ * turned pairs of a head are in sections, the first pairs[0] of them turned by the
+ * first axis, the next pairs[1] by the second, and so on, pair j of a section by
+ * table[a][coordinate][j] = (cos, sin) with the token's coordinate on that axis.
+ * All pairs together are a multiple of 8, at most head_dim / 2; which elements make
+ * pair i of a head is said by wdc_head_norm's `interleaved`, with rot_dim twice all
+ * pairs.  An axis may have no pairs: its table, rows and coordinates are not looked
+ * at.  A coordinate outside its table sets bit 2, and the nearest one is used. */
+typedef struct wdc_rot_axes {
+    int axes;                   /* 1 .. 4                                         */
+    const float* table[4];      /* device [rows][pairs][cos, sin] of each axis (8-byte aligned) */
+    int rows[4], pairs[4];
+    const int* coords;          /* device [T][axes] (4-byte aligned)              */
+} wdc_rot_axes;
+
+/* wdc_op_qk_norm_rope and wdc_op_qk_norm_rope_append with positions of several axes;
+ * the norm's rot is NULL (its rot_positions, rot_dim and positions are not looked at).
+ * Where a token is appended still follows from its place in its sequence. */
+wdc_status wdc_op_qk_norm_rope_axes(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
+                                    const wdc_head_norm* norm, const wdc_rot_axes* axes, void* q, void* k, void* vt,
+                                    wdc_stream stream);
+wdc_status wdc_op_qk_norm_rope_append_axes(wdc_ctx* ctx, const void* qkv, long long ld, int T, int heads,
+                                           const wdc_head_norm* norm, const wdc_rot_axes* axes,
+                                           const wdc_paged_cache* cache, const int* q_start, void* q, wdc_stream stream);
+
+/* A matrix [rows, K] of e2m1 numbers (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives)
+ * with an e4m3 scale for 16 columns and an fp32 scale for each row: element (r, k) stands
+ * for code * (scale * row_scale).  K is a multiple of 64. */
+typedef struct wdc_fp4 {
+    void* codes;                /* device [rows][K / 2]: the even column's code in the low four bits */
+    void* scale;                /* device e4m3 [ceil(rows / 128)][K / 64][512]: row r's scale of columns
+                                   16 j .. 16 j + 15 is byte (r % 32) * 16 + (r / 32 % 4) * 4 + j % 4 of
+                                   piece [r / 128][j / 4], without a sign; what rows behind the last hold
+                                   is not used */
+    float* row_scale;           /* device [rows]                                  */
+} wdc_fp4;
+
+/* Rows to e2m1, x [M, K] in the model dtype (row stride ldx >= K elements, ldx % 8 == 0),
+ * all in IEEE fp32, roundings to nearest even:
+ *   row_scale = max |x| * (1 / 2688) over the row, 0 where that maximum is below 2^-100;
+ *   scale     = e4m3(max |x| / (6 row_scale)) over 16 columns, at most 448;
+ *   code      = e2m1(x * (1 / (scale * row_scale))), at most 6 in size; 0 where the scale is.
+ * A row that holds an infinity or NaN has a NaN row_scale and zeros for the rest: it reads
+ * back, and comes out of a product, as NaN.  Scales of the rows behind M of the last 128
+ * are written as zeros. */
+wdc_status wdc_op_quantize_fp4(wdc_ctx* ctx, const void* x, long long ldx, const wdc_fp4* q, int M, int K,
+                               wdc_stream stream);
+/* And back: x[m, k] = code * (scale * row_scale) in fp32, rounded to the model dtype. */
+wdc_status wdc_op_dequantize_fp4(wdc_ctx* ctx, const wdc_fp4* q, void* x, long long ldx, int M, int K,
+                                 wdc_stream stream);
+
+/* C = epilogue(A W^T) of e2m1 matrices A [M, K] and W [N, K]:
+ *   sum_k (code scale)_A (code scale)_W, in fp32, times A's row_scale[m], times W's row_scale[n];
+ * bias, gelu, res, gate and C as in wdc_op_gemm (C and res [M, N] in the model dtype, res may
+ * equal C); GELU's accuracy as in wdc_op_gemm_fp8.  N % 8 == 0 (WDC_ERR_UNSUPPORTED otherwise). */
+wdc_status wdc_op_gemm_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W, const float* bias, void* C, int M, int N,
+                           int K, int gelu, const void* res, const float* gate, wdc_stream stream);
+/* A gated MLP's first half in one kernel: C [M, N] = f(A W_gate^T + gate_bias) * (A W_up^T +
+ * up_bias) with f(x) = x / (1 + exp(-x)), or GELU_tanh with gelu != 0; W_gate and W_up [N, K],
+ * the biases [N] fp32 or NULL.  The products as above; f is within 2^-18 of its value. */
+wdc_status wdc_op_gated_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W_gate, const wdc_fp4* W_up,
+                            const float* gate_bias, const float* up_bias, void* C, int M, int N, int K, int gelu,
+                            wdc_stream stream);
+
+/* The residual's sum, its norm and its modulation, rows [M, D] in the model dtype:
+ *   r = x + gate * delta                      (x alone without delta; gate NULL = 1)
+ *   y = r / sqrt(mean(r^2) + eps)             (center: (r - mean r) / sqrt(var r + eps))
+ *   out = y * (weight + weight_offset) + shift   (weight NULL: y + shift; shift NULL = 0)
+ * in fp32 from x and delta to the one rounding of each output: the norm is that of the sum
+ * before it is rounded into `total`.  One of out, q8 and q4 takes the result: in the model
+ * dtype, in e4m3 as wdc_op_quantize_fp8 (block_rows 1) lays A out, or in e2m1 as
+ * wdc_op_quantize_fp4 does, both from the fp32 values.  total and out may be x or delta.
+ * D % 16 == 0 (q4: 64), at most 16384; row strides multiples of 8. */
+typedef struct wdc_add_norm {
+    const void* x;              /* device [M, D], row stride ldx elements         */
+    const void* delta;          /* device [M, D], row stride ldd, or NULL         */
+    void* total;                /* device [M, D], row stride ldt: receives r; or NULL */
+    void* out;                  /* device [M, D], row stride ldo; or NULL         */
+    long long ldx, ldd, ldt, ldo;
+    void* q8;                   /* device e4m3 [M, D], contiguous; or NULL        */
+    float* scale;               /* with q8: device fp32 [ceil(D / 128)][M]        */
+    const wdc_fp4* q4;          /* host pointer to an e2m1 matrix [M, D]; or NULL */
+    const float *gate, *weight, *shift;   /* device [sets][D] fp32, or NULL        */
+    float weight_offset;        /* 1 for a modulation by 1 + scale                */
+    float eps;                  /* >= 0                                           */
+    int rows_per_set;           /* row m goes by vectors m / rows_per_set; 0: one set for all */
+    int center;                 /* 0: root-mean-square norm; 1: layer norm        */
+} wdc_add_norm;
+wdc_status wdc_op_add_norm(wdc_ctx* ctx, const wdc_add_norm* norm, int M, int D, wdc_stream stream);
+
 /* ------------------------------------------------------------------ allocation-free variant
  * wdc_observe_noalloc: the streaming half of the skip pass -- the kernelised
  * observation z_hat = sum_i kappa_i z_out_i over K latents together with the

@@ -1075,7 +1075,7 @@ wdc_status wdc_op_gemm_fp8(wdc_ctx* h, const void* A, const float* a_scale, cons
 wdc_status wdc_op_qk_norm_rope(wdc_ctx* h, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
                                const wdc_head_norm* norm, void* q, void* k, void* vt, wdc_stream stream) {
     return chunk_op(h, [&](Ctx* c) {
-        return op_qk_norm_rope(c, qkv, ld, T, heads, kv_heads, d, norm, q, k, vt, (cudaStream_t)stream);
+        return op_qk_norm_rope(c, qkv, ld, T, heads, kv_heads, d, norm, nullptr, q, k, vt, (cudaStream_t)stream);
     });
 }
 
@@ -1083,7 +1083,7 @@ wdc_status wdc_op_qk_norm_rope_append(wdc_ctx* h, const void* qkv, long long ld,
                                       const wdc_head_norm* norm, const wdc_paged_cache* cache, const int* q_start,
                                       void* q, wdc_stream stream) {
     return chunk_op(h, [&](Ctx* c) {
-        return op_qk_norm_rope_append(c, qkv, ld, T, heads, norm, cache, q_start, q, (cudaStream_t)stream);
+        return op_qk_norm_rope_append(c, qkv, ld, T, heads, norm, nullptr, cache, q_start, q, (cudaStream_t)stream);
     });
 }
 
@@ -1091,6 +1091,48 @@ wdc_status wdc_op_attention_paged(wdc_ctx* h, const void* q, const wdc_paged_cac
                                   int heads, int max_new, int frame, void* o, wdc_stream stream) {
     return chunk_op(h, [&](Ctx* c) {
         return op_attention_paged(c, q, cache, q_start, T, heads, max_new, frame, o, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_qk_norm_rope_axes(wdc_ctx* h, const void* qkv, long long ld, int T, int heads, int kv_heads, int d,
+                                    const wdc_head_norm* norm, const wdc_rot_axes* axes, void* q, void* k, void* vt,
+                                    wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        if (!axes) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: no wdc_rot_axes");
+        return op_qk_norm_rope(c, qkv, ld, T, heads, kv_heads, d, norm, axes, q, k, vt, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_qk_norm_rope_append_axes(wdc_ctx* h, const void* qkv, long long ld, int T, int heads,
+                                           const wdc_head_norm* norm, const wdc_rot_axes* axes,
+                                           const wdc_paged_cache* cache, const int* q_start, void* q, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        if (!axes) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: no wdc_rot_axes");
+        return op_qk_norm_rope_append(c, qkv, ld, T, heads, norm, axes, cache, q_start, q, (cudaStream_t)stream);
+    });
+}
+
+wdc_status wdc_op_add_norm(wdc_ctx* h, const wdc_add_norm* norm, int M, int D, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) { return op_add_norm(c, norm, M, D, (cudaStream_t)stream); });
+}
+
+wdc_status wdc_op_quantize_fp4(wdc_ctx* h, const void* x, long long ldx, const wdc_fp4* q, int M, int K, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) { return op_quantize_fp4(c, x, ldx, q, M, K, (cudaStream_t)stream); });
+}
+
+wdc_status wdc_op_dequantize_fp4(wdc_ctx* h, const wdc_fp4* q, void* x, long long ldx, int M, int K, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) { return op_dequantize_fp4(c, q, x, ldx, M, K, (cudaStream_t)stream); });
+}
+
+wdc_status wdc_op_gemm_fp4(wdc_ctx* h, const wdc_fp4* A, const wdc_fp4* W, const float* bias, void* C, int M, int N, int K,
+                           int gelu, const void* res, const float* gate, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) { return op_gemm_fp4(c, A, W, bias, C, M, N, K, gelu, res, gate, (cudaStream_t)stream); });
+}
+
+wdc_status wdc_op_gated_fp4(wdc_ctx* h, const wdc_fp4* A, const wdc_fp4* W_gate, const wdc_fp4* W_up, const float* gate_bias,
+                            const float* up_bias, void* C, int M, int N, int K, int gelu, wdc_stream stream) {
+    return chunk_op(h, [&](Ctx* c) {
+        return op_gated_fp4(c, A, W_gate, W_up, gate_bias, up_bias, C, M, N, K, gelu, (cudaStream_t)stream);
     });
 }
 

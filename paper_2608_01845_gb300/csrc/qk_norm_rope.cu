@@ -28,6 +28,11 @@ struct NormArgs {
     const float2* rot;                 // null: no rotation
     int rot_positions, rot_dim;
     const int* positions;
+    // several axes: the pairs in sections, each with a table of its own
+    int axes;
+    const float2* axis_rot[4];
+    int axis_rows[4], axis_end[4];     // rows of the table; the section's first pair behind it
+    const int* coords;                 // [T][axes]
     void *q, *k, *v;
     int ldv;                           // dense: V^T's row stride
     unsigned vt_tiles;                 // dense: blocks that transpose V
@@ -138,7 +143,8 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
     }
 }
 
-template <typename T, int D, bool APPEND, bool PAIRS>
+// What turns the heads: nothing or one table of positions, or a table for each axis.
+template <typename T, int D, bool APPEND, bool PAIRS, bool AXES>
 __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant__ NormArgs a) {
     using V = Vec<T>;
     constexpr int E = V::E, LPH = D / E, HPW = 32 / LPH;       // elements a lane, lanes a head, heads a warp-width
@@ -215,8 +221,32 @@ __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant
 
     // its angles, for the pairs of this lane
     float cs[E];                                               // cos, sin of each pair
-    const bool turned = a.rot && ea < (PAIRS ? a.rot_dim : half);
-    if (a.rot) {
+    const bool turned = (AXES || a.rot) && ea < (PAIRS ? a.rot_dim : half);
+    if constexpr (AXES) {
+        // (the token, and so its place on each axis, is the same for the whole warp)
+        const int first = PAIRS ? ea / 2 : ea;
+        int begin = 0;
+        for (int x = 0; x < a.axes; ++x) {
+            const int end = a.axis_end[x];
+            if (end == begin) continue;
+            int p = a.coords[(size_t)t * a.axes + x];
+            if (p < 0 || p >= a.axis_rows[x]) {
+                if (lane == 0) atomicOr(a.err, kErrBounds);
+                p = max(0, min(p, a.axis_rows[x] - 1));
+            }
+            const float2* r = a.axis_rot[x] + (size_t)p * (end - begin) - begin;
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i)
+                    if (first + i >= begin && first + i < end) {
+                        const float2 c = r[first + i];
+                        cs[2 * i] = c.x;
+                        cs[2 * i + 1] = c.y;
+                    }
+            }
+            begin = end;
+        }
+    } else if (a.rot) {
         int p = a.positions ? a.positions[t] : place;
         if (p < 0 || p >= a.rot_positions) {
             if (lane == 0) atomicOr(a.err, kErrBounds);
@@ -319,8 +349,10 @@ wdc_status launch(Ctx* c, NormArgs& a, bool pairs, int vt_tiles, cudaStream_t s)
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_NORM, s);
-        if (pairs) launch_kernel(norm_rope_kernel<T, D, APPEND, true>, grid, 256, 0, s, 1, a);
-        else launch_kernel(norm_rope_kernel<T, D, APPEND, false>, grid, 256, 0, s, 1, a);
+        if (a.axes > 0 && pairs) launch_kernel(norm_rope_kernel<T, D, APPEND, true, true>, grid, 256, 0, s, 1, a);
+        else if (a.axes > 0) launch_kernel(norm_rope_kernel<T, D, APPEND, false, true>, grid, 256, 0, s, 1, a);
+        else if (pairs) launch_kernel(norm_rope_kernel<T, D, APPEND, true, false>, grid, 256, 0, s, 1, a);
+        else launch_kernel(norm_rope_kernel<T, D, APPEND, false, false>, grid, 256, 0, s, 1, a);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("norm and rotation: ") + cudaGetErrorString(e));
@@ -350,12 +382,40 @@ wdc_status take(Ctx* c, NormArgs& a, const void* qkv, long long ld, int T, int h
     return WDC_OK;
 }
 
+// The axes, where there are some (null: the table of wdc_head_norm, or none).
+wdc_status take_axes(Ctx* c, NormArgs& a, int d, const wdc_head_norm* n, const wdc_rot_axes* x) {
+    if (!x) return WDC_OK;
+    if (n->rot) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: a table of positions beside axes");
+    if (x->axes < 1 || x->axes > 4) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: 1 to 4 axes wanted");
+    long long pairs = 0;
+    for (int i = 0; i < x->axes; ++i) {
+        if (x->pairs[i] < 0) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: an axis' pairs must be >= 0");
+        pairs += x->pairs[i];
+        if (pairs > d / 2) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: the axes' pairs exceed head_dim / 2");
+        a.axis_end[i] = (int)pairs;
+        if (x->pairs[i] == 0) continue;                        // (its table and coordinates are not looked at)
+        if (x->rows[i] < 1) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: an axis' table needs rows >= 1");
+        if (a.T > 0 && (!x->table[i] || !x->coords)) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
+        if ((uintptr_t)x->table[i] & 7) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: an axis' table must be 8-byte aligned");
+        a.axis_rot[i] = reinterpret_cast<const float2*>(x->table[i]);
+        a.axis_rows[i] = x->rows[i];
+    }
+    if ((uintptr_t)x->coords & 3) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: coords must be 4-byte aligned");
+    if (pairs % 8) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: the axes' pairs must be a multiple of 8 in all");
+    if (pairs == 0) return WDC_OK;                             // nothing is turned
+    a.axes = x->axes;
+    a.coords = x->coords;
+    a.rot_dim = 2 * (int)pairs;
+    return WDC_OK;
+}
+
 }  // namespace
 
 wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n,
-                           void* q, void* k, void* vt, cudaStream_t s) {
+                           const wdc_rot_axes* axes, void* q, void* k, void* vt, cudaStream_t s) {
     NormArgs a{};
     if (wdc_status st = take(c, a, qkv, ld, T, heads, kv, d, n)) return st;
+    if (wdc_status st = take_axes(c, a, d, n, axes)) return st;
     if (T == 0) return WDC_OK;
     if (!q || !k) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)vt) & 15)
@@ -395,10 +455,12 @@ wdc_status check_cache(Ctx* c, const wdc_paged_cache* p, int* page_log2) {
 }
 
 wdc_status op_qk_norm_rope_append(Ctx* c, const void* qkv, long long ld, int T, int heads, const wdc_head_norm* n,
-                                  const wdc_paged_cache* p, const int* q_start, void* q, cudaStream_t s) {
+                                  const wdc_rot_axes* axes, const wdc_paged_cache* p, const int* q_start, void* q,
+                                  cudaStream_t s) {
     NormArgs a{};
     if (wdc_status st = check_cache(c, p, &a.page_log2)) return st;
     if (wdc_status st = take(c, a, qkv, ld, T, heads, p->kv_heads, p->head_dim, n)) return st;
+    if (wdc_status st = take_axes(c, a, p->head_dim, n, axes)) return st;
     if (T == 0 || p->sequences == 0) return WDC_OK;
     if (!q || !q_start) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
     if ((uintptr_t)q & 15) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: pointers must be 16-byte aligned");

@@ -1,0 +1,168 @@
+// What the kernels that write 8 and 4 bits share (quant_fp8.cu, quant_fp4.cu,
+// add_norm.cu): 16-byte loads of a row, maxima, and the conversions.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "dit_kernels.cuh"
+
+namespace wdc {
+
+constexpr float kE4m3Max = 448.0f;
+
+// Maximum that keeps a NaN (fmaxf drops it).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// Four quotients to e4m3, to nearest even; beyond 448 saturated, NaN kept.
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+    uint32_t r;
+    asm("{\n .reg .b16 lo, hi;\n cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n"
+        " mov.b32 %0, {lo, hi};\n}"
+        : "=r"(r)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
+}
+
+// A lane's 8 elements in fp32.
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+__device__ __forceinline__ float absmax8(const float (&v)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(v[i]));
+    return m;
+}
+
+// The eight quotients by a scale outside the range of store8's shorter way.
+static __device__ __noinline__ uint2 quotients(float4 a, float4 b, float s) {
+    return make_uint2(e4m3x4(a.x / s, a.y / s, a.z / s, a.w / s), e4m3x4(b.x / s, b.y / s, b.z / s, b.w / s));
+}
+
+// The eight quotients by s, in e4m3.  With r the correctly rounded reciprocal of s,
+// t = x r corrected once by its remainder, t + (x - t s) r, is the correctly rounded
+// quotient (Markstein, "Computation of elementary functions on the IBM RISC
+// System/6000 processor", 1990) as long as nothing underflows that matters.  Three
+// instructions an element and little code: eight divisions a lane were what the
+// kernel waited for, and their code what a short call fetched (1576 x 3072 bf16 8.2
+// us, now 4.2).
+__device__ __forceinline__ void store8(uint8_t* q, const float (&v)[8], float s) {
+    uint2 w;
+    const float by = s == 0.f ? 1.f : s;           // a block of zeros (or one so small that its scale is)
+    if (by >= 0x1p-100f && by < INFINITY) {
+        const float r = 1.0f / by;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = v[i] * r;
+            y[i] = fmaf(fmaf(-t, by, v[i]), r, t);
+        }
+        w = make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
+    } else {
+        w = quotients(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s);
+    }
+    *reinterpret_cast<uint2*>(q) = w;
+}
+
+// ---------------------------------------------------------------- four bits
+// Scales of 16 columns lie in pieces of 512 bytes, for 128 rows and 64 columns each:
+// byte (row % 32) * 16 + (row / 32 % 4) * 4 + (column / 16) % 4, the order in which
+// the tensor core takes them.  A word holds the four scales of a row's 64 columns.
+constexpr int kPiece4 = 512, kPieceCols4 = 64;
+// The widest matrix of the e2m1 operators (as kMaxWidth8).
+constexpr int kMaxWidth4 = 0x7fffffff - 511;
+constexpr int kMaxRows4 = 0x7fffffff - 127;        // rounded up to 128 rows still an int
+constexpr float kRow4 = 1.0f / 2688;     // a row's scale of its largest magnitude: 6 (e2m1) * 448 (e4m3) steps
+
+__device__ __forceinline__ size_t piece_word4(int row, int piece, int pieces) {
+    return ((size_t)(row >> 7) * pieces + piece) * (kPiece4 / 4) + (row & 31) * 4 + (row >> 5 & 3);
+}
+
+// A row's scale from its largest magnitude: 0 where that is below 2^-100 (no
+// intermediate below is then subnormal), NaN where it is infinite or NaN.
+__device__ __forceinline__ float row_scale4(float top) {
+    return !(top < INFINITY) ? __int_as_float(0x7fffffff) : (top < 0x1p-100f ? 0.f : top * kRow4);
+}
+
+// Eight values to e2m1, the first in the low bits; to nearest even, beyond 6 saturated.
+__device__ __forceinline__ uint32_t e2m1x8(const float (&y)[8]) {
+    uint32_t r;
+    asm("{\n .reg .b8 a, b, c, d;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+        " mov.b32 %0, {a, b, c, d};\n}"
+        : "=r"(r)
+        : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+    return r;
+}
+
+// Their values.
+__device__ __forceinline__ void e2m1_values(uint32_t q, float (&v)[8]) {
+    uint32_t h[4];
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
+        " cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(q));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+
+// A lane's 8 elements, rounded to the model's type.
+__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A lane's 8 neighbouring columns of a row (two lanes a scale, eight a word of
+// scales) to codes and scales; `row` is the row's scale and `six` 6 times it.  The
+// whole warp calls it; lanes past the row's end hold zeros and have no `codes`.
+__device__ __forceinline__ void store_fp4(const float (&v)[8], float row, float six, uint32_t* codes, uint32_t* word) {
+    float top = absmax8(v);
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const bool live = row > 0.f;                   // (not for NaN either)
+    // (IEEE: the quotient of the definition)
+    const uint32_t s = live ? e4m3x4(__fdiv_rn(top, six), 0.f, 0.f, 0.f) & 0xffu : 0u;
+    const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s, __NV_E4M3))) * row;
+    const float by = live && step > 0.f ? __frcp_rn(step) : 0.f;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = live ? v[i] * by : 0.f;
+    const uint32_t q = e2m1x8(y);
+    if (codes) *codes = q;
+    const uint32_t s1 = __shfl_down_sync(0xffffffffu, s, 2), s2 = __shfl_down_sync(0xffffffffu, s, 4),
+                   s3 = __shfl_down_sync(0xffffffffu, s, 6);
+    if (codes && word) *word = s | s1 << 8 | s2 << 16 | s3 << 24;
+}
+
+}  // namespace wdc

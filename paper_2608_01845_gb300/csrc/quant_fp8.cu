@@ -2,85 +2,13 @@
 //   s = max |x| / 448,  q = e4m3(x / s).
 // One pass over x: a block's elements stay in registers between its maximum
 // and its quotients.  Bound by memory: 3 bytes an element for bf16, 5 for fp32.
-#include "dit_kernels.cuh"
+#include "quant.cuh"
 
 namespace wdc {
 
 namespace {
 
 constexpr int kBlock = 128;             // columns (and, for weights, rows) of a block
-constexpr float kE4m3Max = 448.0f;
-
-// Maximum that keeps a NaN (fmaxf drops it).
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-
-// Four quotients to e4m3, to nearest even; beyond 448 saturated, NaN kept.
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
-    uint32_t r;
-    asm("{\n .reg .b16 lo, hi;\n cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n"
-        " mov.b32 %0, {lo, hi};\n}"
-        : "=r"(r)
-        : "f"(a), "f"(b), "f"(c), "f"(d));
-    return r;
-}
-
-// A lane's 8 elements in fp32.
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-
-__device__ __forceinline__ float absmax8(const float (&v)[8]) {
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(v[i]));
-    return m;
-}
-
-// The eight quotients by a scale outside the range of store8's shorter way.
-__device__ __noinline__ uint2 quotients(float4 a, float4 b, float s) {
-    return make_uint2(e4m3x4(a.x / s, a.y / s, a.z / s, a.w / s), e4m3x4(b.x / s, b.y / s, b.z / s, b.w / s));
-}
-
-// The eight quotients by s, in e4m3.  With r the correctly rounded reciprocal of s,
-// t = x r corrected once by its remainder, t + (x - t s) r, is the correctly rounded
-// quotient (Markstein, "Computation of elementary functions on the IBM RISC
-// System/6000 processor", 1990) as long as nothing underflows that matters.  Three
-// instructions an element and little code: eight divisions a lane were what the
-// kernel waited for, and their code what a short call fetched (1576 x 3072 bf16 8.2
-// us, now 4.2).
-__device__ __forceinline__ void store8(uint8_t* q, const float (&v)[8], float s) {
-    uint2 w;
-    const float by = s == 0.f ? 1.f : s;           // a block of zeros (or one so small that its scale is)
-    if (by >= 0x1p-100f && by < INFINITY) {
-        const float r = 1.0f / by;
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float t = v[i] * r;
-            y[i] = fmaf(fmaf(-t, by, v[i]), r, t);
-        }
-        w = make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
-    } else {
-        w = quotients(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s);
-    }
-    *reinterpret_cast<uint2*>(q) = w;
-}
 
 // Scales along rows.  Sixteen lanes hold a block, a warp kSpan neighbouring
 // pairs of blocks of one row (all loaded before the first is reduced), and the

@@ -348,12 +348,24 @@ wdc_status op_gemm_fp8(Ctx* c, const void* A, const float* a_scale, const void* 
                        const float* bias, void* C, int M, int N, int K, int gelu, const void* res, const float* gate,
                        cudaStream_t s);
 wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n,
-                           void* q, void* k, void* vt, cudaStream_t s);
+                           const wdc_rot_axes* axes, void* q, void* k, void* vt, cudaStream_t s);
 wdc_status op_qk_norm_rope_append(Ctx* c, const void* qkv, long long ld, int T, int heads, const wdc_head_norm* n,
-                                  const wdc_paged_cache* p, const int* q_start, void* q, cudaStream_t s);
+                                  const wdc_rot_axes* axes, const wdc_paged_cache* p, const int* q_start, void* q,
+                                  cudaStream_t s);
 wdc_status op_attention_paged(Ctx* c, const void* q, const wdc_paged_cache* p, const int* q_start, int T, int heads,
                               int max_new, int frame, void* o, cudaStream_t s);
 // Checks a cache's description; *page_log2: its page size.
 wdc_status check_cache(Ctx* c, const wdc_paged_cache* p, int* page_log2);
+
+// quant_fp4.cu, gemm_fp4.cu, add_norm.cu: a block in four bits
+wdc_status op_quantize_fp4(Ctx* c, const void* x, long long ldx, const wdc_fp4* q, int M, int K, cudaStream_t s);
+wdc_status op_dequantize_fp4(Ctx* c, const wdc_fp4* q, void* x, long long ldx, int M, int K, cudaStream_t s);
+wdc_status op_gemm_fp4(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const float* bias, void* C, int M, int N, int K, int gelu,
+                       const void* res, const float* gate, cudaStream_t s);
+wdc_status op_gated_fp4(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const wdc_fp4* U, const float* gate_bias,
+                        const float* up_bias, void* C, int M, int N, int K, int gelu, cudaStream_t s);
+wdc_status op_add_norm(Ctx* c, const wdc_add_norm* n, int M, int D, cudaStream_t s);
+// Checks an e2m1 matrix' pointers.
+wdc_status check_fp4(Ctx* c, const wdc_fp4* q);
 
 }  // namespace wdc

@@ -120,6 +120,24 @@ class PagedCacheC(ctypes.Structure):
                 + [(n, ctypes.c_int) for n in ["pages", "page", "kv_heads", "head_dim", "sequences", "table_width"]])
 
 
+class RotAxesC(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int), ("table", ctypes.c_void_p * 4), ("rows", ctypes.c_int * 4),
+                ("pairs", ctypes.c_int * 4), ("coords", ctypes.c_void_p)]
+
+
+class Fp4C(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ["codes", "scale", "row_scale"]]
+
+
+class AddNorm(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ["x", "delta", "total", "out"]]
+                + [(n, ctypes.c_longlong) for n in ["ldx", "ldd", "ldt", "ldo"]]
+                + [("q8", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("q4", ctypes.POINTER(Fp4C))]
+                + [(n, ctypes.c_void_p) for n in ["gate", "weight", "shift"]]
+                + [("weight_offset", ctypes.c_float), ("eps", ctypes.c_float), ("rows_per_set", ctypes.c_int),
+                   ("center", ctypes.c_int)])
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libwdc.so not built at {LIB_PATH}; run `python -m paper_2608_01845_gb300.build`")
@@ -169,6 +187,16 @@ def _load():
         "wdc_op_qk_norm_rope_append": (I, [P, P, ctypes.c_longlong, I, I, ctypes.POINTER(HeadNorm),
                                            ctypes.POINTER(PagedCacheC), P, P, P]),
         "wdc_op_attention_paged": (I, [P, P, ctypes.POINTER(PagedCacheC), P, I, I, I, I, P, P]),
+        "wdc_op_qk_norm_rope_axes": (I, [P, P, ctypes.c_longlong, I, I, I, I, ctypes.POINTER(HeadNorm),
+                                         ctypes.POINTER(RotAxesC), P, P, P, P]),
+        "wdc_op_qk_norm_rope_append_axes": (I, [P, P, ctypes.c_longlong, I, I, ctypes.POINTER(HeadNorm),
+                                                ctypes.POINTER(RotAxesC), ctypes.POINTER(PagedCacheC), P, P, P]),
+        "wdc_op_add_norm": (I, [P, ctypes.POINTER(AddNorm), I, I, P]),
+        "wdc_op_quantize_fp4": (I, [P, P, ctypes.c_longlong, ctypes.POINTER(Fp4C), I, I, P]),
+        "wdc_op_dequantize_fp4": (I, [P, ctypes.POINTER(Fp4C), P, ctypes.c_longlong, I, I, P]),
+        "wdc_op_gemm_fp4": (I, [P, ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), P, P, I, I, I, I, P, P, P]),
+        "wdc_op_gated_fp4": (I, [P, ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), P, P, P, I, I, I, I,
+                                 P]),
         "wdc_observe_noalloc": (I, [ctypes.POINTER(P), I, ctypes.POINTER(D), P, P, P, S, ctypes.c_uint32, P]),
     }
     for name, (res, args) in sig.items():
@@ -245,6 +273,58 @@ class PagedCache:
         self.k, self.v, self.table, self.length = k, v, table, length
         self.c = PagedCacheC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), k.shape[0], k.shape[2],
                              k.shape[1], k.shape[3], table.shape[0], table.shape[1])
+
+
+class Fp4Matrix:
+    """wdc_fp4 over torch tensors, which it keeps alive: codes uint8 [rows, K / 2] (the even
+    column's code in the low four bits), scale float8_e4m3fn [ceil(rows / 128), K / 64, 512]
+    (see include/wdc.h) and row_scale float32 [rows].  ``Fp4Matrix.empty`` allocates one."""
+
+    def __init__(self, codes, scale, row_scale):
+        import torch
+        if codes.dim() != 2 or codes.shape[1] % 32 or codes.shape[1] < 1:
+            raise ValueError("Fp4Matrix: codes must be [rows, K / 2] with K a multiple of 64")
+        M, K = codes.shape[0], 2 * codes.shape[1]
+        _sizes("Fp4Matrix", M, K)
+        self.device = dev = codes.get_device()
+        _tensor("Fp4Matrix", "codes", codes, torch.uint8, codes.shape, dev)
+        _tensor("Fp4Matrix", "scale", scale, torch.float8_e4m3fn, (-(-M // 128), K // 64, 512), dev)
+        _tensor("Fp4Matrix", "row_scale", row_scale, torch.float32, (M,), dev)
+        self.codes, self.scale, self.row_scale, self.shape = codes, scale, row_scale, (M, K)
+        self.c = Fp4C(codes.data_ptr(), scale.data_ptr(), row_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, rows, K, device=0):
+        """An uninitialised matrix on the device (op_quantize_fp4 fills it)."""
+        import torch
+        if K % 64 or K < 64 or rows < 0:
+            raise ValueError(f"Fp4Matrix: {rows} rows of {K} columns (a multiple of 64 is wanted)")
+        e = lambda *shape, dtype: torch.empty(*shape, dtype=dtype, device=f"cuda:{device}")
+        return cls(e(rows, K // 2, dtype=torch.uint8), e(-(-rows // 128), K // 64, 512, dtype=torch.float8_e4m3fn),
+                   e(rows, dtype=torch.float32))
+
+
+class RotAxes:
+    """wdc_rot_axes over torch tensors, which it keeps alive: ``tables``, one float32 [rows, pairs, 2] (cos, sin)
+    for each of 1 to 4 axes, and coords int32 [T, axes], the place of each token on each axis."""
+
+    def __init__(self, tables, coords):
+        import torch
+        tables = list(tables)
+        if not 1 <= len(tables) <= 4 or coords.dim() != 2 or coords.shape[1] != len(tables):
+            raise ValueError("RotAxes: 1 to 4 tables and coords [T, axes]")
+        self.device = dev = coords.get_device()
+        _sizes("RotAxes", coords.shape[0])
+        _tensor("RotAxes", "coords", coords, torch.int32, coords.shape, dev)
+        self.tables, self.coords, self.pairs = tables, coords, 0
+        self.c = RotAxesC(len(tables), coords=coords.data_ptr() or None)
+        for i, t in enumerate(tables):
+            if t.dim() != 3 or t.shape[2] != 2:
+                raise ValueError("RotAxes: a table must be [rows, pairs, 2]")
+            _sizes("RotAxes", t.shape[0], t.shape[1])
+            _tensor("RotAxes", f"tables[{i}]", t, torch.float32, t.shape, dev)
+            self.c.table[i], self.c.rows[i], self.c.pairs[i] = t.data_ptr() or None, t.shape[0], t.shape[1]
+            self.pairs += t.shape[1]
 
 
 def _tensor(what, name, t, dtype, shape, device, row_stride=False):
@@ -565,6 +645,13 @@ class Context:
                                         _address(bias), C.data_ptr(), M, N, K, int(gelu), _address(res), _address(gate),
                                         self._op_stream(stream)), what)
 
+    def _rot_axes(self, what, axes, T, rot, positions):
+        if rot is not None or positions is not None:
+            raise ValueError(f"{what}: rot and positions beside axes")
+        if axes.device != self._operand_types()[1] or axes.coords.shape[0] != T:
+            raise ValueError(f"{what}: axes must be on device {self._operand_types()[1]} with coordinates of {T} tokens")
+        return axes.c
+
     def _head_norm(self, what, d, T, q_weight, k_weight, eps, rot, positions, interleaved):
         _, dev, _, f32, i32 = self._operand_types()
         if q_weight is not None:
@@ -584,9 +671,10 @@ class Context:
                         _address(positions))
 
     def op_qk_norm_rope(self, qkv, q, k, vt=None, q_weight=None, k_weight=None, eps=1e-6, rot=None, positions=None,
-                        interleaved=True, stream=None):
+                        interleaved=True, stream=None, axes=None):
         """wdc_op_qk_norm_rope: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) to q [heads, T, d],
-        k [kv_heads, T, d] and vt [kv_heads, d, T rounded up to 8] (fp16; fp32 and T for an fp32 model)."""
+        k [kv_heads, T, d] and vt [kv_heads, d, T rounded up to 8] (fp16; fp32 and T for an fp32 model).
+        axes (a RotAxes, in place of rot and positions): wdc_op_qk_norm_rope_axes."""
         what, (dt, dev, _, f32, _) = "op_qk_norm_rope", self._operand_types()
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError(f"{what}: q must be [heads, T, d] and k [kv_heads, T, d]")
@@ -600,13 +688,19 @@ class Context:
             bf16 = dt is not f32
             _tensor(what, "vt", vt, torch.float16 if bf16 else dt, (kv, d, -(-T // 8) * 8 if bf16 else T), dev)
         n = self._head_norm(what, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        if axes is not None:
+            x = self._rot_axes(what, axes, T, rot, positions)
+            self._check(LIB.wdc_op_qk_norm_rope_axes(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, kv, d, n, x,
+                                                     q.data_ptr(), k.data_ptr(), _address(vt), self._op_stream(stream)), what)
+            return
         self._check(LIB.wdc_op_qk_norm_rope(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, kv, d, n, q.data_ptr(),
                                             k.data_ptr(), _address(vt), self._op_stream(stream)), what)
 
     def op_qk_norm_rope_append(self, qkv, q, cache, q_start, q_weight=None, k_weight=None, eps=1e-6, rot=None,
-                               positions=None, interleaved=True, stream=None):
+                               positions=None, interleaved=True, stream=None, axes=None):
         """wdc_op_qk_norm_rope_append: rows qkv [T, (heads + 2 kv_heads) * d] (may lie apart) of new tokens to
-        q [T, heads, d], their keys and values into ``cache`` (a PagedCache); q_start int32 [sequences + 1]."""
+        q [T, heads, d], their keys and values into ``cache`` (a PagedCache); q_start int32 [sequences + 1].
+        axes (a RotAxes, in place of rot and positions): wdc_op_qk_norm_rope_append_axes."""
         what, (dt, dev, _, _, i32) = "op_qk_norm_rope_append", self._operand_types()
         if q.dim() != 3:
             raise ValueError(f"{what}: q must be [T, heads, d]")
@@ -618,6 +712,11 @@ class Context:
         _tensor(what, "q", q, dt, (T, H, d), dev)
         _tensor(what, "q_start", q_start, i32, (c.sequences + 1,), dev)
         n = self._head_norm(what, d, T, q_weight, k_weight, eps, rot, positions, interleaved)
+        if axes is not None:
+            x = self._rot_axes(what, axes, T, rot, positions)
+            self._check(LIB.wdc_op_qk_norm_rope_append_axes(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, n, x, c,
+                                                            q_start.data_ptr(), q.data_ptr(), self._op_stream(stream)), what)
+            return
         self._check(LIB.wdc_op_qk_norm_rope_append(self._h, qkv.data_ptr(), _row_stride(qkv), T, H, n, c,
                                                    q_start.data_ptr(), q.data_ptr(), self._op_stream(stream)), what)
 
@@ -637,6 +736,105 @@ class Context:
         self._check(LIB.wdc_op_attention_paged(self._h, q.data_ptr(), c, q_start.data_ptr(), T, H,
                                                max(-1, min(int(max_new), T)), max(-1, min(int(frame), _INT_MAX)),
                                                o.data_ptr(), self._op_stream(stream)), what)
+
+    # ---- a block in four bits
+
+    def _fp4(self, what, name, m, rows, K):
+        if m.device != self._operand_types()[1] or m.shape != (rows, K):
+            raise ValueError(f"{what}: {name} must be an Fp4Matrix ({rows}, {K}) on device {self._operand_types()[1]}, "
+                             f"not {m.shape} on {m.device}")
+        return m.c
+
+    def op_quantize_fp4(self, x, q, stream=None):
+        """wdc_op_quantize_fp4: x [M, K] (rows may lie apart) to q (an Fp4Matrix)."""
+        what, (dt, dev, *_) = "op_quantize_fp4", self._operand_types()
+        M, K = q.shape
+        _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
+        self._check(LIB.wdc_op_quantize_fp4(self._h, x.data_ptr(), _row_stride(x), self._fp4(what, "q", q, M, K), M, K,
+                                            self._op_stream(stream)), what)
+
+    def op_dequantize_fp4(self, q, x, stream=None):
+        """wdc_op_dequantize_fp4: the values of q (an Fp4Matrix) to x [M, K] (rows may lie apart)."""
+        what, (dt, dev, *_) = "op_dequantize_fp4", self._operand_types()
+        M, K = q.shape
+        _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
+        self._check(LIB.wdc_op_dequantize_fp4(self._h, self._fp4(what, "q", q, M, K), x.data_ptr(), _row_stride(x), M, K,
+                                              self._op_stream(stream)), what)
+
+    def op_gemm_fp4(self, A, W, C, bias=None, gelu=False, res=None, gate=None, stream=None):
+        """wdc_op_gemm_fp4: C = epilogue(A W^T) of Fp4Matrix operands, with the epilogues of op_gemm."""
+        what, (dt, dev, _, f32, _) = "op_gemm_fp4", self._operand_types()
+        (M, K), N = A.shape, W.shape[0]
+        _tensor(what, "C", C, dt, (M, N), dev)
+        if bias is not None:
+            _tensor(what, "bias", bias, f32, (N,), dev)
+        if res is not None:
+            _tensor(what, "res", res, dt, (M, N), dev)
+        if gate is not None:
+            _tensor(what, "gate", gate, f32, (N,), dev)
+        self._check(LIB.wdc_op_gemm_fp4(self._h, self._fp4(what, "A", A, M, K), self._fp4(what, "W", W, N, K), _address(bias),
+                                        C.data_ptr(), M, N, K, int(gelu), _address(res), _address(gate),
+                                        self._op_stream(stream)), what)
+
+    def op_gated_fp4(self, A, W_gate, W_up, C, gate_bias=None, up_bias=None, gelu=False, stream=None):
+        """wdc_op_gated_fp4: C = f(A W_gate^T + gate_bias) * (A W_up^T + up_bias) of Fp4Matrix operands; f is SiLU,
+        or GELU (its tanh form)."""
+        what, (dt, dev, _, f32, _) = "op_gated_fp4", self._operand_types()
+        (M, K), N = A.shape, W_gate.shape[0]
+        _tensor(what, "C", C, dt, (M, N), dev)
+        if gate_bias is not None:
+            _tensor(what, "gate_bias", gate_bias, f32, (N,), dev)
+        if up_bias is not None:
+            _tensor(what, "up_bias", up_bias, f32, (N,), dev)
+        self._check(LIB.wdc_op_gated_fp4(self._h, self._fp4(what, "A", A, M, K), self._fp4(what, "W_gate", W_gate, N, K),
+                                         self._fp4(what, "W_up", W_up, N, K), _address(gate_bias), _address(up_bias),
+                                         C.data_ptr(), M, N, K, int(gelu), self._op_stream(stream)), what)
+
+    def op_add_norm(self, x, out, delta=None, gate=None, total=None, weight=None, weight_offset=0.0, shift=None,
+                    center=False, eps=1e-6, rows_per_set=0, scale=None, stream=None):
+        """wdc_op_add_norm: the norm of x + gate * delta (rows of x, delta, total and out may lie apart), modulated by
+        weight + weight_offset and shift, to out: a tensor of the model dtype, float8_e4m3fn with ``scale``
+        [ceil(D/128), M], or an Fp4Matrix.  total: receives the sum.  gate, weight and shift are float32 [sets, D] (or
+        [D]); row m goes by set m // rows_per_set, or all by the only one with rows_per_set=0."""
+        what, (dt, dev, f8, f32, _) = "op_add_norm", self._operand_types()
+        if x.dim() != 2:
+            raise ValueError(f"{what}: x must be [M, D]")
+        M, D = x.shape
+        _sizes(what, M, D)
+        if not 0 <= rows_per_set <= _INT_MAX:
+            raise ValueError(f"{what}: rows_per_set of {rows_per_set}")
+        n = AddNorm(weight_offset=weight_offset, eps=eps, rows_per_set=rows_per_set, center=int(bool(center)))
+        _tensor(what, "x", x, dt, (M, D), dev, row_stride=True)
+        n.x, n.ldx = x.data_ptr(), _row_stride(x)
+        if delta is not None:
+            _tensor(what, "delta", delta, dt, (M, D), dev, row_stride=True)
+            n.delta, n.ldd = delta.data_ptr(), _row_stride(delta)
+        if total is not None:
+            _tensor(what, "total", total, dt, (M, D), dev, row_stride=True)
+            n.total, n.ldt = total.data_ptr(), _row_stride(total)
+        sets = -(-M // rows_per_set) if rows_per_set else 1
+        for name, v in (("gate", gate), ("weight", weight), ("shift", shift)):
+            if v is not None:
+                _tensor(what, name, v, f32, (D,) if v.dim() == 1 and sets == 1 else (sets, D), dev)
+                setattr(n, name, v.data_ptr())
+        if isinstance(out, Fp4Matrix):
+            n.q4 = ctypes.pointer(self._fp4(what, "out", out, M, D))
+        elif out.dtype is f8:
+            _tensor(what, "out", out, f8, (M, D), dev)
+            n.q8 = out.data_ptr()
+            if scale is None:
+                raise ValueError(f"{what}: out in e4m3 needs scale")
+        else:
+            _tensor(what, "out", out, dt, (M, D), dev, row_stride=True)
+            n.out, n.ldo = out.data_ptr(), _row_stride(out)
+        if scale is not None:
+            if not n.q8:
+                raise ValueError(f"{what}: scale goes with out in e4m3")
+            _tensor(what, "scale", scale, f32, (-(-D // 128), M), dev)
+            n.scale = scale.data_ptr()
+        if M == 0:                                         # (empty tensors have no address)
+            return
+        self._check(LIB.wdc_op_add_norm(self._h, n, M, D, self._op_stream(stream)), what)
 
 
 def correlations(x, y):
