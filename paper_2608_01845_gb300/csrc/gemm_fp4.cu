@@ -7,90 +7,320 @@ namespace wdc {
 
 namespace {
 
-constexpr int kTile = 64;
+// ---------------------------------------------------------------------------
+// Few rows of A: W's rows are the MMA's M side (128 of them a tile), BN rows of A its N
+// side, so that a few tokens cost a narrow MMA instead of a mostly empty one and a warp's
+// lanes are neighbouring columns of C.  A tile of BN < 128 is all of A's rows (their scales
+// lie 128 rows a piece, which a tile starts on).  A stage of the ring is 256 of K: the
+// codes' tiles and, for each of its four MMAs, a piece of scales of either side, which one
+// thread copies to the stage's columns of tensor memory before the MMAs.  The sums stay in
+// tensor memory over all of K.
+// A cluster of `split` CTAs shares a tile's K: each sums its part, sends the others their
+// share of the tile's tokens through distributed shared memory and adds what it
+// receives in rank order.
+constexpr int kNarrowThreads = 192;     // TMA producer, MMA issuer, 4 epilogue warps
 
-__device__ __forceinline__ void decode_tile(float (*dst)[kTile + 1], const uint8_t* codes, const uint8_t* scale, int row0,
-                                            int rows, int K, int piece, int pieces) {
-    const int r = threadIdx.x >> 2, part = threadIdx.x & 3, row = row0 + r;
-    uint2 q = make_uint2(0u, 0u);
-    float s = 0.f;
-    if (row < rows) {
-        q = *reinterpret_cast<const uint2*>(codes + ((size_t)row * K + piece * 64 + part * 16) / 2);
-        const uint8_t b = scale[4 * piece_word4(row, piece, pieces) + part];
-        s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3)));
+template <int BN, bool GATED>
+struct Narrow4Cfg {
+    static constexpr int WS = GATED ? 2 : 1;                           // weights
+    static constexpr uint32_t W_BYTES = 128 * 128, A_BYTES = BN * 128, S_BYTES = 4 * kPiece4;
+    static constexpr uint32_t STAGE = WS * W_BYTES + A_BYTES + (WS + 1) * S_BYTES;
+    static constexpr int SCALE_COLS = 16 * (WS + 1);                   // of a stage, in tensor memory
+    static constexpr int ACC_COLS = WS * BN;
+    static constexpr size_t FIXED = 1024 + 512;
+    static constexpr int BY_SMEM = (int)((227 * 1024 - FIXED) / STAGE), BY_TMEM = (512 - ACC_COLS) / SCALE_COLS;
+    static constexpr int STAGES = BY_SMEM < BY_TMEM ? BY_SMEM : BY_TMEM;
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + FIXED;
+    static constexpr uint32_t IDESC = idesc_e2m1(128, BN);
+    static_assert(ACC_COLS * 128 * 4 <= STAGES * STAGE, "partial sums fit the ring");
+    static_assert(STAGE % 1024 == 0 && STAGES * 2 * 8 + 64 <= 512, "tiles are aligned, barriers fit");
+};
+
+template <typename T, int BN, bool GATED>
+__global__ void __launch_bounds__(kNarrowThreads, 1)
+    gemm4_narrow_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmU,
+                        const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmSW,
+                        const __grid_constant__ CUtensorMap tmSU, const __grid_constant__ CUtensorMap tmSA,
+                        const __grid_constant__ Gemm4Args g) {
+    using C = Narrow4Cfg<BN, GATED>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE);
+    uint64_t* empty = full + C::STAGES;
+    uint64_t* done = empty + C::STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int S = g.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
+    const int tile = blockIdx.x / S;
+    const int mt = tile % g.m_tiles, nb = tile / g.m_tiles;            // neighbouring tiles share W
+    const int m0 = mt * BN;
+    const int kb0 = (int)((long long)rank * g.kb / S), kb1 = (int)((long long)(rank + 1) * g.kb / S);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
     }
-    float v[8];
-    e2m1_values(q.x, v);
+    if (warp == 0 && lane == 0) {
+        prefetch_tmap(&tmW);
+        prefetch_tmap(&tmA);
+        prefetch_tmap(&tmSW);
+        prefetch_tmap(&tmSA);
+        if (GATED) {
+            prefetch_tmap(&tmU);
+            prefetch_tmap(&tmSU);
+        }
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    __syncthreads();
+    tc_fence_after();
+    chain_release();
+    chain_wait();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        int stage = 0;
+        uint32_t phase = 0, armed = 0, parity = 0;         // per stage: a copy was issued; its phase
+        for (int kb = kb0; kb < kb1; ++kb) {               // (what lies past K is filled with zeros)
+            if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_flag, g.err)) break;
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&full[stage], C::STAGE);
+                uint8_t* at = smem + stage * C::STAGE;
+                tma_load_2d(at, &tmW, &full[stage], kb * 128, nb * 128);
+                if (GATED) tma_load_2d(at + C::W_BYTES, &tmU, &full[stage], kb * 128, nb * 128);
+                at += C::WS * C::W_BYTES;
+                tma_load_2d(at, &tmA, &full[stage], kb * 128, m0);
+                at += C::A_BYTES;
+                tma_load_3d(at, &tmSW, &full[stage], 0, kb * 4, nb);
+                if (GATED) tma_load_3d(at + C::S_BYTES, &tmSU, &full[stage], 0, kb * 4, nb);
+                tma_load_3d(at + C::WS * C::S_BYTES, &tmSA, &full[stage], 0, kb * 4, mt);
+            }
+            __syncwarp();
+            armed |= 1u << stage;
+            parity = (parity & ~(1u << stage)) | (phase << stage);
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+        // every issued copy has landed before the ring is reused or the CTA exits
+        for (int s = 0; s < C::STAGES; ++s) {
+            if (!((armed >> s) & 1)) continue;
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(&full[s], (parity >> s) & 1) && globaltimer() - t0 < kWaitLimitNs) {
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint32_t base = smem_u32(smem);
+            const uint64_t dw = sdesc_sw128(base), da = sdesc_sw128(base + C::WS * C::W_BYTES);
+            const uint64_t ds = sdesc_rows16(base + C::WS * C::W_BYTES + C::A_BYTES);
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait(&full[stage], phase, abort_flag, g.err)) break;
+                tc_fence_after();
+                // the stage's columns: the MMAs that read them before are done, as its tiles
+                // could not have been loaded again otherwise
+                const uint32_t sc = tmem + (uint32_t)(C::ACC_COLS + stage * C::SCALE_COLS);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dst[r][part * 16 + i] = v[i] * s;
-    e2m1_values(q.y, v);
+                for (int i = 0; i < 4 * (C::WS + 1); ++i)
+                    tc_copy_scales(sc + 4 * i, sdesc_at(ds, stage * C::STAGE + i * kPiece4));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dst[r][part * 16 + 8 + i] = v[i] * s;
+                for (int h = 0; h < C::WS; ++h)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma4(tmem + (uint32_t)(h * BN), sdesc_at(dw, stage * C::STAGE + h * C::W_BYTES + k * 32),
+                                sdesc_at(da, stage * C::STAGE + k * 32), C::IDESC, sc + 16 * h + 4 * k,
+                                sc + 16 * C::WS + 4 * k, kb != kb0 || k != 0);
+                tc_commit(&empty[stage]);
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            }
+            // all MMAs issued by this lane have completed before their sums are read and
+            // tensor memory is freed
+            tc_commit(done);
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(done, 0) && globaltimer() - t0 < kWaitLimitNs) {
+            }
+        }
+        __syncwarp();
+    }
+
+    const int lg = warp & 3;                               // TMEM lane quarter this warp may access
+    const int row = lg * 32 + lane, n = nb * 128 + row;
+    bool ok = true;
+    float rw = 0.f, ru = 0.f, bias = 0.f, up_bias = 0.f, gate = 1.f;
+    if (warp >= 2) {
+        if (n < g.N) {
+            rw = ld_chain(g.rw + n);
+            if (g.bias) bias = ld_chain(g.bias + n);
+            if (g.gate) gate = ld_chain(g.gate + n);
+            if (GATED) {
+                ru = ld_chain(g.ru + n);
+                if (g.up_bias) up_bias = ld_chain(g.up_bias + n);
+            }
+        }
+        ok = mbar_wait_warp(done, 0, abort_flag, g.err) && !*abort_flag;
+        __syncwarp();                                      // (after a wait that gave up nothing else does)
+        tc_fence_after();
+    }
+    const uint32_t lanes = tmem + ((uint32_t)(lg * 32) << 16);
+    const T* res = reinterpret_cast<const T*>(g.res);
+    auto fetch_res = [&](int c) {
+        const int m = m0 + c;
+        return !GATED && g.res && ok && n < g.N && m < g.M ? ld_act<T>(res + (size_t)m * g.N + n) : 0.f;
+    };
+    auto put = [&](int c, float v, float u, float r) {
+        const int m = m0 + c;
+        if (!ok || n >= g.N || m >= g.M) return;
+        const float ra = ld_chain(g.ra + m);
+        v = fmaf(v * ra, rw, bias);
+        if constexpr (GATED) {
+            v = (g.gelu ? gelu_tanh_f(v) : silu_f(v)) * fmaf(u * ra, ru, up_bias);
+        } else {
+            if (g.gelu) v = gelu_tanh_f(v);
+            if (g.res) v = fmaf(gate, v, r);
+        }
+        reinterpret_cast<T*>(g.out)[(size_t)m * g.N + n] = to_act<T>(v);
+    };
+    auto load16 = [&](int c, float (&v)[16]) {             // 16 columns of sums
+        uint32_t p[16];
+        tmem_ld16(lanes + (uint32_t)c, p);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(p[i]);
+    };
+    if (S == 1) {
+        if (warp >= 2) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < BN && m0 + c0 < g.M; c0 += 16) {
+                float v[16], u[16] = {}, r[16];
+                load16(c0, v);
+                if (GATED) load16(BN + c0, u);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) r[c] = fetch_res(c0 + c);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) put(c0 + c, v[c], u[c], r[c]);
+                __syncwarp();
+            }
+        }
+    } else {
+        // partial sums lie as [weights][source][4 tokens of the share][row of W]: a warp
+        // sends one 512-byte run
+        __syncthreads();                                   // this CTA's copies have landed, its MMAs are done
+        cluster_sync_all();                                // every ring is free
+        const int share = BN / 4 / S;                      // groups of 4 tokens a CTA finishes
+        if (warp >= 2) {
+#pragma unroll
+            for (int h = 0; h < C::WS; ++h)
+#pragma unroll 1
+                for (int c0 = 0; c0 < BN; c0 += 16) {
+                    float v[16];
+                    load16(h * BN + c0, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c4 = c0 / 4 + i, to = c4 / share;
+                        const uint32_t off = (uint32_t)(((h * S + rank) * share + c4 - to * share) * 128 + row) * 16u;
+                        st_shared_cluster_v4(mapa_shared(smem_u32(smem) + off, to), __float_as_uint(v[4 * i]),
+                                             __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
+                                             __float_as_uint(v[4 * i + 3]));
+                    }
+                }
+        }
+        cluster_sync_all();
+        if (warp >= 2) {
+            const float4* part = reinterpret_cast<const float4*>(smem);
+            for (int i = 0; i < share; ++i) {
+                const int c = 4 * (rank * share + i);
+                if (m0 + c >= g.M) break;
+                float r[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = fetch_res(c + k);
+                float4 v[2];
+#pragma unroll
+                for (int h = 0; h < C::WS; ++h) {
+                    v[h] = part[(h * S * share + i) * 128 + row];
+                    for (int p = 1; p < S; ++p) {
+                        const float4 x = part[((h * S + p) * share + i) * 128 + row];
+                        v[h].x += x.x; v[h].y += x.y; v[h].z += x.z; v[h].w += x.w;
+                    }
+                }
+                const float4 u = v[C::WS - 1];
+                put(c, v[0].x, u.x, r[0]);
+                put(c + 1, v[0].y, u.y, r[1]);
+                put(c + 2, v[0].z, u.z, r[2]);
+                put(c + 3, v[0].w, u.w, r[3]);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+using NarrowKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                              const CUtensorMap, const Gemm4Args);
+struct Narrow {
+    NarrowKernel kernel;
+    size_t smem;
+};
+template <typename T, bool GATED>
+Narrow narrow(int bn) {
+    switch (bn) {
+        case 16: return {gemm4_narrow_kernel<T, 16, GATED>, Narrow4Cfg<16, GATED>::SMEM};
+        case 32: return {gemm4_narrow_kernel<T, 32, GATED>, Narrow4Cfg<32, GATED>::SMEM};
+        case 64: return {gemm4_narrow_kernel<T, 64, GATED>, Narrow4Cfg<64, GATED>::SMEM};
+        default: return {gemm4_narrow_kernel<T, 128, GATED>, Narrow4Cfg<128, GATED>::SMEM};
+    }
 }
 
 template <typename T, bool GATED>
-__global__ void __launch_bounds__(256) gemm4_plain_kernel(const __grid_constant__ Gemm4Args g) {
-    __shared__ float a[kTile][kTile + 1], w[kTile][kTile + 1];
-    chain_release();
-    chain_wait();
-    const int n_tiles = (g.N + kTile - 1) / kTile;
-    const int m0 = (int)(blockIdx.x / n_tiles) * kTile, n0 = (int)(blockIdx.x % n_tiles) * kTile;
-    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    float acc[2][4][4] = {};
-    for (int p = 0; p < g.pieces; ++p) {
-        decode_tile(a, g.A, g.sa, m0, g.M, g.K, p, g.pieces);
-#pragma unroll
-        for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-            decode_tile(w, h ? g.U : g.W, h ? g.su : g.sw, n0, g.N, g.K, p, g.pieces);
-            __syncthreads();
-            for (int k = 0; k < kTile; ++k) {
-                float x[4], y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[i] = a[ty + 16 * i][k];
-                    y[i] = w[tx + 16 * i][k];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[h][i][j] = fmaf(x[i], y[j], acc[h][i][j]);
-            }
-            __syncthreads();
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m >= g.M || n >= g.N) continue;
-            float v = acc[0][i][j] * g.ra[m] * g.rw[n] + (g.bias ? g.bias[n] : 0.f);
-            T* out = reinterpret_cast<T*>(g.out) + (size_t)m * g.N + n;
-            if constexpr (GATED) {
-                const float u = acc[1][i][j] * g.ra[m] * g.ru[n] + (g.up_bias ? g.up_bias[n] : 0.f);
-                *out = to_act<T>((g.gelu ? gelu_tanh_f(v) : silu_f(v)) * u);
-            } else {
-                if (g.gelu) v = gelu_tanh_f(v);
-                if (g.res) v = fmaf(g.gate ? g.gate[n] : 1.f, v, ld_act<T>(reinterpret_cast<const T*>(g.res) + (size_t)m * g.N + n));
-                *out = to_act<T>(v);
-            }
-        }
-}
-
-wdc_status launch(Ctx* c, const Gemm4Args& g, cudaStream_t s) {
-    const long long tiles = ((long long)(g.M - 1) / kTile + 1) * ((g.N - 1) / kTile + 1);
-    if (tiles > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM: more than 2^31 - 1 thread blocks");
+wdc_status launch_narrow(Ctx* c, Gemm4Args g, int bn, int split, cudaStream_t s) {
+    static PerDevice<bool> attr;
+    attr.get(c->device, [](bool& ok) {
+        ok = true;
+        for (int n : {16, 32, 64, 128}) ok &= allow_smem(narrow<T, GATED>(n).kernel, narrow<T, GATED>(n).smem);
+        return ok;
+    });
+    g.m_tiles = (g.M - 1) / bn + 1;
+    g.n_tiles = (g.N - 1) / 128 + 1;
+    g.kb = (g.K - 1) / kTileK4 + 1;
+    g.split = split;
+    const long long ctas = (long long)g.m_tiles * g.n_tiles * split;
+    if (ctas > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM: more than 2^31 - 1 thread blocks");
+    CUtensorMap tw, tu, ta, tsw, tsu, tsa;
+    std::string why;
+    if (!encode_codes(&tw, g.W, g.N, g.K, 128, &why) || !encode_codes(&tu, GATED ? g.U : g.W, g.N, g.K, 128, &why) ||
+        !encode_codes(&ta, g.A, g.M, g.K, bn, &why) || !encode_scales(&tsw, g.sw, g.N, g.pieces, &why) ||
+        !encode_scales(&tsu, GATED ? g.su : g.sw, g.N, g.pieces, &why) || !encode_scales(&tsa, g.sa, g.M, g.pieces, &why))
+        return fail(c, WDC_ERR_CUDA, why);
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_GEMM, s);
-        const bool bf16 = c->cfg.dtype == WDC_BF16;
-        auto k = g.U ? (bf16 ? gemm4_plain_kernel<__nv_bfloat16, true> : gemm4_plain_kernel<float, true>)
-                     : (bf16 ? gemm4_plain_kernel<__nv_bfloat16, false> : gemm4_plain_kernel<float, false>);
-        launch_kernel(k, dim3((unsigned)tiles), 256, 0, s, 1, g);
+        const Narrow k = narrow<T, GATED>(bn);
+        launch_kernel(k.kernel, dim3((unsigned)ctas), kNarrowThreads, k.smem, s, split, tw, tu, ta, tsw, tsu, tsa, g);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 GEMM launch: ") + cudaGetErrorString(e));
     return WDC_OK;
+}
+
+wdc_status launch(Ctx* c, const Gemm4Args& g, cudaStream_t s) {
+    const int bn = g.M <= 16 ? 16 : (g.M <= 32 ? 32 : (g.M <= 64 ? 64 : 128));
+    const long long tiles = ((long long)(g.M - 1) / bn + 1) * ((g.N - 1) / 128 + 1);
+    int split = 1;
+    while (split < 8 && 2 * split <= bn / 4 && tiles * split * 2 <= c->num_sms && g.K / kTileK4 >= 4 * split) split *= 2;
+    if (c->cfg.dtype == WDC_BF16)
+        return g.U ? launch_narrow<__nv_bfloat16, true>(c, g, bn, split, s) : launch_narrow<__nv_bfloat16, false>(c, g, bn, split, s);
+    return g.U ? launch_narrow<float, true>(c, g, bn, split, s) : launch_narrow<float, false>(c, g, bn, split, s);
 }
 
 // What both products check; WDC_OK with *none: there is nothing to do.

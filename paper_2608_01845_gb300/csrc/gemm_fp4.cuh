@@ -17,7 +17,23 @@ struct Gemm4Args {
     void* out;
     int gelu;
     unsigned* err;
+    int m_tiles, n_tiles;
+    int kb;                             // tiles of K (kTileK4)
+    int split, stages;                  // narrow kernel: CTAs a tile, tiles of its ring
 };
+
+constexpr int kTileK4 = 256;            // of K: 128 bytes of codes, a row of the swizzled tiles, and four pieces of scales
+
+// Tensor maps of codes [rows][K / 2] in boxes of `box` rows by 128 bytes, and of scales in
+// boxes of four pieces.
+inline bool encode_codes(CUtensorMap* m, const void* codes, int rows, int K, int box, std::string* why) {
+    return encode_tmap_2d(m, codes, (uint64_t)K / 2, (uint64_t)rows, (uint64_t)K / 2, kTileK4 / 2, box, why,
+                          CU_TENSOR_MAP_DATA_TYPE_UINT8);
+}
+inline bool encode_scales(CUtensorMap* m, const void* scale, int rows, int pieces, std::string* why) {
+    return encode_tmap_3d(m, scale, kPiece4 / 2, pieces, (uint64_t)(rows - 1) / 128 + 1, kPiece4, (uint64_t)pieces * kPiece4,
+                          kPiece4 / 2, 4, 1, why, false, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
 
 __device__ __forceinline__ float silu_f(float x) { return __fdividef(x, 1.0f + __expf(-x)); }
 

@@ -175,6 +175,14 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorM
         ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar_cluster, int x, int y,
+                                                 int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
 
 // Address of the same shared-memory variable in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t mapa_shared(uint32_t local_addr, uint32_t rank) {
@@ -291,6 +299,24 @@ __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
            | ((uint32_t)(M >> 4) << 24);   // M / 16
 }
 
+// Instruction descriptor of kind::mxf4nvf4 (block-scaled e2m1 A and B, K-major) with
+// e4m3 scales, fp32 accumulation.
+__host__ __device__ constexpr uint32_t idesc_e2m1(int M, int N) {
+    return (1u << 7)                       // A format: e2m1
+           | (1u << 10)                    // B format: e2m1
+           | ((uint32_t)(N >> 3) << 17)    // N / 8 (scale format 0: unsigned e4m3)
+           | ((uint32_t)(M >> 4) << 24);   // M / 16
+}
+// Shared-memory descriptor of rows of 16 bytes, one behind the other (no swizzle:
+// core matrices of 8 rows, 128 bytes apart), for tc_copy_scales.
+__device__ __forceinline__ uint64_t sdesc_rows16(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);          // start address
+    d |= (uint64_t)(128u >> 4) << 32;                   // stride byte offset: 8 rows
+    d |= (uint64_t)1 << 46;                             // descriptor version
+    return d;
+}
+
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_result, uint32_t ncols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_result)),
                  "r"(ncols)
@@ -323,6 +349,34 @@ __device__ __forceinline__ void tc_mma8(uint32_t d_tmem, uint64_t adesc, uint64_
         " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
         "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
         : "memory");
+}
+// D[tmem] (+)= (A scale_A)[smem] * (B scale_B)[smem]^T for e2m1 operands (64 of K an
+// instruction), a scale for 16 of K: scales[tmem], four columns for 128 rows, column c
+// lane l's word being the four scales of row 32 c + l.
+__device__ __forceinline__ void tc_mma4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t a_scale,
+                                        uint32_t b_scale, uint32_t accum) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accum)
+        : "memory");
+}
+__device__ __forceinline__ void tc_mma4_2(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t a_scale,
+                                          uint32_t b_scale, uint32_t accum) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accum)
+        : "memory");
+}
+// 32 rows of 16 bytes of shared memory into four columns of tensor memory, the same in
+// each quarter of its lanes.  Done before MMAs that the thread issues after it.
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t sdesc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+// In both CTAs of the pair, each from its own shared memory.
+__device__ __forceinline__ void tc_copy_scales2(uint32_t taddr, uint64_t sdesc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
 // D[tmem] (+)= A[tmem] * B[smem]^T
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
