@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libwdc.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "step_kernels.cu", "dit.cu", "gemm_tc.cu", "attn_tc.cu", "graph_rollout.cu", "quant_fp8.cu",
            "gemm_fp8.cu", "gemm_fp8_pair.cu", "qk_norm_rope.cu", "attn_paged.cu", "quant_fp4.cu",
-           "gemm_fp4.cu", "add_norm.cu"]
+           "gemm_fp4.cu", "gemm_fp4_pair.cu", "add_norm.cu"]
 
 
 def nvcc():

@@ -314,6 +314,7 @@ wdc_status launch_narrow(Ctx* c, Gemm4Args g, int bn, int split, cudaStream_t s)
 }
 
 wdc_status launch(Ctx* c, const Gemm4Args& g, cudaStream_t s) {
+    if (c->num_sms >= 2 && g.M > 256) return launch_gemm4_pair(c, g, s);
     const int bn = g.M <= 16 ? 16 : (g.M <= 32 ? 32 : (g.M <= 64 ? 64 : 128));
     const long long tiles = ((long long)(g.M - 1) / bn + 1) * ((g.N - 1) / 128 + 1);
     int split = 1;

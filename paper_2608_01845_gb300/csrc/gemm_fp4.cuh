@@ -19,7 +19,8 @@ struct Gemm4Args {
     unsigned* err;
     int m_tiles, n_tiles;
     int kb;                             // tiles of K (kTileK4)
-    int split, stages;                  // narrow kernel: CTAs a tile, tiles of its ring
+    int split;                          // narrow kernel: CTAs a tile
+    int group_n;                        // pair kernel: column blocks of a raster group
 };
 
 constexpr int kTileK4 = 256;            // of K: 128 bytes of codes, a row of the swizzled tiles, and four pieces of scales
@@ -36,5 +37,8 @@ inline bool encode_scales(CUtensorMap* m, const void* scale, int rows, int piece
 }
 
 __device__ __forceinline__ float silu_f(float x) { return __fdividef(x, 1.0f + __expf(-x)); }
+
+// gemm_fp4_pair.cu
+wdc_status launch_gemm4_pair(Ctx* c, const Gemm4Args& g, cudaStream_t s);
 
 }  // namespace wdc
