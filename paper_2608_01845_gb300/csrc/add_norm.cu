@@ -26,168 +26,214 @@ struct AddNormArgs {
 };
 
 constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
-constexpr int kMaxThreads = 512;
+constexpr int kMaxThreads = 512;                   // of a row, and of a block
+constexpr int kMaxRows = 8;                        // of a block at a time
 constexpr int kMaxD = 8 * kHeld * kMaxThreads;
 
-struct Sum {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
-};
-struct Max {
-    __device__ __forceinline__ float operator()(float a, float b) const { return max_nan(a, b); }
-};
-// Over the blockDim.x threads of a row; every thread of the block calls it.  `part` is
-// not in use by an earlier call any more.
-template <class Op>
-__device__ __forceinline__ float over_row(float a, float (*part)[16], Op op) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a = op(a, __shfl_xor_sync(0xffffffffu, a, o));
-    if (blockDim.x == 32) return a;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.y][threadIdx.x >> 5] = a;
-    __syncthreads();
-    a = part[threadIdx.y][0];
-    for (int i = 1; i < (int)(blockDim.x >> 5); ++i) a = op(a, part[threadIdx.y][i]);
-    return a;
-}
-
+// Each threadIdx.y takes rows a grid apart, with all blockDim.x threads of a row and V
+// pieces of 8 columns a thread; the next row's loads are under way while one is worked on.
+// The warps of a row meet once for its statistics: each brings the mean of its own values
+// and the squares around it, which join exactly as those of the whole row would be formed
+// (the squares around the row's mean are those plus n (mean - row's mean)^2 a warp).
 template <typename T, int OUT, int V>
 __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
-    __shared__ float part[3][8][16];
+    __shared__ float2 stat[2][kMaxRows][kMaxThreads / 32];
+    __shared__ float tops[2][kMaxRows][kMaxThreads / 32];
     chain_release();
     chain_wait();
-    const int m = (int)(blockIdx.x * blockDim.y + threadIdx.y);
-    const bool live = m < a.M;
-    const size_t set = live && a.rows_per_set ? (size_t)(m / a.rows_per_set) * a.D : 0;
+    const int y = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const unsigned step = gridDim.x * blockDim.y, M = a.M; // (unsigned: a row and a step stay below 2^32)
+    // (e2m1: the rows behind M of the last 128 too, whose scales are zero)
+    const unsigned rows = OUT == kE2m1 ? (M + 127) / 128 * 128 : M;
     auto column = [&](int u) { return (u * (int)blockDim.x + (int)threadIdx.x) * 8; };
-    float v[V][8];
+    auto meet = [&]() {
+        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(y + 1), "r"(blockDim.x) : "memory");
+    };
+    auto count = [&](int w) {                              // a warp's columns
+        int n = 0;
 #pragma unroll
-    for (int u = 0; u < V; ++u) {
-        const int k = column(u);
-        if (live && k < a.D) {
-            load8(reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx + k, v[u]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-        }
-    }
-    if (a.delta) {
-        float d[V][8];
+        for (int u = 0; u < V; ++u) n += max(0, min(256, a.D - (u * (int)blockDim.x + w * 32) * 8));
+        return (float)n;
+    };
+    const float n = count(warp), by_n = n > 0.f ? 1.0f / n : 0.f;
+    Raw8<T> xr[V], dr[V];
+    auto load = [&](unsigned m) {
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (live && column(u) < a.D) load8(reinterpret_cast<const T*>(a.delta) + (size_t)m * a.ldd + column(u), d[u]);
+            if (m < M && column(u) < a.D) {
+                load_raw(reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx + column(u), xr[u]);
+                if (a.delta) load_raw(reinterpret_cast<const T*>(a.delta) + (size_t)m * a.ldd + column(u), dr[u]);
+            }
+    };
+    unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
+    int parity = 0;
+    load(m);
+    for (; m < rows; m += step, parity ^= 1) {
+        const bool live = m < M;
+        const size_t set = live && a.rows_per_set ? (size_t)(m / (unsigned)a.rows_per_set) * a.D : 0;
+        float v[V][8];
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             const int k = column(u);
-            if (!live || k >= a.D) continue;
-            float g[8];
-            if (a.gate) {
-                load8(a.gate + set + k, g);
+            if (live && k < a.D) {
+                widen8(xr[u], v[u]);
+                if (a.delta) {
+                    float d[8];
+                    widen8(dr[u], d);
+                    if (a.gate) {
+                        float g[8];
+                        load8(a.gate + set + k, g);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[u][i] = fmaf(g[i], d[i], v[u][i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[u][i] += d[i];
+                    }
+                }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = 1.f;
+                for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = fmaf(g[i], d[u][i], v[u][i]);
         }
-    }
-    if (a.total) {
+        load(m + step);
+        if (a.total) {
 #pragma unroll
-        for (int u = 0; u < V; ++u)
-            if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.total) + (size_t)m * a.ldt + column(u), v[u]);
-    }
-    if (a.center) {
-        float s = 0.f;
+            for (int u = 0; u < V; ++u)
+                if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.total) + (size_t)m * a.ldt + column(u), v[u]);
+        }
+        float mean = 0.f, ss = 0.f;
+        if (a.center) {
 #pragma unroll
-        for (int u = 0; u < V; ++u)
+            for (int u = 0; u < V; ++u)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[u][i];
-        const float mean = over_row(s, part[0], Sum()) * a.by;
+                for (int i = 0; i < 8; ++i) mean += v[u][i];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+            mean *= by_n;
+        }
 #pragma unroll
         for (int u = 0; u < V; ++u)
             if (column(u) < a.D) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] -= mean;
+                for (int i = 0; i < 8; ++i) ss = fmaf(v[u][i] - mean, v[u][i] - mean, ss);
             }
-    }
-    float ss = 0.f;
 #pragma unroll
-    for (int u = 0; u < V; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(v[u][i], v[u][i], ss);
-    const float inv = rsqrtf(over_row(ss, part[1], Sum()) * a.by + a.eps);
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-        const int k = column(u);
-        if (!live || k >= a.D) continue;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] *= inv;
-        if (a.weight) {
-            float w[8];
-            load8(a.weight + set + k, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] *= w[i] + a.offset;
+        for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        if (warps > 1) {
+            if (lane == 0) stat[parity][y][warp] = make_float2(mean, ss);
+            meet();
+            ss = 0.f;
+            float all = 0.f;
+            if (a.center) {
+                for (int w = 0; w < warps; ++w) all = fmaf(stat[parity][y][w].x, count(w), all);
+                all *= a.by;
+            }
+            for (int w = 0; w < warps; ++w) {
+                const float2 s = stat[parity][y][w];
+                ss += a.center ? fmaf(count(w) * (s.x - all), s.x - all, s.y) : s.y;
+            }
+            mean = all;
         }
-        if (a.shift) {
-            float w[8];
-            load8(a.shift + set + k, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] += w[i];
-        }
-    }
-    if constexpr (OUT == kSame) {
-#pragma unroll
-        for (int u = 0; u < V; ++u)
-            if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.out) + (size_t)m * a.ldo + column(u), v[u]);
-    } else if constexpr (OUT == kE4m3) {
+        const float inv = rsqrtf(ss * a.by + a.eps);
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             const int k = column(u);
-            float top = absmax8(v[u]);
+            if (!live || k >= a.D) continue;
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float s = top / kE4m3Max;
-            if (live && k < a.D) {
-                store8(reinterpret_cast<uint8_t*>(a.out) + (size_t)m * a.D + k, v[u], s);
-                if (k % 128 == 0) a.scale[(size_t)(k / 128) * a.M + m] = s;
+            for (int i = 0; i < 8; ++i) v[u][i] = (v[u][i] - mean) * inv;
+            if (a.weight) {
+                float w[8];
+                load8(a.weight + set + k, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] *= w[i] + a.offset;
+            }
+            if (a.shift) {
+                float w[8];
+                load8(a.shift + set + k, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] += w[i];
             }
         }
-    } else {
-        float top = 0.f;
+        if constexpr (OUT == kSame) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
-        const float row = row_scale4(over_row(top, part[2], Max())), six = 6.f * row;
-        const int pieces = a.D / kPieceCols4;
+            for (int u = 0; u < V; ++u)
+                if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.out) + (size_t)m * a.ldo + column(u), v[u]);
+        } else if constexpr (OUT == kE4m3) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-            const int k = column(u);
-            uint32_t* codes =
-                live && k < a.D ? reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(a.out) + ((size_t)m * a.D + k) / 2) : nullptr;
-            uint32_t* word = k < a.D && k % kPieceCols4 == 0 ? a.words + piece_word4(m, k / kPieceCols4, pieces) : nullptr;
-            store_fp4(v[u], row, six, codes, word);
-            if (!live && word) *word = 0u;
+            for (int u = 0; u < V; ++u) {
+                const int k = column(u);
+                float top = absmax8(v[u]);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float s = top / kE4m3Max;
+                if (live && k < a.D) {
+                    store8(reinterpret_cast<uint8_t*>(a.out) + (size_t)m * a.D + k, v[u], s);
+                    if (k % 128 == 0) a.scale[(size_t)(k / 128) * a.M + m] = s;
+                }
+            }
+        } else {
+            float top = 0.f;
+#pragma unroll
+            for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (warps > 1) {
+                if (lane == 0) tops[parity][y][warp] = top;
+                meet();
+                for (int w = 0; w < warps; ++w) top = max_nan(top, tops[parity][y][w]);
+            }
+            const float row = row_scale4(top), six = 6.f * row;
+            const int pieces = a.D / kPieceCols4;
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                const int k = column(u);
+                uint32_t* codes = live && k < a.D ? reinterpret_cast<uint32_t*>(a.out) + ((size_t)m * a.D + k) / 8 : nullptr;
+                uint32_t* word = k < a.D && k % kPieceCols4 == 0 ? a.words + piece_word4((int)m, k / kPieceCols4, pieces) : nullptr;
+                store_fp4(v[u], row, six, codes, word);
+                if (!live && word) *word = 0u;
+            }
+            if (live && threadIdx.x == 0) a.row_scale[m] = row;
         }
-        if (live && threadIdx.x == 0) a.row_scale[m] = row;
     }
+}
+
+// Blocks of a kernel that the device holds at a time.
+template <class K>
+int resident(const Ctx* c, K kernel, int threads) {
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 1;
+    }
+    return n * c->num_sms;
+}
+
+template <typename T, int OUT, int V>
+wdc_status launch(Ctx* c, const AddNormArgs& a, int warps, cudaStream_t s) {
+    const int per = warps >= 8 ? 1 : (8 / warps < kMaxRows ? 8 / warps : kMaxRows);
+    const long long rows = OUT == kE2m1 ? ((long long)(a.M - 1) / 128 + 1) * 128 : a.M;
+    const long long blocks = (rows + per - 1) / per;
+    static PerDevice<int> held[kMaxThreads / 32 + 1];
+    const int most = held[warps].get(c->device, [&](int& n) {
+        n = resident(c, add_norm_kernel<T, OUT, V>, 32 * warps * per);
+        return true;
+    });
+    {
+        OverlapScope ov(c, s);
+        LaunchScope ls(c, WDC_K_NORM, s);
+        launch_kernel(add_norm_kernel<T, OUT, V>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(32 * warps, per), 0, s, 1, a);
+    }
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("residual norm: ") + cudaGetErrorString(e));
+    return WDC_OK;
 }
 
 template <typename T, int OUT>
 wdc_status launch(Ctx* c, const AddNormArgs& a, cudaStream_t s) {
     const int eights = a.D / 8;
-    const int v = eights <= 32 ? 1 : (eights <= 128 ? 2 : kHeld);
+    const int v = eights <= 32 ? 1 : (eights <= 2 * kMaxThreads ? 2 : kHeld);
     const int warps = (eights + 32 * v - 1) / (32 * v);
-    const int per = warps >= 8 ? 1 : (warps >= 4 ? 2 : (warps >= 2 ? 4 : 8));
-    // (e2m1: the rows behind M of the last 128 too, whose scales are zero)
-    const long long rows = OUT == kE2m1 ? ((long long)(a.M - 1) / 128 + 1) * 128 : a.M;
-    const dim3 block(32 * warps, per), grid((unsigned)((rows + per - 1) / per));
-    {
-        OverlapScope ov(c, s);
-        LaunchScope ls(c, WDC_K_NORM, s);
-        if (v == 1) launch_kernel(add_norm_kernel<T, OUT, 1>, grid, block, 0, s, 1, a);
-        else if (v == 2) launch_kernel(add_norm_kernel<T, OUT, 2>, grid, block, 0, s, 1, a);
-        else launch_kernel(add_norm_kernel<T, OUT, kHeld>, grid, block, 0, s, 1, a);
-    }
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("residual norm: ") + cudaGetErrorString(e));
-    return WDC_OK;
+    return v == 1 ? launch<T, OUT, 1>(c, a, warps, s) : (v == 2 ? launch<T, OUT, 2>(c, a, warps, s) : launch<T, OUT, kHeld>(c, a, warps, s));
 }
 
 template <typename T>

@@ -21,59 +21,74 @@ struct Quant4Args {
     int M, K, pieces;                  // pieces: K / 64
 };
 
-// The largest magnitude of a row over its W warps (blockDim.x threads), NaN kept.
-// `part`: [rows of the block][32]; every thread of the block calls it.
-__device__ __forceinline__ float row_max(float a, float (*part)[32]) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
-    if (blockDim.x == 32) return a;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.y][threadIdx.x >> 5] = a;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    a = lane < (int)(blockDim.x >> 5) ? part[threadIdx.y][lane] : 0.f;
+constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
+constexpr int kMaxThreads = 512;                   // of a row, and of a block
+constexpr int kMaxRows = 8;                        // of a block at a time
+
+__device__ __forceinline__ float warp_max(float a) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
     return a;
 }
 
-// A row of blockDim.x threads, V pieces of 8 columns a thread; rows past M (of the
-// last 128) get scales of zero.
+// Each threadIdx.y takes rows a grid apart, with all blockDim.x threads of a row and V
+// pieces of 8 columns a thread; the next row's loads are under way while one is worked on.
+// Rows past M (of the last 128) get scales of zero.
 template <typename T, int V>
-__global__ void __launch_bounds__(512) quantize4_kernel(const __grid_constant__ Quant4Args a) {
-    __shared__ float part[16][32];
+__global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_constant__ Quant4Args a) {
+    __shared__ float tops[2][kMaxRows][kMaxThreads / 32];
     chain_release();
     chain_wait();
-    const int m = (int)(blockIdx.x * blockDim.y + threadIdx.y);
-    const T* x = reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx;
-    float v[V][8], top = 0.f;
+    const int y = threadIdx.y, warps = blockDim.x >> 5;
+    const unsigned step = gridDim.x * blockDim.y, M = a.M, rows = (M + 127) / 128 * 128;   // (a row and a step: below 2^32)
+    auto column = [&](int u) { return (u * (int)blockDim.x + (int)threadIdx.x) * 8; };
+    Raw8<T> raw[V];
+    auto load = [&](unsigned m) {
 #pragma unroll
-    for (int u = 0; u < V; ++u) {
-        const int k = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
-        if (m < a.M && k < a.K) {
-            load8(x + k, v[u]);
-        } else {
+        for (int u = 0; u < V; ++u)
+            if (m < M && column(u) < a.K) load_raw(reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx + column(u), raw[u]);
+    };
+    unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
+    int parity = 0;
+    load(m);
+    for (; m < rows; m += step, parity ^= 1) {
+        const bool live = m < M;
+        float v[V][8], top = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+        for (int u = 0; u < V; ++u) {
+            if (live && column(u) < a.K) {
+                widen8(raw[u], v[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+            }
         }
-    }
+        load(m + step);
 #pragma unroll
-    for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
-    const float row = row_scale4(row_max(top, part)), six = 6.f * row;
+        for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
+        top = warp_max(top);
+        if (warps > 1) {
+            if ((threadIdx.x & 31) == 0) tops[parity][y][threadIdx.x >> 5] = top;
+            asm volatile("bar.sync %0, %1;" ::"r"(y + 1), "r"(blockDim.x) : "memory");
+            for (int w = 0; w < warps; ++w) top = max_nan(top, tops[parity][y][w]);
+        }
+        const float row = row_scale4(top), six = 6.f * row;
 #pragma unroll
-    for (int u = 0; u < V; ++u) {
-        const int k = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
-        uint32_t* codes = m < a.M && k < a.K ? reinterpret_cast<uint32_t*>(a.codes + ((size_t)m * a.K + k) / 2) : nullptr;
-        uint32_t* word = k < a.K && k % kPieceCols4 == 0 ? a.scale + piece_word4(m, k / kPieceCols4, a.pieces) : nullptr;
-        store_fp4(v[u], row, six, codes, word);
-        if (m >= a.M && word) *word = 0u;
+        for (int u = 0; u < V; ++u) {
+            const int k = column(u);
+            uint32_t* codes = live && k < a.K ? reinterpret_cast<uint32_t*>(a.codes) + ((size_t)m * a.K + k) / 8 : nullptr;
+            uint32_t* word = k < a.K && k % kPieceCols4 == 0 ? a.scale + piece_word4((int)m, k / kPieceCols4, a.pieces) : nullptr;
+            store_fp4(v[u], row, six, codes, word);
+            if (!live && word) *word = 0u;
+        }
+        if (live && threadIdx.x == 0) a.row_scale[m] = row;
     }
-    if (m < a.M && threadIdx.x == 0) a.row_scale[m] = row;
 }
 
 // Rows wider than a block's registers: read twice, the second time from L2.
 template <typename T>
 __global__ void __launch_bounds__(512) quantize4_wide_kernel(const __grid_constant__ Quant4Args a) {
-    __shared__ float part[1][32];
+    __shared__ float tops[16];
     chain_release();
     chain_wait();
     const int m = (int)blockIdx.x;
@@ -87,7 +102,11 @@ __global__ void __launch_bounds__(512) quantize4_wide_kernel(const __grid_consta
         load8(x + k, v);
         top = max_nan(top, absmax8(v));
     }
-    const float row = row_scale4(row_max(top, part)), six = 6.f * row;
+    top = warp_max(top);
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+    for (int w = 0; w < 16; ++w) top = max_nan(top, tops[w]);
+    const float row = row_scale4(top), six = 6.f * row;
     for (long long k0 = 0; k0 < a.K; k0 += blockDim.x * 8) {        // (whole warps: the lanes trade scales)
         const long long k = k0 + threadIdx.x * 8;
         if (k < a.K) {
@@ -104,48 +123,68 @@ __global__ void __launch_bounds__(512) quantize4_wide_kernel(const __grid_consta
     if (threadIdx.x == 0) a.row_scale[m] = row;
 }
 
-// Eight columns a thread.
+// Eight columns a thread of kBackRows rows, blockDim.y apart.
+constexpr int kBackRows = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) dequantize4_kernel(const uint8_t* codes, const uint8_t* scale, const float* row_scale,
-                                                          T* x, long long ldx, int M, int K, int pieces) {
+__global__ void __launch_bounds__(256) dequantize4_kernel(const uint32_t* codes, const uint8_t* scale, const float* row_scale,
+                                                          T* x, long long ldx, int M, int K, int pieces, int segments) {
     chain_release();
     chain_wait();
-    const int per = K / 8;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long row = i / per;
-    if (row >= M) return;
-    const int m = (int)row, k = (int)(i - row * per) * 8;
-    const uint32_t q = *reinterpret_cast<const uint32_t*>(codes + ((size_t)m * K + k) / 2);
-    const uint8_t s = scale[4 * piece_word4(m, k / kPieceCols4, pieces) + (k / 16) % 4];
-    const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s, __NV_E4M3))) * row_scale[m];
-    float v[8];
-    e2m1_values(q, v);
+    const int k = ((int)(blockIdx.x % segments) * (int)blockDim.x + (int)threadIdx.x) * 8;
+    if (k >= K) return;
+    const unsigned m0 = blockIdx.x / segments * (blockDim.y * kBackRows) + threadIdx.y;
+    uint32_t q[kBackRows];
+    uint8_t s[kBackRows];
+    float r[kBackRows];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= step;
-    put8(x + (size_t)m * ldx + k, v);
+    for (int i = 0; i < kBackRows; ++i) {
+        const unsigned m = m0 + i * blockDim.y;
+        if (m >= (unsigned)M) continue;
+        q[i] = codes[((size_t)m * K + k) / 8];
+        s[i] = scale[4 * piece_word4((int)m, k / kPieceCols4, pieces) + (k / 16) % 4];
+        r[i] = row_scale[m];
+    }
+#pragma unroll
+    for (int i = 0; i < kBackRows; ++i) {
+        const unsigned m = m0 + i * blockDim.y;
+        if (m >= (unsigned)M) continue;
+        const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s[i], __NV_E4M3))) * r[i];
+        float v[8];
+        e2m1_values(q[i], v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= step;
+        put8(x + (size_t)m * ldx + k, v);
+    }
 }
 
-constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
-constexpr int kMaxThreads = 512;
+template <typename T, int V>
+void launch_held(Ctx* c, const Quant4Args& a, int warps, cudaStream_t s) {
+    const int per = warps >= 8 ? 1 : (8 / warps < kMaxRows ? 8 / warps : kMaxRows);
+    const long long rows = ((long long)(a.M - 1) / 128 + 1) * 128, blocks = (rows + per - 1) / per;
+    static PerDevice<int> held[kMaxThreads / 32 + 1];
+    const int most = held[warps].get(c->device, [&](int& n) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, quantize4_kernel<T, V>, 32 * warps * per, 0) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            n = 1;
+        }
+        n *= c->num_sms;
+        return true;
+    });
+    launch_kernel(quantize4_kernel<T, V>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(32 * warps, per), 0, s, 1, a);
+}
 
 template <typename T>
 wdc_status launch(Ctx* c, const Quant4Args& a, cudaStream_t s) {
-    const long long rows = ((long long)(a.M - 1) / 128 + 1) * 128;      // those behind M: scales of zero
     const int eights = a.K / 8;
+    const int v = eights <= 32 ? 1 : (eights <= 2 * kMaxThreads ? 2 : kHeld), warps = (eights + 32 * v - 1) / (32 * v);
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_OTHER, s);
-        if (eights > kHeld * kMaxThreads) {
-            launch_kernel(quantize4_wide_kernel<T>, dim3((unsigned)rows), 512, 0, s, 1, a);
-        } else {
-            const int v = eights <= 32 ? 1 : (eights <= 128 ? 2 : kHeld);
-            const int warps = (eights + 32 * v - 1) / (32 * v);
-            const int per = warps >= 8 ? 1 : (warps >= 4 ? 2 : (warps >= 2 ? 4 : 8));
-            const dim3 block(32 * warps, per), grid((unsigned)(rows / per));
-            if (v == 1) launch_kernel(quantize4_kernel<T, 1>, grid, block, 0, s, 1, a);
-            else if (v == 2) launch_kernel(quantize4_kernel<T, 2>, grid, block, 0, s, 1, a);
-            else launch_kernel(quantize4_kernel<T, kHeld>, grid, block, 0, s, 1, a);
-        }
+        if (eights > kHeld * kMaxThreads)                  // (a block a row, those behind M of the last 128 too)
+            launch_kernel(quantize4_wide_kernel<T>, dim3(((unsigned)a.M + 127) / 128 * 128), 512, 0, s, 1, a);
+        else if (v == 1) launch_held<T, 1>(c, a, warps, s);
+        else if (v == 2) launch_held<T, 2>(c, a, warps, s);
+        else launch_held<T, kHeld>(c, a, warps, s);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 quantize: ") + cudaGetErrorString(e));
@@ -154,13 +193,17 @@ wdc_status launch(Ctx* c, const Quant4Args& a, cudaStream_t s) {
 
 template <typename T>
 wdc_status launch_back(Ctx* c, const wdc_fp4& q, T* x, long long ldx, int M, int K, cudaStream_t s) {
-    const long long blocks = ((long long)M * (K / 8) + 255) / 256;
+    const int eights = K / 8;
+    int tx = 8;
+    while (tx < eights && tx < 256) tx *= 2;
+    const int ty = 256 / tx, segments = (eights + tx - 1) / tx;
+    const long long blocks = ((long long)(M - 1) / (ty * kBackRows) + 1) * segments;
     if (blocks > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 dequantize: more than 2^31 - 1 thread blocks");
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_OTHER, s);
-        launch_kernel(dequantize4_kernel<T>, dim3((unsigned)blocks), 256, 0, s, 1, (const uint8_t*)q.codes,
-                      (const uint8_t*)q.scale, (const float*)q.row_scale, x, ldx, M, K, K / kPieceCols4);
+        launch_kernel(dequantize4_kernel<T>, dim3((unsigned)blocks), dim3(tx, ty), 0, s, 1, (const uint32_t*)q.codes,
+                      (const uint8_t*)q.scale, (const float*)q.row_scale, x, ldx, M, K, K / kPieceCols4, segments);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 dequantize: ") + cudaGetErrorString(e));
