@@ -26,29 +26,29 @@ struct AddNormArgs {
 };
 
 constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
-constexpr int kMaxThreads = 512;                   // of a row, and of a block
-constexpr int kMaxRows = 8;                        // of a block at a time
+constexpr int kMaxThreads = 512;                   // of a row
+constexpr int kRowsAtOnce = 8;                     // of a block whose rows have a warp each
 constexpr int kMaxD = 8 * kHeld * kMaxThreads;
 
-// Each threadIdx.y takes rows a grid apart, with all blockDim.x threads of a row and V
-// pieces of 8 columns a thread; the next row's loads are under way while one is worked on.
-// The warps of a row meet once for its statistics: each brings the mean of its own values
-// and the squares around it, which join exactly as those of the whole row would be formed
-// (the squares around the row's mean are those plus n (mean - row's mean)^2 a warp).
+// A block takes rows a grid apart: one at a time with all its threads, or (blockDim.y ==
+// kRowsAtOnce) one a warp; a thread has V pieces of 8 columns, and the next row's loads
+// are under way while one is worked on.  The warps of a row meet once for its
+// statistics: each brings the mean of its own values and the squares around it, which join
+// exactly as those of the whole row would be formed (the squares around the row's mean
+// are those plus n (mean - row's mean)^2 a warp).
 template <typename T, int OUT, int V>
 __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
-    __shared__ float2 stat[2][kMaxRows][kMaxThreads / 32];
-    __shared__ float tops[2][kMaxRows][kMaxThreads / 32];
+    __shared__ float2 stat[2][kMaxThreads / 32];
+    __shared__ float tops[2][kMaxThreads / 32];
     chain_release();
     chain_wait();
-    const int y = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const unsigned step = gridDim.x * blockDim.y, M = a.M; // (unsigned: a row and a step stay below 2^32)
     // (e2m1: the rows behind M of the last 128 too, whose scales are zero)
     const unsigned rows = OUT == kE2m1 ? (M + 127) / 128 * 128 : M;
-    auto column = [&](int u) { return (u * (int)blockDim.x + (int)threadIdx.x) * 8; };
-    auto meet = [&]() {
-        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(y + 1), "r"(blockDim.x) : "memory");
-    };
+    int col[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) col[u] = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
     auto count = [&](int w) {                              // a warp's columns
         int n = 0;
 #pragma unroll
@@ -56,13 +56,18 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
         return (float)n;
     };
     const float n = count(warp), by_n = n > 0.f ? 1.0f / n : 0.f;
+    const int other = lane & 15;                           // the warp whose statistics this lane joins
+    const float n_other = other < warps ? count(other) : 0.f;
     Raw8<T> xr[V], dr[V];
     auto load = [&](unsigned m) {
+        if (m >= M) return;
+        const T* x = reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx;
+        const T* d = reinterpret_cast<const T*>(a.delta) + (size_t)m * a.ldd;
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (m < M && column(u) < a.D) {
-                load_raw(reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx + column(u), xr[u]);
-                if (a.delta) load_raw(reinterpret_cast<const T*>(a.delta) + (size_t)m * a.ldd + column(u), dr[u]);
+            if (col[u] < a.D) {
+                load_raw(x + col[u], xr[u]);
+                if (a.delta) load_raw(d + col[u], dr[u]);
             }
     };
     unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
@@ -74,21 +79,19 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
         float v[V][8];
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            const int k = column(u);
-            if (live && k < a.D) {
+            if (live && col[u] < a.D) {
                 widen8(xr[u], v[u]);
                 if (a.delta) {
-                    float d[8];
+                    float d[8], g[8];
                     widen8(dr[u], d);
                     if (a.gate) {
-                        float g[8];
-                        load8(a.gate + set + k, g);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[u][i] = fmaf(g[i], d[i], v[u][i]);
+                        load8(a.gate + set + col[u], g);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[u][i] += d[i];
+                        for (int i = 0; i < 8; ++i) g[i] = 1.f;
                     }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[u][i] = fmaf(g[i], d[i], v[u][i]);
                 }
             } else {
 #pragma unroll
@@ -96,10 +99,11 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
             }
         }
         load(m + step);
-        if (a.total) {
+        if (a.total && live) {
+            T* total = reinterpret_cast<T*>(a.total) + (size_t)m * a.ldt;
 #pragma unroll
             for (int u = 0; u < V; ++u)
-                if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.total) + (size_t)m * a.ldt + column(u), v[u]);
+                if (col[u] < a.D) put8(total + col[u], v[u]);
         }
         float mean = 0.f, ss = 0.f;
         if (a.center) {
@@ -113,55 +117,61 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
         }
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (column(u) < a.D) {
+            if (col[u] < a.D) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = fmaf(v[u][i] - mean, v[u][i] - mean, ss);
             }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         if (warps > 1) {
-            if (lane == 0) stat[parity][y][warp] = make_float2(mean, ss);
-            meet();
-            ss = 0.f;
-            float all = 0.f;
+            if (lane == 0) stat[parity][warp] = make_float2(mean, ss);
+            __syncthreads();
+            const float2 s = other < warps ? stat[parity][other] : make_float2(0.f, 0.f);
+            ss = s.y;
             if (a.center) {
-                for (int w = 0; w < warps; ++w) all = fmaf(stat[parity][y][w].x, count(w), all);
-                all *= a.by;
+                mean = s.x * n_other;
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+                mean *= a.by;
+                ss = fmaf(n_other * (s.x - mean), s.x - mean, ss);
             }
-            for (int w = 0; w < warps; ++w) {
-                const float2 s = stat[parity][y][w];
-                ss += a.center ? fmaf(count(w) * (s.x - all), s.x - all, s.y) : s.y;
-            }
-            mean = all;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         }
-        const float inv = rsqrtf(ss * a.by + a.eps);
+        const float inv = rsqrtf(ss * a.by + a.eps), back = -mean * inv;
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            const int k = column(u);
-            if (!live || k >= a.D) continue;
+            if (!live || col[u] >= a.D) continue;
+            if (a.center) {
+                // (fused: what the product would be rounded by is far below the sum's own error)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = (v[u][i] - mean) * inv;
+                for (int i = 0; i < 8; ++i) v[u][i] = fmaf(v[u][i], inv, back);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] *= inv;
+            }
             if (a.weight) {
                 float w[8];
-                load8(a.weight + set + k, w);
+                load8(a.weight + set + col[u], w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[u][i] *= w[i] + a.offset;
             }
             if (a.shift) {
                 float w[8];
-                load8(a.shift + set + k, w);
+                load8(a.shift + set + col[u], w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[u][i] += w[i];
             }
         }
         if constexpr (OUT == kSame) {
+            T* out = reinterpret_cast<T*>(a.out) + (size_t)m * a.ldo;
 #pragma unroll
             for (int u = 0; u < V; ++u)
-                if (live && column(u) < a.D) put8(reinterpret_cast<T*>(a.out) + (size_t)m * a.ldo + column(u), v[u]);
+                if (live && col[u] < a.D) put8(out + col[u], v[u]);
         } else if constexpr (OUT == kE4m3) {
 #pragma unroll
             for (int u = 0; u < V; ++u) {
-                const int k = column(u);
+                const int k = col[u];
                 float top = absmax8(v[u]);
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -172,50 +182,40 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
                 }
             }
         } else {
-            float top = 0.f;
+            float tops8[V], top = 0.f;
 #pragma unroll
-            for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
+            for (int u = 0; u < V; ++u) top = max_nan(top, tops8[u] = absmax8(v[u]));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
             if (warps > 1) {
-                if (lane == 0) tops[parity][y][warp] = top;
-                meet();
-                for (int w = 0; w < warps; ++w) top = max_nan(top, tops[parity][y][w]);
+                if (lane == 0) tops[parity][warp] = top;
+                __syncthreads();
+                top = other < warps ? tops[parity][other] : 0.f;
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
             }
-            const float row = row_scale4(top), six = 6.f * row;
-            const int pieces = a.D / kPieceCols4;
+            const Row4 row(top);
+            uint8_t* codes = reinterpret_cast<uint8_t*>(a.out) + (size_t)m * a.D / 2;
+            uint32_t* words = a.words + piece_word4((int)m, 0, a.D / kPieceCols4);
 #pragma unroll
             for (int u = 0; u < V; ++u) {
-                const int k = column(u);
-                uint32_t* codes = live && k < a.D ? reinterpret_cast<uint32_t*>(a.out) + ((size_t)m * a.D + k) / 8 : nullptr;
-                uint32_t* word = k < a.D && k % kPieceCols4 == 0 ? a.words + piece_word4((int)m, k / kPieceCols4, pieces) : nullptr;
-                store_fp4(v[u], row, six, codes, word);
-                if (!live && word) *word = 0u;
+                uint32_t* word = words + (size_t)(col[u] / kPieceCols4) * (kPiece4 / 4);
+                store_fp4(v[u], tops8[u], row, live && col[u] < a.D, reinterpret_cast<uint32_t*>(codes + col[u] / 2), word);
+                if (!live && col[u] < a.D && col[u] % kPieceCols4 == 0) *word = 0u;
             }
-            if (live && threadIdx.x == 0) a.row_scale[m] = row;
+            if (live && threadIdx.x == 0) a.row_scale[m] = row.row;
         }
     }
 }
 
-// Blocks of a kernel that the device holds at a time.
-template <class K>
-int resident(const Ctx* c, K kernel, int threads) {
-    int n = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess || n < 1) {
-        cudaGetLastError();
-        n = 1;
-    }
-    return n * c->num_sms;
-}
-
 template <typename T, int OUT, int V>
 wdc_status launch(Ctx* c, const AddNormArgs& a, int warps, cudaStream_t s) {
-    const int per = warps >= 8 ? 1 : (8 / warps < kMaxRows ? 8 / warps : kMaxRows);
+    const int per = warps == 1 ? kRowsAtOnce : 1;
     const long long rows = OUT == kE2m1 ? ((long long)(a.M - 1) / 128 + 1) * 128 : a.M;
     const long long blocks = (rows + per - 1) / per;
     static PerDevice<int> held[kMaxThreads / 32 + 1];
     const int most = held[warps].get(c->device, [&](int& n) {
-        n = resident(c, add_norm_kernel<T, OUT, V>, 32 * warps * per);
+        n = resident_blocks(c, add_norm_kernel<T, OUT, V>, 32 * warps * per);
         return true;
     });
     {

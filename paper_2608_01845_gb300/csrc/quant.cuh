@@ -56,11 +56,14 @@ template <typename T> __device__ __forceinline__ void load8(const T* p, float (&
     widen8(r, v);
 }
 
+// The largest of three magnitudes, NaN kept.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float absmax8(const float (&v)[8]) {
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(v[i]));
-    return m;
+    return max_abs(max_abs(max_abs(v[0], v[1], v[2]), v[3], v[4]), max_abs(v[5], v[6], v[7]), 0.f);
 }
 
 // The eight quotients by a scale outside the range of store8's shorter way.
@@ -91,6 +94,17 @@ __device__ __forceinline__ void store8(uint8_t* q, const float (&v)[8], float s)
         w = quotients(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s);
     }
     *reinterpret_cast<uint2*>(q) = w;
+}
+
+// Blocks of a kernel that the device holds at a time.
+template <class K>
+int resident_blocks(const Ctx* c, K kernel, int threads) {
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 1;
+    }
+    return n * c->num_sms;
 }
 
 // ---------------------------------------------------------------- four bits
@@ -156,25 +170,42 @@ __device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// A row's scale, 6 times it and the reciprocal of that.
+struct Row4 {
+    float row, six, by_six;
+    bool live;                                     // neither 0 nor NaN
+    __device__ __forceinline__ explicit Row4(float top)
+        : row(row_scale4(top)), six(6.f * row), by_six(1.0f / six), live(row > 0.f) {}
+};
+
+// IEEE's quotient of a and a row's six: by its reciprocal and remainder (Markstein, see
+// store8) as long as nothing that matters underflows; out of line below that.
+static __device__ __noinline__ float small_quotient(float a, float six) { return a / six; }
+
 // A lane's 8 neighbouring columns of a row (two lanes a scale, eight a word of
-// scales) to codes and scales; `row` is the row's scale and `six` 6 times it.  The
-// whole warp calls it; lanes past the row's end hold zeros and have no `codes`.
-__device__ __forceinline__ void store_fp4(const float (&v)[8], float row, float six, uint32_t* codes, uint32_t* word) {
-    float top = absmax8(v);
+// scales) to codes and scales; `top`: their largest magnitude.  The whole warp calls it;
+// lanes past the row's end (!in) hold zeros; `word` is looked at in every eighth lane.
+__device__ __forceinline__ void store_fp4(const float (&v)[8], float top, const Row4& r, bool in, uint32_t* codes, uint32_t* word) {
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const bool live = row > 0.f;                   // (not for NaN either)
-    // (IEEE: the quotient of the definition)
-    const uint32_t s = live ? e4m3x4(__fdiv_rn(top, six), 0.f, 0.f, 0.f) & 0xffu : 0u;
-    const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s, __NV_E4M3))) * row;
-    const float by = live && step > 0.f ? __frcp_rn(step) : 0.f;
+    const float t = top * r.by_six;
+    float quotient = fmaf(fmaf(-t, r.six, top), r.by_six, t);
+    if (r.six < 0x1p-80f) quotient = small_quotient(top, r.six);       // (the row's, so the warp's)
+    uint32_t s;
+    float scale;
+    asm("{\n .reg .b16 p, h;\n .reg .b32 w;\n cvt.rn.satfinite.e4m3x2.f32 p, %3, %2;\n cvt.rn.f16x2.e4m3x2 w, p;\n"
+        " mov.b32 {h, _}, w;\n cvt.f32.f16 %1, h;\n cvt.u32.u16 %0, p;\n}"
+        : "=r"(s), "=f"(scale)
+        : "f"(r.live ? quotient : 0.f), "f"(0.f));
+    const float step = scale * r.row;
+    const float by = step > 0.f ? 1.0f / step : 0.f;
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = live ? v[i] * by : 0.f;
+    for (int i = 0; i < 8; ++i) y[i] = v[i] * by;
     const uint32_t q = e2m1x8(y);
-    if (codes) *codes = q;
-    const uint32_t s1 = __shfl_down_sync(0xffffffffu, s, 2), s2 = __shfl_down_sync(0xffffffffu, s, 4),
-                   s3 = __shfl_down_sync(0xffffffffu, s, 6);
-    if (codes && word) *word = s | s1 << 8 | s2 << 16 | s3 << 24;
+    if (in) *codes = r.live ? q : 0u;              // (a NaN's or infinity's row)
+    s |= __shfl_down_sync(0xffffffffu, s, 2) << 8;
+    s |= __shfl_down_sync(0xffffffffu, s, 4) << 16;
+    if (in && (threadIdx.x & 7) == 0) *word = s;
 }
 
 }  // namespace wdc

@@ -6,6 +6,8 @@
 // The row's scale needs the whole row before the first code: a row stays in the
 // registers of its warps between the two, so x is read once.  Bound by memory: 2.56
 // bytes an element for bf16, 4.56 for fp32.
+#include <type_traits>
+
 #include "quant.cuh"
 
 namespace wdc {
@@ -22,8 +24,8 @@ struct Quant4Args {
 };
 
 constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
-constexpr int kMaxThreads = 512;                   // of a row, and of a block
-constexpr int kMaxRows = 8;                        // of a block at a time
+constexpr int kMaxThreads = 512;                   // of a row
+constexpr int kRowsAtOnce = 8;                     // of a block whose rows have a warp each
 
 __device__ __forceinline__ float warp_max(float a) {
 #pragma unroll
@@ -31,32 +33,35 @@ __device__ __forceinline__ float warp_max(float a) {
     return a;
 }
 
-// Each threadIdx.y takes rows a grid apart, with all blockDim.x threads of a row and V
-// pieces of 8 columns a thread; the next row's loads are under way while one is worked on.
-// Rows past M (of the last 128) get scales of zero.
+// A block takes rows a grid apart: one at a time with all its threads, or (blockDim.y ==
+// kRowsAtOnce) one a warp; a thread has V pieces of 8 columns, and the next row's loads
+// are under way while one is worked on.  Rows past M (of the last 128) get scales of zero.
 template <typename T, int V>
 __global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_constant__ Quant4Args a) {
-    __shared__ float tops[2][kMaxRows][kMaxThreads / 32];
+    __shared__ float tops[2][kMaxThreads / 32];
     chain_release();
     chain_wait();
-    const int y = threadIdx.y, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const unsigned step = gridDim.x * blockDim.y, M = a.M, rows = (M + 127) / 128 * 128;   // (a row and a step: below 2^32)
-    auto column = [&](int u) { return (u * (int)blockDim.x + (int)threadIdx.x) * 8; };
+    int col[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) col[u] = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
     Raw8<T> raw[V];
     auto load = [&](unsigned m) {
+        if (m >= M) return;
+        const T* x = reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx;
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (m < M && column(u) < a.K) load_raw(reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx + column(u), raw[u]);
+            if (col[u] < a.K) load_raw(x + col[u], raw[u]);
     };
     unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
     int parity = 0;
     load(m);
-    for (; m < rows; m += step, parity ^= 1) {
-        const bool live = m < M;
-        float v[V][8], top = 0.f;
+    for (; m < M; m += step, parity ^= 1) {
+        float v[V][8], top8[V], top = 0.f;
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            if (live && column(u) < a.K) {
+            if (col[u] < a.K) {
                 widen8(raw[u], v[u]);
             } else {
 #pragma unroll
@@ -65,24 +70,26 @@ __global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_con
         }
         load(m + step);
 #pragma unroll
-        for (int u = 0; u < V; ++u) top = max_nan(top, absmax8(v[u]));
+        for (int u = 0; u < V; ++u) top = max_nan(top, top8[u] = absmax8(v[u]));
         top = warp_max(top);
         if (warps > 1) {
-            if ((threadIdx.x & 31) == 0) tops[parity][y][threadIdx.x >> 5] = top;
-            asm volatile("bar.sync %0, %1;" ::"r"(y + 1), "r"(blockDim.x) : "memory");
-            for (int w = 0; w < warps; ++w) top = max_nan(top, tops[parity][y][w]);
-        }
-        const float row = row_scale4(top), six = 6.f * row;
+            if (lane == 0) tops[parity][threadIdx.x >> 5] = top;
+            __syncthreads();
+            top = (lane & 15) < warps ? tops[parity][lane & 15] : 0.f;
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-            const int k = column(u);
-            uint32_t* codes = live && k < a.K ? reinterpret_cast<uint32_t*>(a.codes) + ((size_t)m * a.K + k) / 8 : nullptr;
-            uint32_t* word = k < a.K && k % kPieceCols4 == 0 ? a.scale + piece_word4((int)m, k / kPieceCols4, a.pieces) : nullptr;
-            store_fp4(v[u], row, six, codes, word);
-            if (!live && word) *word = 0u;
+            for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
-        if (live && threadIdx.x == 0) a.row_scale[m] = row;
+        const Row4 row(top);
+        uint8_t* codes = a.codes + (size_t)m * (unsigned)a.K / 2;
+        uint32_t* words = a.scale + piece_word4((int)m, 0, a.pieces);
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            store_fp4(v[u], top8[u], row, col[u] < a.K, reinterpret_cast<uint32_t*>(codes + col[u] / 2),
+                      words + (size_t)(col[u] / kPieceCols4) * (kPiece4 / 4));
+        if (threadIdx.x == 0) a.row_scale[m] = row.row;
     }
+    for (; m < rows; m += step)
+        for (int p = threadIdx.x; p < a.pieces; p += blockDim.x) a.scale[piece_word4((int)m, p, a.pieces)] = 0u;
 }
 
 // Rows wider than a block's registers: read twice, the second time from L2.
@@ -106,7 +113,7 @@ __global__ void __launch_bounds__(512) quantize4_wide_kernel(const __grid_consta
     if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
     __syncthreads();
     for (int w = 0; w < 16; ++w) top = max_nan(top, tops[w]);
-    const float row = row_scale4(top), six = 6.f * row;
+    const Row4 row(top);
     for (long long k0 = 0; k0 < a.K; k0 += blockDim.x * 8) {        // (whole warps: the lanes trade scales)
         const long long k = k0 + threadIdx.x * 8;
         if (k < a.K) {
@@ -115,32 +122,32 @@ __global__ void __launch_bounds__(512) quantize4_wide_kernel(const __grid_consta
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.f;
         }
-        uint32_t* codes = k < a.K ? reinterpret_cast<uint32_t*>(a.codes + ((size_t)m * a.K + k) / 2) : nullptr;
-        uint32_t* word =
-            k < a.K && k % kPieceCols4 == 0 ? a.scale + piece_word4(m, (int)(k / kPieceCols4), a.pieces) : nullptr;
-        store_fp4(v, row, six, codes, word);
+        store_fp4(v, absmax8(v), row, k < a.K, reinterpret_cast<uint32_t*>(a.codes + ((size_t)m * a.K + k) / 2),
+                  a.scale + piece_word4(m, (int)(k / kPieceCols4), a.pieces));
     }
-    if (threadIdx.x == 0) a.row_scale[m] = row;
+    if (threadIdx.x == 0) a.row_scale[m] = row.row;
 }
 
-// Eight columns a thread of kBackRows rows, blockDim.y apart.
+// 16 bytes of x a thread, in kBackRows rows blockDim.y apart.
 constexpr int kBackRows = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) dequantize4_kernel(const uint32_t* codes, const uint8_t* scale, const float* row_scale,
+__global__ void __launch_bounds__(256) dequantize4_kernel(const uint8_t* codes, const uint8_t* scale, const float* row_scale,
                                                           T* x, long long ldx, int M, int K, int pieces, int segments) {
+    constexpr int E = 16 / (int)sizeof(T);
+    using Codes = typename std::conditional<E == 8, uint32_t, uint16_t>::type;
     chain_release();
     chain_wait();
-    const int k = ((int)(blockIdx.x % segments) * (int)blockDim.x + (int)threadIdx.x) * 8;
+    const int k = ((int)(blockIdx.x % segments) * (int)blockDim.x + (int)threadIdx.x) * E;
     if (k >= K) return;
     const unsigned m0 = blockIdx.x / segments * (blockDim.y * kBackRows) + threadIdx.y;
-    uint32_t q[kBackRows];
+    Codes q[kBackRows];
     uint8_t s[kBackRows];
     float r[kBackRows];
 #pragma unroll
     for (int i = 0; i < kBackRows; ++i) {
         const unsigned m = m0 + i * blockDim.y;
         if (m >= (unsigned)M) continue;
-        q[i] = codes[((size_t)m * K + k) / 8];
+        q[i] = *reinterpret_cast<const Codes*>(codes + ((size_t)m * K + k) / 2);
         s[i] = scale[4 * piece_word4((int)m, k / kPieceCols4, pieces) + (k / 16) % 4];
         r[i] = row_scale[m];
     }
@@ -153,21 +160,19 @@ __global__ void __launch_bounds__(256) dequantize4_kernel(const uint32_t* codes,
         e2m1_values(q[i], v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= step;
-        put8(x + (size_t)m * ldx + k, v);
+        T* to = x + (size_t)m * ldx + k;
+        if constexpr (E == 8) put8(to, v);
+        else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
     }
 }
 
 template <typename T, int V>
 void launch_held(Ctx* c, const Quant4Args& a, int warps, cudaStream_t s) {
-    const int per = warps >= 8 ? 1 : (8 / warps < kMaxRows ? 8 / warps : kMaxRows);
+    const int per = warps == 1 ? kRowsAtOnce : 1;
     const long long rows = ((long long)(a.M - 1) / 128 + 1) * 128, blocks = (rows + per - 1) / per;
     static PerDevice<int> held[kMaxThreads / 32 + 1];
     const int most = held[warps].get(c->device, [&](int& n) {
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, quantize4_kernel<T, V>, 32 * warps * per, 0) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            n = 1;
-        }
-        n *= c->num_sms;
+        n = resident_blocks(c, quantize4_kernel<T, V>, 32 * warps * per);
         return true;
     });
     launch_kernel(quantize4_kernel<T, V>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(32 * warps, per), 0, s, 1, a);
@@ -176,7 +181,7 @@ void launch_held(Ctx* c, const Quant4Args& a, int warps, cudaStream_t s) {
 template <typename T>
 wdc_status launch(Ctx* c, const Quant4Args& a, cudaStream_t s) {
     const int eights = a.K / 8;
-    const int v = eights <= 32 ? 1 : (eights <= 2 * kMaxThreads ? 2 : kHeld), warps = (eights + 32 * v - 1) / (32 * v);
+    const int v = eights <= 32 ? 1 : (eights <= (sizeof(T) == 2 ? 64 : 2 * kMaxThreads) ? 2 : kHeld), warps = (eights + 32 * v - 1) / (32 * v);
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_OTHER, s);
@@ -193,16 +198,16 @@ wdc_status launch(Ctx* c, const Quant4Args& a, cudaStream_t s) {
 
 template <typename T>
 wdc_status launch_back(Ctx* c, const wdc_fp4& q, T* x, long long ldx, int M, int K, cudaStream_t s) {
-    const int eights = K / 8;
+    const int across = K / (16 / (int)sizeof(T));
     int tx = 8;
-    while (tx < eights && tx < 256) tx *= 2;
-    const int ty = 256 / tx, segments = (eights + tx - 1) / tx;
+    while (tx < across && tx < 256) tx *= 2;
+    const int ty = 256 / tx, segments = (across + tx - 1) / tx;
     const long long blocks = ((long long)(M - 1) / (ty * kBackRows) + 1) * segments;
     if (blocks > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 dequantize: more than 2^31 - 1 thread blocks");
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_OTHER, s);
-        launch_kernel(dequantize4_kernel<T>, dim3((unsigned)blocks), dim3(tx, ty), 0, s, 1, (const uint32_t*)q.codes,
+        launch_kernel(dequantize4_kernel<T>, dim3((unsigned)blocks), dim3(tx, ty), 0, s, 1, (const uint8_t*)q.codes,
                       (const uint8_t*)q.scale, (const float*)q.row_scale, x, ldx, M, K, K / kPieceCols4, segments);
     }
     cudaError_t e = cudaGetLastError();
