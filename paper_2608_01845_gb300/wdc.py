@@ -7,6 +7,7 @@ import time -- there is no fallback path.
 """
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libwdc.so")
@@ -137,6 +138,8 @@ class AddNorm(ctypes.Structure):
                 + [("weight_offset", ctypes.c_float), ("eps", ctypes.c_float), ("rows_per_set", ctypes.c_int),
                    ("center", ctypes.c_int)])
 
+
+_ADD_NORM = struct.Struct("=4Q4q6Q2f2i")       # the same
 
 def _load():
     if not os.path.exists(LIB_PATH):
@@ -370,6 +373,14 @@ def _address(t):
 def _row_stride(t):
     """Elements from one row to the next; of a single row, its length."""
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _rows(what, name, t, dtype, shape, device):
+    """_tensor of a matrix whose rows may lie apart: its address and row stride."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr(), shape[1] or 1
+    _tensor(what, name, t, dtype, shape, device, row_stride=True)
+    return t.data_ptr(), _row_stride(t)
 
 
 class Context:
@@ -749,17 +760,15 @@ class Context:
         """wdc_op_quantize_fp4: x [M, K] (rows may lie apart) to q (an Fp4Matrix)."""
         what, (dt, dev, *_) = "op_quantize_fp4", self._operand_types()
         M, K = q.shape
-        _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
-        self._check(LIB.wdc_op_quantize_fp4(self._h, x.data_ptr(), _row_stride(x), self._fp4(what, "q", q, M, K), M, K,
-                                            self._op_stream(stream)), what)
+        p, ld = _rows(what, "x", x, dt, q.shape, dev)
+        self._check(LIB.wdc_op_quantize_fp4(self._h, p, ld, self._fp4(what, "q", q, M, K), M, K, self._op_stream(stream)), what)
 
     def op_dequantize_fp4(self, q, x, stream=None):
         """wdc_op_dequantize_fp4: the values of q (an Fp4Matrix) to x [M, K] (rows may lie apart)."""
         what, (dt, dev, *_) = "op_dequantize_fp4", self._operand_types()
         M, K = q.shape
-        _tensor(what, "x", x, dt, (M, K), dev, row_stride=True)
-        self._check(LIB.wdc_op_dequantize_fp4(self._h, self._fp4(what, "q", q, M, K), x.data_ptr(), _row_stride(x), M, K,
-                                              self._op_stream(stream)), what)
+        p, ld = _rows(what, "x", x, dt, q.shape, dev)
+        self._check(LIB.wdc_op_dequantize_fp4(self._h, self._fp4(what, "q", q, M, K), p, ld, M, K, self._op_stream(stream)), what)
 
     def op_gemm_fp4(self, A, W, C, bias=None, gelu=False, res=None, gate=None, stream=None):
         """wdc_op_gemm_fp4: C = epilogue(A W^T) of Fp4Matrix operands, with the epilogues of op_gemm."""
@@ -803,37 +812,38 @@ class Context:
         _sizes(what, M, D)
         if not 0 <= rows_per_set <= _INT_MAX:
             raise ValueError(f"{what}: rows_per_set of {rows_per_set}")
-        n = AddNorm(weight_offset=weight_offset, eps=eps, rows_per_set=rows_per_set, center=int(bool(center)))
-        _tensor(what, "x", x, dt, (M, D), dev, row_stride=True)
-        n.x, n.ldx = x.data_ptr(), _row_stride(x)
+        shape = (M, D)
+        p, ldx = _rows(what, "x", x, dt, shape, dev)
+        d = t = o = q8 = sc = ldd = ldt = ldo = q4 = 0
         if delta is not None:
-            _tensor(what, "delta", delta, dt, (M, D), dev, row_stride=True)
-            n.delta, n.ldd = delta.data_ptr(), _row_stride(delta)
+            d, ldd = _rows(what, "delta", delta, dt, shape, dev)
         if total is not None:
-            _tensor(what, "total", total, dt, (M, D), dev, row_stride=True)
-            n.total, n.ldt = total.data_ptr(), _row_stride(total)
+            t, ldt = _rows(what, "total", total, dt, shape, dev)
         sets = -(-M // rows_per_set) if rows_per_set else 1
-        for name, v in (("gate", gate), ("weight", weight), ("shift", shift)):
+        vectors = [0, 0, 0]
+        for i, v in enumerate((gate, weight, shift)):
             if v is not None:
-                _tensor(what, name, v, f32, (D,) if v.dim() == 1 and sets == 1 else (sets, D), dev)
-                setattr(n, name, v.data_ptr())
+                _tensor(what, ("gate", "weight", "shift")[i], v, f32, (D,) if sets == 1 and v.dim() == 1 else (sets, D), dev)
+                vectors[i] = v.data_ptr()
         if isinstance(out, Fp4Matrix):
-            n.q4 = ctypes.pointer(self._fp4(what, "out", out, M, D))
+            q4 = ctypes.addressof(self._fp4(what, "out", out, M, D))
         elif out.dtype is f8:
-            _tensor(what, "out", out, f8, (M, D), dev)
-            n.q8 = out.data_ptr()
+            _tensor(what, "out", out, f8, shape, dev)
+            q8 = out.data_ptr()
             if scale is None:
                 raise ValueError(f"{what}: out in e4m3 needs scale")
         else:
-            _tensor(what, "out", out, dt, (M, D), dev, row_stride=True)
-            n.out, n.ldo = out.data_ptr(), _row_stride(out)
+            o, ldo = _rows(what, "out", out, dt, shape, dev)
         if scale is not None:
-            if not n.q8:
+            if not q8 and M > 0:
                 raise ValueError(f"{what}: scale goes with out in e4m3")
             _tensor(what, "scale", scale, f32, (-(-D // 128), M), dev)
-            n.scale = scale.data_ptr()
+            sc = scale.data_ptr()
         if M == 0:                                         # (empty tensors have no address)
             return
+        # (packed at once: its eighteen fields set one by one took longer than the call)
+        n = AddNorm.from_buffer_copy(_ADD_NORM.pack(p, d, t, o, ldx, ldd, ldt, ldo, q8, sc, q4, *vectors,
+                                                    weight_offset, eps, rows_per_set, 1 if center else 0))
         self._check(LIB.wdc_op_add_norm(self._h, n, M, D, self._op_stream(stream)), what)
 
 

@@ -90,6 +90,15 @@ def test_struct_layouts(tmp_path, cname, struct):
     layout(tmp_path, cname, struct)
 
 
+def test_packed_residual_norm():
+    """What the binding packs at once lands in the struct's fields."""
+    v = list(range(1, 15)) + [0.5, 0.25, 15, 1]
+    n = wdc.AddNorm.from_buffer_copy(wdc._ADD_NORM.pack(*v))
+    assert wdc._ADD_NORM.size == ctypes.sizeof(n)
+    got = [getattr(n, f) if f != "q4" else ctypes.cast(n.q4, ctypes.c_void_p).value for f, _ in n._fields_]
+    assert got == v
+
+
 def test_null_context_is_refused():
     L, N, q = wdc.LIB, None, wdc.Fp4C()
     assert L.wdc_op_quantize_fp4(N, N, 64, q, 1, 64, N) == 1
