@@ -616,7 +616,10 @@ wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_c
  * floating point, their products, a gated MLP's among them, and the rotation of a
  * video's heads by frame, row and column.  As the chunk operators: asynchronous on
  * `stream`, checked before any launch, capturable, and nothing is launched where there
- * are no rows.  A call of wdc_op_gemm_fp4 or wdc_op_gated_fp4 needs no workspace. */
+ * are no rows.  A product may split the sums of some of its tiles and join them through a
+ * workspace of its own that the context owns: two calls of wdc_op_gemm_fp4 or
+ * wdc_op_gated_fp4 of one context, and graphs that hold some, must not run concurrently.
+ * (The results of equal calls are equal bit for bit.) */
 
 /* Positions of several axes (frame, row and column of a video's token, say): the
  * turned pairs of a head are in sections, the first pairs[0] of them turned by the

@@ -1034,6 +1034,11 @@ wdc_status dit_create(Ctx* c) {
         if (cudaMemset(c->attn_counters, 0, counters) != cudaSuccess) return fail(c, WDC_ERR_CUDA, "DiT init: attention counters");
         c->attn_part_samples = t->B;
     }
+    c->fp4_parts = c->num_sms / 2;                           // (one a pair of SMs)
+    const size_t counted = (size_t)c->fp4_parts * 16 * sizeof(unsigned);
+    if ((s = dalloc(c, (void**)&c->fp4_work, (size_t)c->fp4_parts * 256 * 256 * sizeof(float)))) return s;
+    if ((s = dalloc(c, (void**)&c->fp4_counters, counted))) return s;
+    if (cudaMemset(c->fp4_counters, 0, counted) != cudaSuccess) return fail(c, WDC_ERR_CUDA, "DiT init: fp4 product counters");
     const long long npe = (long long)t->Lv * t->D;
     LaunchScope ls(c, WDC_K_OTHER, 0);
     if (t->dtype == WDC_BF16)
@@ -1056,6 +1061,9 @@ void dit_destroy(Ctx* c) {
     c->attn_part_rounds = 0;
     c->attn_counters = nullptr;
     c->attn_records = nullptr;
+    c->fp4_work = nullptr;
+    c->fp4_counters = nullptr;
+    c->fp4_parts = 0;
 }
 
 static uint16_t f32_to_bf16_bits(float f) {

@@ -3,6 +3,9 @@
 // and of two such products the gated form act(A W^T) * (A U^T).
 #include "gemm_fp4.cuh"
 
+#include <cmath>
+#include <type_traits>
+
 namespace wdc {
 
 namespace {
@@ -27,7 +30,7 @@ struct Narrow4Cfg {
     static constexpr uint32_t STAGE = WS * W_BYTES + A_BYTES + (WS + 1) * S_BYTES;
     static constexpr int SCALE_COLS = 16 * (WS + 1);                   // of a stage, in tensor memory
     static constexpr int ACC_COLS = WS * BN;
-    static constexpr size_t FIXED = 1024 + 512;
+    static constexpr size_t FIXED = 1024 + 512 + BN * 4;               // alignment, barriers, the tokens' scales
     static constexpr int BY_SMEM = (int)((227 * 1024 - FIXED) / STAGE), BY_TMEM = (512 - ACC_COLS) / SCALE_COLS;
     static constexpr int STAGES = BY_SMEM < BY_TMEM ? BY_SMEM : BY_TMEM;
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + FIXED;
@@ -45,7 +48,8 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
     using C = Narrow4Cfg<BN, GATED>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE);
+    float* token_scale = reinterpret_cast<float*>(smem + C::STAGES * C::STAGE);
+    uint64_t* full = reinterpret_cast<uint64_t*>(token_scale + BN);
     uint64_t* empty = full + C::STAGES;
     uint64_t* done = empty + C::STAGES;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
@@ -156,6 +160,10 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
     bool ok = true;
     float rw = 0.f, ru = 0.f, bias = 0.f, up_bias = 0.f, gate = 1.f;
     if (warp >= 2) {
+        // (fetched where they are used, a group of 16 tokens behind the other, they took 1 us each)
+        const int c = threadIdx.x - 64;
+        if (c < BN) token_scale[c] = m0 + c < g.M ? ld_chain(g.ra + m0 + c) : 0.f;
+        asm volatile("bar.sync 1, 128;" ::: "memory");     // the four warps
         if (n < g.N) {
             rw = ld_chain(g.rw + n);
             if (g.bias) bias = ld_chain(g.bias + n);
@@ -170,23 +178,36 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
         tc_fence_after();
     }
     const uint32_t lanes = tmem + ((uint32_t)(lg * 32) << 16);
-    const T* res = reinterpret_cast<const T*>(g.res);
-    auto fetch_res = [&](int c) {
-        const int m = m0 + c;
-        return !GATED && g.res && ok && n < g.N && m < g.M ? ld_act<T>(res + (size_t)m * g.N + n) : 0.f;
-    };
-    auto put = [&](int c, float v, float u, float r) {
-        const int m = m0 + c;
-        if (!ok || n >= g.N || m >= g.M) return;
-        const float ra = ld_chain(g.ra + m);
-        v = fmaf(v * ra, rw, bias);
-        if constexpr (GATED) {
-            v = (g.gelu ? gelu_tanh_f(v) : silu_f(v)) * fmaf(u * ra, ru, up_bias);
-        } else {
-            if (g.gelu) v = gelu_tanh_f(v);
-            if (g.res) v = fmaf(gate, v, r);
+    // Finishes CH tokens from c on.  All is worked out for all of them, and only what lies in C
+    // is loaded and stored: a branch a token leaves the warp, alone on its scheduler, waiting
+    // for each instruction in turn.
+    const bool mine = ok && n < g.N;
+    auto finish = [&](int c, auto& v, auto& u) {
+        constexpr int CH = sizeof(v) / sizeof(float);
+        const int left = mine ? g.M - m0 - c : 0;          // tokens
+        const size_t at = (size_t)(m0 + c) * g.N + n;
+        float r[CH];
+        if (!GATED && g.res) {
+            const T* res = reinterpret_cast<const T*>(g.res) + at;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) r[i] = i < left ? ld_act<T>(res + (size_t)i * g.N) : 0.f;
         }
-        reinterpret_cast<T*>(g.out)[(size_t)m * g.N + n] = to_act<T>(v);
+        T* out = reinterpret_cast<T*>(g.out) + at;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const float ra = token_scale[c + i];
+            float x = fmaf(v[i] * ra, rw, bias);
+            if constexpr (GATED) {
+                x = (g.gelu ? gelu_tanh_f(x) : silu_f(x)) * fmaf(u[i] * ra, ru, up_bias);
+            } else {
+                if (g.gelu) x = gelu_tanh_f(x);
+                if (g.res) x = fmaf(gate, x, r[i]);
+            }
+            v[i] = x;
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (i < left) out[(size_t)i * g.N] = to_act<T>(v[i]);
     };
     auto load16 = [&](int c, float (&v)[16]) {             // 16 columns of sums
         uint32_t p[16];
@@ -199,13 +220,10 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
         if (warp >= 2) {
 #pragma unroll 1
             for (int c0 = 0; c0 < BN && m0 + c0 < g.M; c0 += 16) {
-                float v[16], u[16] = {}, r[16];
+                float v[16], u[16] = {};
                 load16(c0, v);
                 if (GATED) load16(BN + c0, u);
-#pragma unroll
-                for (int c = 0; c < 16; ++c) r[c] = fetch_res(c0 + c);
-#pragma unroll
-                for (int c = 0; c < 16; ++c) put(c0 + c, v[c], u[c], r[c]);
+                finish(c0, v, u);
                 __syncwarp();
             }
         }
@@ -219,7 +237,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
 #pragma unroll
             for (int h = 0; h < C::WS; ++h)
 #pragma unroll 1
-                for (int c0 = 0; c0 < BN; c0 += 16) {
+                for (int c0 = 0; c0 < BN && m0 + c0 < g.M; c0 += 16) {
                     float v[16];
                     load16(h * BN + c0, v);
 #pragma unroll
@@ -235,26 +253,24 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
         cluster_sync_all();
         if (warp >= 2) {
             const float4* part = reinterpret_cast<const float4*>(smem);
-            for (int i = 0; i < share; ++i) {
-                const int c = 4 * (rank * share + i);
-                if (m0 + c >= g.M) break;
-                float r[4];
+            // G groups from i on, the sources in rank order
+            auto join = [&](int i, auto groups) {
+                constexpr int G = decltype(groups)::value;
+                float v[2][4 * G] = {};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = fetch_res(c + k);
-                float4 v[2];
+                for (int h = 0; h < C::WS; ++h)
+                    for (int p = 0; p < S; ++p)
 #pragma unroll
-                for (int h = 0; h < C::WS; ++h) {
-                    v[h] = part[(h * S * share + i) * 128 + row];
-                    for (int p = 1; p < S; ++p) {
-                        const float4 x = part[((h * S + p) * share + i) * 128 + row];
-                        v[h].x += x.x; v[h].y += x.y; v[h].z += x.z; v[h].w += x.w;
-                    }
-                }
-                const float4 u = v[C::WS - 1];
-                put(c, v[0].x, u.x, r[0]);
-                put(c + 1, v[0].y, u.y, r[1]);
-                put(c + 2, v[0].z, u.z, r[2]);
-                put(c + 3, v[0].w, u.w, r[3]);
+                        for (int k = 0; k < G; ++k) {
+                            const float4 x = part[((h * S + p) * share + i + k) * 128 + row];
+                            v[h][4 * k] += x.x; v[h][4 * k + 1] += x.y; v[h][4 * k + 2] += x.z; v[h][4 * k + 3] += x.w;
+                        }
+                finish(4 * (rank * share + i), v[0], v[1]);
+            };
+            if (share % 4 == 0) {
+                for (int i = 0; i < share && m0 + 4 * (rank * share + i) < g.M; i += 4) join(i, std::integral_constant<int, 4>());
+            } else {
+                for (int i = 0; i < share && m0 + 4 * (rank * share + i) < g.M; ++i) join(i, std::integral_constant<int, 1>());
             }
         }
     }
@@ -313,15 +329,65 @@ wdc_status launch_narrow(Ctx* c, Gemm4Args g, int bn, int split, cudaStream_t s)
     return WDC_OK;
 }
 
+// The kernel for a shape is the one with the least estimated time, by fits to a sweep (us,
+// bf16, no residual, operands in L2; narrow kernel n<tokens a tile>,<CTAs a tile>; pair kernel p):
+//                          n16,1  n16,4  n32,1  n32,4  n64,1  n64,4  n128,1 n128,4    p
+//   4 x 1024 x 1024          3.6    4.4                                3.8           6.9
+//   4 x 4096 x 16384        13.9    7.2                               14.3   14.7   22.8
+//   4 x 15360 x 5120         6.7   17.9                               12.2          15.9
+//   32 x 4096 x 4096                       6.4    6.0                  6.5          10.1
+//   32 x 4096 x 16384                     14.6    8.1                 14.8    9.2   22.9
+//   64 x 27648 x 2048                                    11.3         14.0          12.7
+//   64 x 4096 x 16384                                    15.6    9.1  15.6   10.2   23.0
+//   100 x 1024 x 1024                                                  6.4           7.7
+//   200 x 4096 x 4096                                                  9.3   17.7   11.1
+//   200 x 15360 x 5120                                                19.2          12.9
+//   400 x 4096 x 16384                                                18.0          24.0
+//   700 x 4096 x 4096                                                 17.8          11.5
+//   gated 64 x 10240 x 4096                               9.7         10.6          16.9
+//   gated 200 x 10240 x 4096                                          23.1          17.3
+// A narrow CTA takes kStage us for 256 of K and a little for each token; more CTAs than
+// the device holds (fewer than its SMs in clusters of 8) take turns; a cluster's launch
+// and exchange cost what `split` adds.
+struct Choice {
+    int bn, split;                     // split 0: the pair kernel
+};
+Choice choose(const Ctx* c, int M, int N, int K, bool gated) {
+    constexpr double kStage[2][4] = {{0.17, 0.17, 0.175, 0.17}, {0.28, 0.28, 0.30, 0.36}};
+    const int kb = (K - 1) / kTileK4 + 1;
+    Choice best{128, 1};
+    double least = 1e30;
+    auto offer = [&](int bn, int split, double est) {
+        if (est < least) {
+            least = est;
+            best = {bn, split};
+        }
+    };
+    for (int i = 0; i < 4; ++i) {
+        const int bn = 16 << i;
+        if (bn < 128 && M > bn) continue;
+        const double tiles = (double)((M - 1) / bn + 1) * ((N - 1) / 128 + 1), tokens = M < bn ? M : bn;
+        for (int split = 1; split <= 8 && split <= bn / 4 && (split == 1 || 2 * split <= kb); split *= 2) {
+            const double held = split == 8 ? 0.74 * c->num_sms : c->num_sms;
+            const double turn = (kb + split - 1) / split * kStage[gated][i] + 1.6 + 0.024 * tokens / split;
+            const double join = (gated ? 2.0 : 1.4) + (gated ? 0.04 : 0.02) * tokens + (bn == 128 ? 1.0 : 0.0);
+            offer(bn, split, 1.5 + ceil(tiles * split / held) * (turn + (split > 1 ? join : 0.0)));
+        }
+    }
+    if (c->num_sms >= 2) {
+        const double tiles = (double)((M - 1) / 256 + 1) * ((N - 1) / (gated ? 128 : 256) + 1);
+        offer(256, 0, 4.4 + ceil(tiles / (c->num_sms / 2)) * (kb * 0.265 + 1.4));
+    }
+    return best;
+}
+
 wdc_status launch(Ctx* c, const Gemm4Args& g, cudaStream_t s) {
-    if (c->num_sms >= 2 && g.M > 256) return launch_gemm4_pair(c, g, s);
-    const int bn = g.M <= 16 ? 16 : (g.M <= 32 ? 32 : (g.M <= 64 ? 64 : 128));
-    const long long tiles = ((long long)(g.M - 1) / bn + 1) * ((g.N - 1) / 128 + 1);
-    int split = 1;
-    while (split < 8 && 2 * split <= bn / 4 && tiles * split * 2 <= c->num_sms && g.K / kTileK4 >= 4 * split) split *= 2;
+    const Choice ch = choose(c, g.M, g.N, g.K, g.U != nullptr);
+    if (ch.split == 0) return launch_gemm4_pair(c, g, s);
     if (c->cfg.dtype == WDC_BF16)
-        return g.U ? launch_narrow<__nv_bfloat16, true>(c, g, bn, split, s) : launch_narrow<__nv_bfloat16, false>(c, g, bn, split, s);
-    return g.U ? launch_narrow<float, true>(c, g, bn, split, s) : launch_narrow<float, false>(c, g, bn, split, s);
+        return g.U ? launch_narrow<__nv_bfloat16, true>(c, g, ch.bn, ch.split, s)
+                   : launch_narrow<__nv_bfloat16, false>(c, g, ch.bn, ch.split, s);
+    return g.U ? launch_narrow<float, true>(c, g, ch.bn, ch.split, s) : launch_narrow<float, false>(c, g, ch.bn, ch.split, s);
 }
 
 // What both products check; WDC_OK with *none: there is nothing to do.

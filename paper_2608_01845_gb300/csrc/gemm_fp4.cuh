@@ -20,7 +20,11 @@ struct Gemm4Args {
     int m_tiles, n_tiles;
     int kb;                             // tiles of K (kTileK4)
     int split;                          // narrow kernel: CTAs a tile
-    int group_n;                        // pair kernel: column blocks of a raster group
+    // pair kernel: column blocks of a raster group; tiles that a pair takes whole, the tiles
+    // behind them and the parts of K those are split in; the parts' sums and counters
+    int group_n, whole, tail, parts;
+    float* work;
+    unsigned* counters;
 };
 
 constexpr int kTileK4 = 256;            // of K: 128 bytes of codes, a row of the swizzled tiles, and four pieces of scales

@@ -9,6 +9,12 @@
 // 240 columns of five stages leave no room for a second tile's sums, so eight epilogue
 // warps first take the tile to their registers, a row a lane and 128 columns a warp, and
 // hand tensor memory back before they finish it.
+//
+// Tiles that would make a last round of fewer than the pairs are split over K, and these
+// parts come first: each writes its sums to the context's workspace, a warp's 32 x 128
+// at a time, and the warp that comes last (a counter a warp's piece) adds all of them in
+// the order of K and finishes the tile, while the MMAs of the whole tiles run; nobody
+// waits for another.
 #include "gemm_fp4.cuh"
 #include "pair_epilogue.cuh"
 
@@ -68,7 +74,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int tiles = g.m_tiles * g.n_tiles;
+    // this pair's jobs: at most one part of a tile, then a whole tile each
+    const int first = pair < g.tail * g.parts ? 1 : 0, jobs = first + (g.whole - pair + pairs - 1) / pairs;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(&full[s], 1);
@@ -111,6 +118,28 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         mb = r / width;
         nb = first + (r - mb * width);
     };
+    // job j: its tile's place and its part of K; what the part is of (tail tile, -1: none)
+    struct Job {
+        int mb, nb, kb0, kb1, tail, part;
+    };
+    auto job = [&](int j) {
+        Job t;
+        int tile = pair + (j - first) * pairs;
+        t.tail = -1;
+        t.part = 0;
+        t.kb0 = 0;
+        t.kb1 = g.kb;
+        if (j < first) {
+            t.tail = pair / g.parts;
+            t.part = pair - t.tail * g.parts;
+            tile = g.whole + t.tail;
+            t.kb0 = (int)((long long)t.part * g.kb / g.parts);
+            t.kb1 = (int)((long long)(t.part + 1) * g.kb / g.parts);
+            if (g.parts == 1) t.tail = -1;
+        }
+        place(tile, t.mb, t.nb);
+        return t;
+    };
 
     if (warp < 4) {
       setmaxnreg_dec<kRegsControl>();
@@ -118,13 +147,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           int stage = 0;
           uint32_t phase = 0, armed = 0, parity = 0;         // per stage: a copy was issued; its phase
           bool ok = true;
-          for (int tile = pair; tile < tiles && ok; tile += pairs) {
-              int mb, nb;
-              place(tile, mb, nb);
-              const int mblock = mb * 2 + (int)rank;         // of 128 rows
+          for (int j = 0; j < jobs && ok; ++j) {
+              const Job t = job(j);
+              const int nb = t.nb, mblock = t.mb * 2 + (int)rank;    // of 128 rows
               const int w0 = GATED ? nb * 128 : nb * 256 + (int)rank * 128;
               const CUtensorMap* weights = GATED && rank == 1 ? &tmU : &tmW;
-              for (int kb = 0; kb < g.kb; ++kb) {
+              for (int kb = t.kb0; kb < t.kb1; ++kb) {
                   if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_flag, g.err)) { ok = false; break; }
                   if (elect_one()) {
                       if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * C::STAGE);
@@ -163,10 +191,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               int stage = 0;
               uint32_t phase = 0, tphase = 0;
               bool ok = true;                                // this lane's waits (elect_one)
-              for (int tile = pair; tile < tiles; tile += pairs) {
+              for (int j = 0; j < jobs; ++j) {
+                  const Job t = job(j);
                   ok = ok && mbar_wait(tempty, tphase ^ 1u, abort_flag, g.err);
                   tphase ^= 1u;
-                  for (int kb = 0; kb < g.kb; ++kb) {
+                  for (int kb = t.kb0; kb < t.kb1; ++kb) {
                       ok = ok && mbar_wait(&full[stage], phase, abort_flag, g.err);
                       tc_fence_after();
                       if (elect_one() && ok) {
@@ -183,8 +212,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
                           for (int k = 0; k < 4; ++k)
                               tc_mma4_2(tmem, sdesc_at(da, stage * C::STAGE + k * 32), sdesc_at(db, stage * C::STAGE + k * 32),
-                                        C::IDESC, sc + 12 * k, sc + 12 * k + 4, kb != 0 || k != 0);
-                          if (kb + 1 == g.kb) tc_commit2_mc(tfull, (uint16_t)0x3);
+                                        C::IDESC, sc + 12 * k, sc + 12 * k + 4, kb != t.kb0 || k != 0);
+                          if (kb + 1 == t.kb1) tc_commit2_mc(tfull, (uint16_t)0x3);
                           tc_commit2_mc(&empty[stage], (uint16_t)0x3);
                       }
                       __syncwarp();
@@ -201,9 +230,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       } else if (warp == 2) {
           // the tile's vectors: [half h of the 256 sums' columns][rw, bias, gate][128]
           uint32_t phase = 0;
-          for (int tile = pair; tile < tiles; tile += pairs) {
-              int mb, nb;
-              place(tile, mb, nb);
+          for (int j = 0; j < jobs; ++j) {
+              const int nb = job(j).nb;
               float v[2][3][4];
 #pragma unroll
               for (int h = 0; h < 2; ++h)
@@ -247,13 +275,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             pending = true;
         };
-        for (int tile = pair; tile < tiles && ok; tile += pairs) {
-            int mb, nb;
-            place(tile, mb, nb);
-            const int m0 = mb * 256 + (int)rank * 128 + quarter * 32, n0 = nb * BN + side * COLS;
+        for (int j = 0; j < jobs && ok; ++j) {
+            const Job t = job(j);
+            const int m0 = t.mb * 256 + (int)rank * 128 + quarter * 32, n0 = t.nb * BN + side * COLS;
             const int end = min(n0 + COLS, g.N);
-            const bool rows = m0 < g.M;
-            if (RESID && rows && n0 < end) request(n0, m0);
+            bool rows = m0 < g.M;                          // the warp has something to finish
+            if (RESID && rows && n0 < end && t.tail < 0) request(n0, m0);
             const float ra = m0 + lane < g.M ? ld_chain(g.ra + m0 + lane) : 0.f;
             if (!mbar_wait_warp(tfull, tphase, abort_flag, g.err)) { ok = false; break; }
             tc_fence_after();
@@ -270,6 +297,31 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             if (lane == 0) mbar_arrive_remote_relaxed(leader);
             if (!mbar_wait_warp(vfull, tphase, abort_flag, g.err)) { ok = false; break; }
             tphase ^= 1u;
+            if (t.tail >= 0 && rows) {
+                const size_t piece = (size_t)(t.tail * 2 + (int)rank) * 8 + (warp - 4);
+                float4* parts = reinterpret_cast<float4*>(g.work) + piece * g.parts * (32 * 32) + lane;
+#pragma unroll
+                for (int c = 0; c < 128; c += 4)
+                    __stcg(parts + t.part * (32 * 32) + c / 4 * 32, make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
+                __threadfence();
+                __syncwarp();
+                unsigned before = 0;
+                if (lane == 0) before = atomicAdd(g.counters + piece, 1u);
+                rows = __shfl_sync(0xffffffffu, before, 0) + 1 == (unsigned)g.parts;
+                if (rows) {                                // the last one: all parts, in order
+                    __threadfence();
+                    if (lane == 0) g.counters[piece] = 0u;
+                    if (RESID && n0 < end) request(n0, m0);
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+                    for (int q = 0; q < g.parts; ++q)
+#pragma unroll
+                        for (int c = 0; c < 128; c += 4) {
+                            const float4 v = __ldcg(parts + q * (32 * 32) + c / 4 * 32);
+                            acc[c] += v.x; acc[c + 1] += v.y; acc[c + 2] += v.z; acc[c + 3] += v.w;
+                        }
+                }
+            }
             if (rows) {
                 // rw, bias and gate of the warp's columns; gated: of W_gate's, and behind them W_up's
                 const float* vec = GATED ? vectors + side * 64 : vectors + side * 3 * 128;
@@ -399,6 +451,23 @@ int resident_pairs(const Ctx* c, PairKernel k) {
     return n < c->num_sms / 2 ? n : c->num_sms / 2;
 }
 
+// Parts of K that `tail` tiles are split in, before whole tiles of kb stages: the parts'
+// stages, and what of their merging the next tile's stages do not hide.
+int tail_parts(int tail, int pairs, int kb) {
+    constexpr double kStage = 0.30, kMerge = 8.0, kPart = 0.8;     // us
+    int best = 1;
+    double least = kb * kStage;
+    for (int p = 2; p <= 8 && tail > 0 && tail * p <= pairs && 2 * p <= kb; ++p) {
+        const double merge = kMerge + p * kPart - kb * kStage;
+        const double est = (kb + p - 1) / p * kStage + (merge > 0.0 ? merge : 0.0);
+        if (est < least) {
+            least = est;
+            best = p;
+        }
+    }
+    return best;
+}
+
 template <typename T>
 wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
     static PerDevice<bool> fits;
@@ -442,11 +511,17 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
         !encode_tmap_2d(&tc, g.out, N, M, ldc, 128 / sizeof(T), 32, &why, kOut) ||
         !encode_tmap_2d(&tr, g.res ? g.res : g.out, N, M, ldc, 128 / sizeof(T), 32, &why, kOut))
         return fail(c, WDC_ERR_CUDA, why);
+    const int pairs = resident_pairs(c, k);
+    g.tail = (int)(tiles % pairs);
+    g.whole = (int)(tiles - g.tail);
+    g.parts = g.whole > 0 ? tail_parts(g.tail, pairs, g.kb) : 1;
+    if (g.parts > c->fp4_parts / (g.tail > 0 ? g.tail : 1)) g.parts = 1;
+    g.work = c->fp4_work;
+    g.counters = c->fp4_counters;
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_GEMM, s);
-        const int pairs = resident_pairs(c, k);
-        launch_kernel(k, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), kPairThreads, Pair4Cfg::SMEM, s, 2, ta, tw, tu, tsa,
+        launch_kernel(k, dim3(2 * (unsigned)(g.whole > 0 ? pairs : g.tail * g.parts)), kPairThreads, Pair4Cfg::SMEM, s, 2, ta, tw, tu, tsa,
                       tsw, tsu, tc, tr, g);
     }
     cudaError_t e = cudaGetLastError();

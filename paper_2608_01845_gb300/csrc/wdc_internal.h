@@ -179,6 +179,12 @@ struct Ctx {
     unsigned* attn_counters = nullptr; // a paged attention's units: parts done, 0 between launches
     void* attn_records = nullptr;      // and, of two tiles, the unit that each part is of
 
+    // split fp4 products: the sums of fp4_parts parts of tiles (256 x 256 fp32 each) and a
+    // counter of the parts done for each warp's piece of a tile, 0 between launches
+    float* fp4_work = nullptr;
+    unsigned* fp4_counters = nullptr;
+    int fp4_parts = 0;
+
     // graph rollout (device-side control flow), built on first use
     GraphRollout* grollout = nullptr;
 

@@ -113,7 +113,7 @@ def test_gemm(contexts, M, N, K, kind):
 
 
 SHAPES = [(3, 264, 576), (40, 392, 8256), (100, 1544, 4160), (520, 2312, 2112), (1030, 2056, 1088), (2309, 3080, 576),
-          (700, 12296, 320)]
+          (700, 12296, 320), (300, 1032, 16448)]                   # the last: tiles' sums split over K
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
@@ -203,6 +203,18 @@ def test_nonfinite_rows_stay_in_their_rows(contexts, M):
     assert np.isnan(got[[5, 11]]).all() and np.isnan(got[:, [20, 33]]).all() and not np.isfinite(got[9]).any()
     rest = np.delete(np.delete(got, [5, 9, 11], 0), [20, 33], 1)
     assert np.isfinite(rest).all() and np.allclose(rest, np.delete(np.delete(y, [5, 9, 11], 0), [20, 33], 1), rtol=1e-4, atol=1e-4)
+
+
+def test_split_sums_repeat_themselves(contexts):
+    """Parts of K are added in their order whichever comes last: the same bits every time, on any stream."""
+    A, W, y, mag = product_case(51, 1300, 1544, 8256)
+    a, w, outs = matrix(*A), matrix(*W), []
+    for i in range(6):
+        C = torch.empty(1300, 1544, device="cuda")
+        contexts["f32"].op_gemm_fp4(a, w, C)
+        outs.append(C)
+    assert (np.abs(host(outs[0]) - y) <= product_bound(y, mag, 8256) + 2.0 ** -24 * np.abs(y)).all()
+    assert all(torch.equal(outs[0], c) for c in outs[1:]) and contexts["f32"].device_errors() == 0
 
 
 # ---------------------------------------------------------------- residual and norm
