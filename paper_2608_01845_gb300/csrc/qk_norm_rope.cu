@@ -4,10 +4,12 @@
 //   a' = a cos - b sin, b' = b cos + a sin for each pair (a, b).
 // Bound by memory: each row is read once and written once, the angles of a
 // token are read once for a few of its heads.  A lane holds 16 bytes of a head, so a
-// head of 64 bf16 is 8 lanes and a sum over it three shuffles; a warp takes
-// kGroups neighbouring warp-widths of one token's heads, all loaded before the
-// first is reduced.  Sums, weights and angles are fp32; the one rounding is that
+// head of 64 bf16 is 8 lanes and a sum over it three shuffles; a warp takes a run
+// of one token's heads, kGroups warp-widths at a time, the next ones' loads under way
+// while these are worked on (the angles are the token's: loaded once a run).  Sums, weights and angles are fp32; the one rounding is that
 // of the result.
+#include <type_traits>
+
 #include "dit_kernels.cuh"
 #include "paged_index.h"
 
@@ -16,13 +18,16 @@ namespace wdc {
 namespace {
 
 constexpr int kGroups = 4;
-constexpr int kVtTokens = 64;          // tokens of a V^T tile
+// Tokens of a V^T tile (17776 x 48 heads of 64: with 64 tokens the tiles took 65 us).
+template <typename T>
+constexpr int kVtTokens = sizeof(T) == 2 ? 128 : 64;
 
 struct NormArgs {
     const void* qkv;
     long long ld;
     int T, heads, kv;
-    int chunks;                        // warps a token
+    int chunks;                        // of kGroups warp-widths, a token
+    int per, runs;                     // chunks a warp takes; warps a token
     const float *wq, *wk;
     float eps;
     const float2* rot;                 // null: no rotation
@@ -54,6 +59,9 @@ template <> struct Vec<float> {
         const float2 a = *reinterpret_cast<const float2*>(p), b = *reinterpret_cast<const float2*>(q);
         v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
     }
+    static __device__ __forceinline__ void widen(const uint4& u, float (&v)[4]) {
+        v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+    }
     static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
@@ -70,15 +78,19 @@ __device__ __forceinline__ void widen(uint32_t w, float& a, float& b) {
     a = __uint_as_float(w << 16);
     b = __uint_as_float(w & 0xffff0000u);
 }
+// 16 bytes as they lie, in one piece or in two halves.
+template <typename T> __device__ __forceinline__ uint4 load_bits(const T* p) { return *reinterpret_cast<const uint4*>(p); }
+template <typename T> __device__ __forceinline__ uint4 load_bits(const T* p, const T* q) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(q);
+    return make_uint4(a.x, a.y, b.x, b.y);
+}
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int E = 8;
     static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        widen(u.x, v[0], v[1]); widen(u.y, v[2], v[3]); widen(u.z, v[4], v[5]); widen(u.w, v[6], v[7]);
+        widen(*reinterpret_cast<const uint4*>(p), v);
     }
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, const __nv_bfloat16* q, float (&v)[8]) {
-        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(q);
-        widen(a.x, v[0], v[1]); widen(a.y, v[2], v[3]); widen(b.x, v[4], v[5]); widen(b.y, v[6], v[7]);
+    static __device__ __forceinline__ void widen(const uint4& u, float (&v)[8]) {
+        wdc::widen(u.x, v[0], v[1]); wdc::widen(u.y, v[2], v[3]); wdc::widen(u.z, v[4], v[5]); wdc::widen(u.w, v[6], v[7]);
     }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
         *reinterpret_cast<uint4*>(p) =
@@ -90,19 +102,20 @@ template <> struct Vec<__nv_bfloat16> {
     }
 };
 
-// One tile of V^T: kVtTokens tokens of one head through shared memory.
+// One tile of V^T: kTokens tokens of one head through shared memory.
 template <typename T, int D>
 __device__ void transpose_v(const NormArgs& a, int tile) {
     using V = Vec<T>;
     using Out = typename std::conditional<sizeof(T) == 2, __half, float>::type;
-    constexpr int LDS = kVtTokens + 4 / (int)sizeof(Out);      // (an odd number of words: columns meet different banks)
+    constexpr int kTokens = kVtTokens<T>;
+    constexpr int LDS = kTokens + 4 / (int)sizeof(Out);      // (an odd number of words: columns meet different banks)
     __shared__ alignas(16) Out sm[D * LDS];
-    const int tiles = (a.T + kVtTokens - 1) / kVtTokens;
-    const int head = tile / tiles, t0 = (tile - head * tiles) * kVtTokens;
-    const int n = min(kVtTokens, a.T - t0);
+    const int tiles = (a.T + kTokens - 1) / kTokens;
+    const int head = tile / tiles, t0 = (tile - head * tiles) * kTokens;
+    const int n = min(kTokens, a.T - t0);
     const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)(a.heads + a.kv + head) * D;
     bool sat = false;
-    constexpr int PER = D / V::E, N = kVtTokens * PER / 256;   // lanes a token; pieces a thread
+    constexpr int PER = D / V::E, N = kTokens * PER / 256;   // lanes a token; pieces a thread
     float v[N][V::E];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -124,7 +137,7 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
     __syncthreads();
     Out* dst = reinterpret_cast<Out*>(a.v) + (size_t)head * D * a.ldv + t0;
     if constexpr (sizeof(T) == 2) {
-        constexpr int VEC = kVtTokens / 8;                     // 16-byte pieces a row
+        constexpr int VEC = kTokens / 8;                     // 16-byte pieces a row
         for (int i = threadIdx.x; i < D * VEC; i += 256) {
             const int r = i / VEC, t = (i % VEC) * 8;
             const Out* s = sm + r * LDS + t;
@@ -136,16 +149,17 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
             }
         }
     } else {
-        for (int i = threadIdx.x; i < D * kVtTokens; i += 256) {
-            const int r = i / kVtTokens, t = i % kVtTokens;
+        for (int i = threadIdx.x; i < D * kTokens; i += 256) {
+            const int r = i / kTokens, t = i % kTokens;
             if (t < n) dst[(size_t)r * a.ldv + t] = sm[r * LDS + t];
         }
     }
 }
 
 // What turns the heads: nothing or one table of positions, or a table for each axis.
-template <typename T, int D, bool APPEND, bool PAIRS, bool AXES>
-__global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant__ NormArgs a) {
+// RUNS: a warp may have several chunks.
+template <typename T, int D, bool APPEND, bool PAIRS, bool AXES, bool RUNS>
+__global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __grid_constant__ NormArgs a) {
     using V = Vec<T>;
     constexpr int E = V::E, LPH = D / E, HPW = 32 / LPH;       // elements a lane, lanes a head, heads a warp-width
     chain_release();
@@ -163,9 +177,10 @@ __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant
     }
     const int lane = threadIdx.x & 31;
     const long long w = (long long)block * 8 + (threadIdx.x >> 5);
-    const long long tl = w / a.chunks;
+    const long long tl = w / a.runs;
     if (tl >= a.T) return;
-    const int t = (int)tl, chunk = (int)(w - tl * a.chunks);
+    const int t = (int)tl, chunk0 = (int)(w - tl * a.runs) * (RUNS ? a.per : 1);
+    const int chunk1 = RUNS ? min(chunk0 + a.per, a.chunks) : chunk0 + 1;
     const int n_heads = APPEND ? a.heads + 2 * a.kv : a.heads + a.kv;
     const int half = a.rot_dim >> 1, l = lane % LPH;
 
@@ -178,19 +193,20 @@ __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant
         ea = l < lanes ? l * (E / 2) : a.rot_dim + (l - lanes) * E;
         eb = l < lanes ? half + ea : ea + E / 2;
     }
-    float x[kGroups][E];
+    uint4 bits[kGroups];
     const T* row = reinterpret_cast<const T*>(a.qkv) + (size_t)t * a.ld;
+    auto load = [&](int chunk) {
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-        const int h = (chunk * kGroups + u) * HPW + lane / LPH;
-        if (h < n_heads) {
-            if constexpr (PAIRS) V::load(row + (size_t)h * D + ea, x[u]);
-            else V::load(row + (size_t)h * D + ea, row + (size_t)h * D + eb, x[u]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[u][i] = 0.f;
+        for (int u = 0; u < kGroups; ++u) {
+            const int h = (chunk * kGroups + u) * HPW + lane / LPH;
+            bits[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (h < n_heads) {
+                if constexpr (PAIRS) bits[u] = load_bits(row + (size_t)h * D + ea);
+                else bits[u] = load_bits(row + (size_t)h * D + ea, row + (size_t)h * D + eb);
+            }
         }
-    }
+    };
+    load(chunk0);
 
     // this token's place: its row of the cache and its position
     int place = t;
@@ -262,76 +278,83 @@ __global__ void __launch_bounds__(256, 4) norm_rope_kernel(const __grid_constant
         }
     }
 
+    for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+        uint4 now[kGroups];
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-        const int h = (chunk * kGroups + u) * HPW + lane / LPH;
-        float ss = 0.f;
+        for (int u = 0; u < kGroups; ++u) now[u] = bits[u];
+        if (RUNS && chunk + 1 < chunk1) load(chunk + 1);
 #pragma unroll
-        for (int i = 0; i < E; ++i) ss = fmaf(x[u][i], x[u][i], ss);
+        for (int u = 0; u < kGroups; ++u) {
+            const int h = (chunk * kGroups + u) * HPW + lane / LPH;
+            float x[E], ss = 0.f;
+            V::widen(now[u], x);
 #pragma unroll
-        for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        if (h >= n_heads) continue;
-        auto put = [&](T* head, const float (&v)[E]) {
-            if constexpr (PAIRS) V::store(head + ea, v);
-            else V::store(head + ea, head + eb, v);
-        };
-        if (APPEND && h >= a.heads + a.kv) {
-            const int g = h - a.heads - a.kv;
-            bool sat = false;
-            uint32_t p[E / 2];
+            for (int i = 0; i < E; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-            for (int i = 0; i < E; i += 2) {
-                const __half2 v = __halves2half2(to_vt_half(x[u][i], sat), to_vt_half(x[u][i + 1], sat));
-                p[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
-            }
-            if (keep) {
-                __half* dst = reinterpret_cast<__half*>(a.v) + (((slot + g) << a.page_log2) + in_page) * D;
-                if constexpr (E == 8) {
-                    if constexpr (PAIRS) {
-                        *reinterpret_cast<uint4*>(dst + ea) = make_uint4(p[0], p[1], p[2], p[3]);
-                    } else {
-                        *reinterpret_cast<uint2*>(dst + ea) = make_uint2(p[0], p[1]);
-                        *reinterpret_cast<uint2*>(dst + eb) = make_uint2(p[2], p[3]);
-                    }
+            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            if (h >= n_heads) continue;
+            auto put = [&](T* head, const float (&v)[E]) {
+                if constexpr (PAIRS) V::store(head + ea, v);
+                else V::store(head + ea, head + eb, v);
+            };
+            if (APPEND && h >= a.heads + a.kv) {
+                const int g = h - a.heads - a.kv;
+                bool sat = false;
+                uint32_t p[E / 2];
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    const __half2 v = __halves2half2(to_vt_half(x[i], sat), to_vt_half(x[i + 1], sat));
+                    p[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
                 }
-                if (sat) atomicOr(a.err, kErrVSaturated);
+                if (keep) {
+                    __half* dst = reinterpret_cast<__half*>(a.v) + (((slot + g) << a.page_log2) + in_page) * D;
+                    if constexpr (E == 8) {
+                        if constexpr (PAIRS) {
+                            *reinterpret_cast<uint4*>(dst + ea) = make_uint4(p[0], p[1], p[2], p[3]);
+                        } else {
+                            *reinterpret_cast<uint2*>(dst + ea) = make_uint2(p[0], p[1]);
+                            *reinterpret_cast<uint2*>(dst + eb) = make_uint2(p[2], p[3]);
+                        }
+                    }
+                    if (sat) atomicOr(a.err, kErrVSaturated);
+                }
+                continue;
             }
-            continue;
-        }
-        const float inv = rsqrtf(ss * (1.0f / D) + a.eps);     // (2 ulp; IEEE's root and quotient are 30 instructions)
-        float y[E];
-        const float* wt = h < a.heads ? a.wq : a.wk;
+            const float inv = rsqrtf(ss * (1.0f / D) + a.eps);     // (2 ulp; IEEE's root and quotient are 30 instructions)
+            float y[E];
+            const float* wt = h < a.heads ? a.wq : a.wk;
 #pragma unroll
-        for (int i = 0; i < E; ++i) y[i] = x[u][i] * inv;
-        if (wt) {
-            float f[E];
-            if constexpr (E == 8) {
-                Vec<float>::load(wt + ea, *reinterpret_cast<float(*)[4]>(&f[0]));
-                Vec<float>::load(wt + eb, *reinterpret_cast<float(*)[4]>(&f[4]));
+            for (int i = 0; i < E; ++i) y[i] = x[i] * inv;
+            if (wt) {
+                float f[E];
+                if constexpr (E == 8) {
+                    Vec<float>::load(wt + ea, *reinterpret_cast<float(*)[4]>(&f[0]));
+                    Vec<float>::load(wt + eb, *reinterpret_cast<float(*)[4]>(&f[4]));
+                } else {
+                    Vec<float>::load(wt + ea, wt + eb, f);
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) y[i] *= f[i];
+            }
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) {
+                    float& p = y[PAIRS ? 2 * i : i];
+                    float& q = y[PAIRS ? 2 * i + 1 : i + E / 2];
+                    const float c = p, d = q;
+                    p = c * cs[2 * i] - d * cs[2 * i + 1];
+                    q = d * cs[2 * i] + c * cs[2 * i + 1];
+                }
+            }
+            if (h < a.heads) {
+                put(reinterpret_cast<T*>(a.q) + (APPEND ? (size_t)t * a.heads + h : (size_t)h * a.T + t) * D, y);
             } else {
-                Vec<float>::load(wt + ea, wt + eb, f);
-            }
-#pragma unroll
-            for (int i = 0; i < E; ++i) y[i] *= f[i];
-        }
-        if (turned) {
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                float& p = y[PAIRS ? 2 * i : i];
-                float& q = y[PAIRS ? 2 * i + 1 : i + E / 2];
-                const float c = p, d = q;
-                p = c * cs[2 * i] - d * cs[2 * i + 1];
-                q = d * cs[2 * i] + c * cs[2 * i + 1];
-            }
-        }
-        if (h < a.heads) {
-            put(reinterpret_cast<T*>(a.q) + (APPEND ? (size_t)t * a.heads + h : (size_t)h * a.T + t) * D, y);
-        } else {
-            const int g = h - a.heads;
-            if constexpr (APPEND) {
-                if (keep) put(reinterpret_cast<T*>(a.k) + (((slot + g) << a.page_log2) + in_page) * D, y);
-            } else {
-                put(reinterpret_cast<T*>(a.k) + ((size_t)g * a.T + t) * D, y);
+                const int g = h - a.heads;
+                if constexpr (APPEND) {
+                    if (keep) put(reinterpret_cast<T*>(a.k) + (((slot + g) << a.page_log2) + in_page) * D, y);
+                } else {
+                    put(reinterpret_cast<T*>(a.k) + ((size_t)g * a.T + t) * D, y);
+                }
             }
         }
     }
@@ -342,17 +365,27 @@ wdc_status launch(Ctx* c, NormArgs& a, bool pairs, int vt_tiles, cudaStream_t s)
     constexpr int HPW = 32 / (D / Vec<T>::E);
     const int n_heads = APPEND ? a.heads + 2 * a.kv : a.heads + a.kv;
     a.chunks = (n_heads + kGroups * HPW - 1) / (kGroups * HPW);
-    const long long blocks = ((long long)a.T * a.chunks + 7) / 8;
+    // as many chunks a warp as leave four runs for each of the 24 warps an SM that the device holds
+    const long long most = (long long)a.T * a.chunks / (4 * 24 * c->num_sms);
+    a.per = most < 1 ? 1 : (most < a.chunks ? (int)most : a.chunks);
+    a.runs = (a.chunks + a.per - 1) / a.per;
+    const long long blocks = ((long long)a.T * a.runs + 7) / 8;
     if (blocks + vt_tiles > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^31 - 1 thread blocks");
     a.vt_tiles = (unsigned)vt_tiles;
     const dim3 grid((unsigned)(blocks + vt_tiles));
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_NORM, s);
-        if (a.axes > 0 && pairs) launch_kernel(norm_rope_kernel<T, D, APPEND, true, true>, grid, 256, 0, s, 1, a);
-        else if (a.axes > 0) launch_kernel(norm_rope_kernel<T, D, APPEND, false, true>, grid, 256, 0, s, 1, a);
-        else if (pairs) launch_kernel(norm_rope_kernel<T, D, APPEND, true, false>, grid, 256, 0, s, 1, a);
-        else launch_kernel(norm_rope_kernel<T, D, APPEND, false, false>, grid, 256, 0, s, 1, a);
+        auto go = [&](auto kernel) { launch_kernel(kernel, grid, 256, 0, s, 1, a); };
+        auto of = [&](auto p, auto x) {
+            constexpr bool P = decltype(p)::value, X = decltype(x)::value;
+            if (a.per > 1) go(norm_rope_kernel<T, D, APPEND, P, X, true>);
+            else go(norm_rope_kernel<T, D, APPEND, P, X, false>);
+        };
+        if (a.axes > 0 && pairs) of(std::true_type(), std::true_type());
+        else if (a.axes > 0) of(std::false_type(), std::true_type());
+        else if (pairs) of(std::true_type(), std::false_type());
+        else of(std::false_type(), std::false_type());
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("norm and rotation: ") + cudaGetErrorString(e));
@@ -424,7 +457,8 @@ wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int hea
     if (bf16 && T > 0x7fffffff - 7) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: T too large");
     a.q = q; a.k = k; a.v = vt;
     a.ldv = bf16 ? (T + 7) / 8 * 8 : T;
-    const long long tiles = vt ? (long long)((T - 1) / kVtTokens + 1) * kv : 0;
+    const int per_tile = bf16 ? kVtTokens<__nv_bfloat16> : kVtTokens<float>;
+    const long long tiles = vt ? (long long)((T - 1) / per_tile + 1) * kv : 0;
     if (tiles > 0x3fffffff) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^30 thread blocks");
     if (bf16)
         return d == 64 ? launch<__nv_bfloat16, 64, false>(c, a, n->interleaved, (int)tiles, s)
