@@ -820,11 +820,17 @@ class Context:
         if total is not None:
             t, ldt = _rows(what, "total", total, dt, shape, dev)
         sets = -(-M // rows_per_set) if rows_per_set else 1
-        vectors = [0, 0, 0]
-        for i, v in enumerate((gate, weight, shift)):
-            if v is not None:
-                _tensor(what, ("gate", "weight", "shift")[i], v, f32, (D,) if sets == 1 and v.dim() == 1 else (sets, D), dev)
-                vectors[i] = v.data_ptr()
+        g = w = h = 0
+        vector = lambda name, v: _tensor(what, name, v, f32, (D,) if sets == 1 and v.dim() == 1 else (sets, D), dev)
+        if gate is not None:
+            vector("gate", gate)
+            g = gate.data_ptr()
+        if weight is not None:
+            vector("weight", weight)
+            w = weight.data_ptr()
+        if shift is not None:
+            vector("shift", shift)
+            h = shift.data_ptr()
         if isinstance(out, Fp4Matrix):
             q4 = ctypes.addressof(self._fp4(what, "out", out, M, D))
         elif out.dtype is f8:
@@ -842,7 +848,7 @@ class Context:
         if M == 0:                                         # (empty tensors have no address)
             return
         # (packed at once: its eighteen fields set one by one took longer than the call)
-        n = AddNorm.from_buffer_copy(_ADD_NORM.pack(p, d, t, o, ldx, ldd, ldt, ldo, q8, sc, q4, *vectors,
+        n = AddNorm.from_buffer_copy(_ADD_NORM.pack(p, d, t, o, ldx, ldd, ldt, ldo, q8, sc, q4, g, w, h,
                                                     weight_offset, eps, rows_per_set, 1 if center else 0))
         self._check(LIB.wdc_op_add_norm(self._h, n, M, D, self._op_stream(stream)), what)
 
