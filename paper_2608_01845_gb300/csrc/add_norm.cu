@@ -58,6 +58,8 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
     const float n = count(warp), by_n = n > 0.f ? 1.0f / n : 0.f;
     const int other = lane & 15;                           // the warp whose statistics this lane joins
     const float n_other = other < warps ? count(other) : 0.f;
+    const bool wide_rows = is_wide(a.x) && is_wide(a.delta) && is_wide(a.total) && is_wide(a.out);
+    const bool wide_sets = is_wide(a.gate) && is_wide(a.weight) && is_wide(a.shift);
     Raw8<T> xr[V], dr[V];
     auto load = [&](unsigned m) {
         if (m >= M) return;
@@ -66,8 +68,8 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
 #pragma unroll
         for (int u = 0; u < V; ++u)
             if (col[u] < a.D) {
-                load_raw(x + col[u], xr[u]);
-                if (a.delta) load_raw(d + col[u], dr[u]);
+                load_once(x + col[u], xr[u], wide_rows);
+                if (a.delta) load_once(d + col[u], dr[u], wide_rows);
             }
     };
     unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
@@ -85,7 +87,7 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
                     float d[8], g[8];
                     widen8(dr[u], d);
                     if (a.gate) {
-                        load8(a.gate + set + col[u], g);
+                        load8(a.gate + set + col[u], g, wide_sets);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) g[i] = 1.f;
@@ -103,7 +105,7 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
             T* total = reinterpret_cast<T*>(a.total) + (size_t)m * a.ldt;
 #pragma unroll
             for (int u = 0; u < V; ++u)
-                if (col[u] < a.D) put8(total + col[u], v[u]);
+                if (col[u] < a.D) put8(total + col[u], v[u], wide_rows);
         }
         float mean = 0.f, ss = 0.f;
         if (a.center) {
@@ -152,13 +154,13 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
             }
             if (a.weight) {
                 float w[8];
-                load8(a.weight + set + col[u], w);
+                load8(a.weight + set + col[u], w, wide_sets);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[u][i] *= w[i] + a.offset;
             }
             if (a.shift) {
                 float w[8];
-                load8(a.shift + set + col[u], w);
+                load8(a.shift + set + col[u], w, wide_sets);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[u][i] += w[i];
             }
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
             T* out = reinterpret_cast<T*>(a.out) + (size_t)m * a.ldo;
 #pragma unroll
             for (int u = 0; u < V; ++u)
-                if (live && col[u] < a.D) put8(out + col[u], v[u]);
+                if (live && col[u] < a.D) put8(out + col[u], v[u], wide_rows);
         } else if constexpr (OUT == kE4m3) {
 #pragma unroll
             for (int u = 0; u < V; ++u) {

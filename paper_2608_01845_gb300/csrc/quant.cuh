@@ -35,7 +35,33 @@ __device__ __forceinline__ void load_raw(const float* p, Raw8<float>& r) {
     r.a = reinterpret_cast<const float4*>(p)[0];
     r.b = reinterpret_cast<const float4*>(p)[1];
 }
-__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, Raw8<__nv_bfloat16>& r) {
+// The same, and a store, in one instruction where the address is a multiple of 32 bytes
+// (`wide`): two of 16 bytes, 32 apart from lane to lane, pass through L1 in twice as many
+// cycles.
+__device__ __forceinline__ void load_raw(const float* p, Raw8<float>& r, bool wide) {
+    if (wide)
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(r.a.x), "=f"(r.a.y), "=f"(r.a.z), "=f"(r.a.w), "=f"(r.b.x), "=f"(r.b.y), "=f"(r.b.z), "=f"(r.b.w)
+                     : "l"(p));
+    else
+        load_raw(p, r);
+}
+// Rows that are read once leave L1 to what is read again.
+__device__ __forceinline__ void load_once(const float* p, Raw8<float>& r, bool wide) {
+    if (wide)
+        asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(r.a.x), "=f"(r.a.y), "=f"(r.a.z), "=f"(r.a.w), "=f"(r.b.x), "=f"(r.b.y), "=f"(r.b.z), "=f"(r.b.w)
+                     : "l"(p));
+    else
+        load_raw(p, r);
+}
+__device__ __forceinline__ void load_once(const __nv_bfloat16* p, Raw8<__nv_bfloat16>& r, bool) {
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w)
+                 : "l"(p));
+}
+__device__ __forceinline__ bool is_wide(const void* p) { return ((uintptr_t)p & 31) == 0; }
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, Raw8<__nv_bfloat16>& r, bool = true) {
     r.a = *reinterpret_cast<const uint4*>(p);
 }
 __device__ __forceinline__ void widen8(const Raw8<float>& r, float (&v)[8]) {
@@ -50,9 +76,9 @@ __device__ __forceinline__ void widen8(const Raw8<__nv_bfloat16>& r, float (&v)[
         v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8], bool wide = false) {
     Raw8<T> r;
-    load_raw(p, r);
+    load_raw(p, r, wide);
     widen8(r, v);
 }
 
@@ -156,11 +182,17 @@ __device__ __forceinline__ void e2m1_values(uint32_t q, float (&v)[8]) {
 }
 
 // A lane's 8 elements, rounded to the model's type.
-__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+__device__ __forceinline__ void put8(float* p, const float (&v)[8], bool wide = false) {
+    if (wide) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                     "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                     : "memory");
+        return;
+    }
     reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
-__device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8]) {
+__device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8], bool = true) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -46,13 +46,14 @@ __global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_con
     int col[V];
 #pragma unroll
     for (int u = 0; u < V; ++u) col[u] = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
+    const bool wide = is_wide(a.x);
     Raw8<T> raw[V];
     auto load = [&](unsigned m) {
         if (m >= M) return;
         const T* x = reinterpret_cast<const T*>(a.x) + (size_t)m * a.ldx;
 #pragma unroll
         for (int u = 0; u < V; ++u)
-            if (col[u] < a.K) load_raw(x + col[u], raw[u]);
+            if (col[u] < a.K) load_raw(x + col[u], raw[u], wide);
     };
     unsigned m = blockIdx.x * blockDim.y + threadIdx.y;
     int parity = 0;
