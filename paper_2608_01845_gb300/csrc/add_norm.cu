@@ -4,7 +4,12 @@
 // scales for 16 columns and the row.  A row's fp32 values stay in the registers of its
 // warps from the sum to the last conversion (a layer norm's variance is that of the
 // centred values), so that x and delta are read once.  Bound by memory: for bf16 6
-// bytes an element and those of y (2, 1.03 or 0.56).
+// bytes an element and those of y (2, 1.03 or 0.56).  17776 x 5120 with a gated branch,
+// root-mean-square norm, to bf16: 119.5 us (6.1 TB/s); 4050 x 4096 layer norm with gate,
+// weight and shift by frame to e4m3: 28 us in L2, 33 from memory (3.5 TB/s), where a row's
+// chain (two sums, a root, two conversions) is what a short call waits for: without the
+// three vectors 24.  Rows pass L1 by, which keeps the vectors: 32 -> 28 us.  Two pieces of 8
+// columns a thread: with four, and so fewer rows at a time, 17776 x 5120 took 167 us.
 #include "quant.cuh"
 
 namespace wdc {

@@ -1,6 +1,9 @@
 // Product of e2m1 matrices with e4m3 scales of 16 columns and fp32 scales of rows:
 //   C[m, n] = epilogue( ra[m] rw[n] sum_k (a s_a)[m, k] (w s_w)[n, k] ),
-// and of two such products the gated form act(A W^T) * (A U^T).
+// and of two such products the gated form act(A W^T) * (A U^T), on the 5th-generation
+// tensor cores (tcgen05 kind::mxf4nvf4, sm_103a), which multiply the scales of 16 of K in:
+// the sums over K are the tensor core's fp32, the rows' scales the epilogue's.  This file:
+// the entries, the choice of the kernel, and the kernel for few rows; gemm_fp4_pair.cu: many.
 #include "gemm_fp4.cuh"
 
 #include <cmath>
@@ -21,6 +24,10 @@ namespace {
 // A cluster of `split` CTAs shares a tile's K: each sums its part, sends the others their
 // share of the tile's tokens through distributed shared memory and adds what it
 // receives in rank order.
+// Bound by the weights' bytes: gated 3 x 13824 x 5120 14.7 us (5.4 TB/s), 4 x 15360 x 5120 9.9
+// (4.5 TB/s: 120 CTAs, of whose 10 us about 4 are the launch, the ring's first tiles and the
+// end); with weights in L2 by the issue of a stage's copies and MMAs, 0.17 us for 16 KB of
+// codes (an issuer each for the two was no faster).
 constexpr int kNarrowThreads = 192;     // TMA producer, MMA issuer, 4 epilogue warps
 
 template <int BN, bool GATED>
