@@ -21,8 +21,9 @@
 // x 4096 x 16384 330 us (7.2 PFLOP/s, four times the measured bf16 burst is 7.8).  A stage
 // takes about 600 cycles, its MMAs 512: the twelve copies of its scales pass through the same
 // queue (between MMAs, or from another warp, they cost more: 4864 x 4096 x 16384 85 us, then
-// 94 to 97); from a tile's last MMA to the next one's first pass about 1300 (commit, the reads
-// into registers 175, the arrival at the issuer, its first stage).  Tiles of 192 columns with
+// 94 to 97); from a tile's last MMA to the next one's first pass about 1000 (commit, the reads
+// into registers 175, the arrival at the issuer; the first copies are under way by then: gated
+// 1576 x 10240 x 4096 52.5 -> 51.6).  Tiles of 192 columns with
 // room for two left the scales 2.7 stages, and waiting for their columns cost more: 159 us.
 // Parts of the last tiles before the whole ones: 1350 x 4096 x 16384 44.6 -> 36 us.
 #include "gemm_fp4.cuh"
@@ -201,33 +202,51 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               int stage = 0;
               uint32_t phase = 0, tphase = 0;
               bool ok = true;                                // this lane's waits (elect_one)
+              // (a stage's columns are free once its tiles have landed: they could not have been
+              // loaded again before the MMAs that read the columns were done)
+              auto copies = [&]() {
+                  const uint32_t sc = tmem + (uint32_t)(256 + stage * C::SCALE_COLS);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                      const uint32_t at = stage * C::STAGE + k * kPiece4;
+                      tc_copy_scales2(sc + 12 * k, sdesc_at(ds, at));
+                      tc_copy_scales2(sc + 12 * k + 4, sdesc_at(ds, at + C::S_BYTES));
+                      tc_copy_scales2(sc + 12 * k + 8, sdesc_at(ds, at + 2 * C::S_BYTES));
+                  }
+              };
+              auto mmas = [&](bool first, bool last) {
+                  const uint32_t sc = tmem + (uint32_t)(256 + stage * C::SCALE_COLS);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                      tc_mma4_2(tmem, sdesc_at(da, stage * C::STAGE + k * 32), sdesc_at(db, stage * C::STAGE + k * 32), C::IDESC,
+                                sc + 12 * k, sc + 12 * k + 4, !first || k != 0);
+                  if (last) tc_commit2_mc(tfull, (uint16_t)0x3);
+                  tc_commit2_mc(&empty[stage], (uint16_t)0x3);
+              };
+              auto advance = [&]() {
+                  __syncwarp();
+                  if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+              };
               for (int j = 0; j < jobs; ++j) {
                   const Job t = job(j);
+                  // a tile's first copies are under way while the tile before is taken
+                  ok = ok && mbar_wait(&full[stage], phase, abort_flag, g.err);
+                  tc_fence_after();
+                  if (elect_one() && ok) copies();
+                  __syncwarp();
                   ok = ok && mbar_wait(tempty, tphase ^ 1u, abort_flag, g.err);
                   tphase ^= 1u;
-                  for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                  tc_fence_after();
+                  if (elect_one() && ok) mmas(true, t.kb0 + 1 == t.kb1);
+                  advance();
+                  for (int kb = t.kb0 + 1; kb < t.kb1; ++kb) {
                       ok = ok && mbar_wait(&full[stage], phase, abort_flag, g.err);
                       tc_fence_after();
                       if (elect_one() && ok) {
-                          // (the stage's columns are free: its tiles could not have been
-                          // loaded again before the MMAs that read them were done)
-                          const uint32_t sc = tmem + (uint32_t)(256 + stage * C::SCALE_COLS);
-#pragma unroll
-                          for (int k = 0; k < 4; ++k) {
-                              const uint32_t at = stage * C::STAGE + k * kPiece4;
-                              tc_copy_scales2(sc + 12 * k, sdesc_at(ds, at));
-                              tc_copy_scales2(sc + 12 * k + 4, sdesc_at(ds, at + C::S_BYTES));
-                              tc_copy_scales2(sc + 12 * k + 8, sdesc_at(ds, at + 2 * C::S_BYTES));
-                          }
-#pragma unroll
-                          for (int k = 0; k < 4; ++k)
-                              tc_mma4_2(tmem, sdesc_at(da, stage * C::STAGE + k * 32), sdesc_at(db, stage * C::STAGE + k * 32),
-                                        C::IDESC, sc + 12 * k, sc + 12 * k + 4, kb != t.kb0 || k != 0);
-                          if (kb + 1 == t.kb1) tc_commit2_mc(tfull, (uint16_t)0x3);
-                          tc_commit2_mc(&empty[stage], (uint16_t)0x3);
+                          copies();
+                          mmas(false, kb + 1 == t.kb1);
                       }
-                      __syncwarp();
-                      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                      advance();
                   }
               }
               if (elect_one()) tc_commit2_mc(mma_done, (uint16_t)0x1);
