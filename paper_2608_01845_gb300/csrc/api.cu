@@ -458,6 +458,9 @@ wdc_status wdc_device_errors(wdc_ctx* h, unsigned* bits) {
     WDC_CUDA_TRY(c, cudaDeviceSynchronize());
     WDC_CUDA_TRY(c, cudaMemcpy(bits, c->err, sizeof(unsigned), cudaMemcpyDeviceToHost));
     WDC_CUDA_TRY(c, cudaMemset(c->err, 0, sizeof(unsigned)));
+    // (a product whose wait gave up may have left some of its parts uncounted)
+    if ((*bits & kErrTimeout) && c->fp4_counters)
+        WDC_CUDA_TRY(c, cudaMemset(c->fp4_counters, 0, (size_t)c->fp4_parts * 16 * sizeof(unsigned)));
     return zeros_written(c);
 }
 

@@ -319,7 +319,7 @@ class RotAxes:
         self.device = dev = coords.get_device()
         _sizes("RotAxes", coords.shape[0])
         _tensor("RotAxes", "coords", coords, torch.int32, coords.shape, dev)
-        self.tables, self.coords, self.pairs = tables, coords, 0
+        self.tables, self.coords = tables, coords
         self.c = RotAxesC(len(tables), coords=coords.data_ptr() or None)
         for i, t in enumerate(tables):
             if t.dim() != 3 or t.shape[2] != 2:
@@ -327,7 +327,6 @@ class RotAxes:
             _sizes("RotAxes", t.shape[0], t.shape[1])
             _tensor("RotAxes", f"tables[{i}]", t, torch.float32, t.shape, dev)
             self.c.table[i], self.c.rows[i], self.c.pairs[i] = t.data_ptr() or None, t.shape[0], t.shape[1]
-            self.pairs += t.shape[1]
 
 
 def _tensor(what, name, t, dtype, shape, device, row_stride=False):
