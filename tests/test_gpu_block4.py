@@ -508,6 +508,97 @@ def test_captured_on_another_stream_and_replayed(contexts):
     assert all(torch.equal(x, y) for x, y in zip(first, b.results()))
 
 
+def test_two_contexts_at_once(contexts):
+    """Split products of two contexts on two streams, each with its own workspace."""
+    A, W, _, _ = product_case(51, 1300, 1544, 8256)
+    a, w = matrix(*A), matrix(*W)
+    both = [contexts["bf16"], wdc.Context(wdc.make_config(dtype=wdc.BF16, **MODEL), 2)]
+    outs = [[torch.empty(1300, 1544, dtype=torch.bfloat16, device="cuda") for _ in range(4)] for _ in both]
+    streams = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for i in range(4):
+        for c, o, st in zip(both, outs, streams):
+            c.op_gemm_fp4(a, w, o[i], stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(outs[0][0], t) for o in outs for t in o)
+    assert all(c.device_errors() == 0 for c in both)
+
+
+def test_after_a_wait_that_gave_up(contexts):
+    """The context is as before: a split product's counters too."""
+    ctx = contexts["f32"]
+    A, W, y, mag = product_case(51, 1300, 1544, 8256)
+    ctx.selftest_wait_timeout(1000)
+    assert ctx.device_errors() == 1
+    C = torch.empty(1300, 1544, device="cuda")
+    ctx.op_gemm_fp4(matrix(*A), matrix(*W), C)
+    assert (np.abs(host(C) - y) <= product_bound(y, mag, 8256) + 2.0 ** -24 * np.abs(y)).all() and ctx.device_errors() == 0
+
+
+# ---------------------------------------------------------------- offsets past 32 bits
+def ends(t, n=3):
+    return torch.cat([t[:n], t[-n:]])
+
+
+def test_rows_past_32_bits(contexts):
+    """More than 2^31 elements: the first and the last rows of a matrix of codes and back."""
+    ctx, M, K = contexts["bf16"], 66000, 32832
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    rows = rows_of(5, 6, K, "bf16")
+    x[:3], x[-3:] = dev(rows[:3], torch.bfloat16), dev(rows[3:], torch.bfloat16)
+    q = wdc.Fp4Matrix.empty(M, K)
+    ctx.op_quantize_fp4(x, q)
+    x.fill_(7.0)
+    ctx.op_dequantize_fp4(q, x)
+    want = block4.values(*block4.quantize(rows))
+    assert (np.abs(host(ends(x)) - want) <= (2.0 ** -8 + 2.0 ** -22) * np.abs(want)).all()
+    assert np.array_equal(block4.unpack(ends(q.codes).cpu().numpy()), block4.quantize(rows)[0])
+    assert bool((x[3:-3] == 0).all())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_results_past_32_bits(contexts, gated):
+    ctx, M, N, K = contexts["bf16"], 66000, 32832, 64
+    A, W = block4.quantize(rows_of(6, 6, K, "bf16")), block4.quantize(rows_of(7, 4, K, "bf16"))
+    a = wdc.Fp4Matrix(*(torch.zeros_like(t) for t in (lambda m: (m.codes, m.scale, m.row_scale))(wdc.Fp4Matrix.empty(M, K))))
+    w = wdc.Fp4Matrix(*(torch.zeros_like(t) for t in (lambda m: (m.codes, m.scale, m.row_scale))(wdc.Fp4Matrix.empty(N, K))))
+    for m, v, n in ((a, A, M), (w, W, N)):
+        k = len(v[2]) // 2
+        at = np.concatenate([np.arange(k), np.arange(n - k, n)])
+        m.codes[at], m.row_scale[at] = torch.from_numpy(block4.pack(v[0])).cuda(), dev(v[2])
+        r, j = at[:, None], np.arange(K // 16)[None]
+        m.scale.view(torch.uint8)[r // 128, j // 4, r % 32 * 16 + r // 32 % 4 * 4 + j % 4] = dev(v[1], F8).view(torch.uint8)
+    C = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    if gated:
+        ctx.op_gated_fp4(a, w, w, C)
+    else:
+        ctx.op_gemm_fp4(a, w, C)
+    y = block4.values(*A) @ block4.values(*W).T
+    mag = np.abs(block4.values(*A)) @ np.abs(block4.values(*W)).T
+    e = product_bound(y, mag, K)
+    if gated:
+        f = block4.silu(y)
+        y, e = f * y, (1.13 * e + 2.0 ** -18 * np.abs(f) + 1e-6) * np.abs(y) + np.abs(f) * e + 3 * e * e
+    got = host(ends(ends(C).t().contiguous(), 2).t())
+    assert (np.abs(got - y) <= e + 2.0 ** -8 * np.abs(y)).all()
+    assert bool((C[3:-3] == 0).all()) and bool((C[:, 2:-2] == 0).all()) and ctx.device_errors() == 0
+
+
+def test_norm_past_32_bits(contexts):
+    ctx, M, D = contexts["bf16"], 140000, 16384
+    x = torch.ones(M, D, dtype=torch.bfloat16, device="cuda")
+    rows = synth.bf16_round(synth.normal(8, (6, D)))
+    x[:3], x[-3:] = dev(rows[:3], torch.bfloat16), dev(rows[3:], torch.bfloat16)
+    q, s = torch.empty(M, D, dtype=F8, device="cuda"), torch.empty(D // 128, M, device="cuda")
+    ctx.op_add_norm(x, q, scale=s)
+    ctx.op_add_norm(x, x)                                          # in place
+    _, _, y, err = norm_errors(rows, {}, 0.0, False, 1e-6, 0)
+    assert (np.abs(host(ends(x)) - y) <= err + 2.0 ** -8 * np.abs(y)).all()
+    step = host(ends(s.t().contiguous())).repeat(128, 1)
+    assert (np.abs(host(ends(q)) * step - y) <= err + 2.0 ** -20 * np.abs(y) + np.maximum(2.0 ** -4 * (np.abs(y) + err), 2.0 ** -10 * step)).all()
+    assert bool((x[3:-3] == 1).all())
+
+
 # ---------------------------------------------------------------- refusals
 def test_refusals_of_the_library(contexts):
     ctx = contexts["bf16"]
