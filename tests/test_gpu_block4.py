@@ -2,6 +2,7 @@
 and the gated one, the residual's norm, rotation by several axes, and all of them
 together, at the sizes and values where they can go wrong."""
 import ctypes
+import functools
 
 import numpy as np
 import pytest
@@ -113,17 +114,23 @@ def test_gemm(contexts, M, N, K, kind):
 
 
 SHAPES = [(3, 264, 576), (40, 392, 8256), (100, 1544, 4160), (520, 2312, 2112), (1030, 2056, 1088), (2309, 3080, 576),
-          (700, 12296, 320), (300, 1032, 16448)]                   # the last: tiles' sums split over K
+          (700, 12296, 320), (300, 1032, 16448)]
+
+
+@functools.lru_cache(1)
+def epilogue_case(M, N, K):
+    A, W, y, mag = product_case(31, M, N, K)
+    return A, W, matrix(*A), matrix(*W), y, mag
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", SHAPES)
 @pytest.mark.parametrize("mode", ["bias", "gelu", "resid", "resid_gelu", "gateless"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
 def test_gemm_epilogues(contexts, M, N, K, mode, kind):
     """The epilogue's own error: 1.13 (GELU's steepest slope) of the sum's, 2^-18 of
     GELU's value for its exponential and quotient, the gate's multiple of both."""
     ctx = contexts[kind]
-    A, W, y, mag = product_case(31, M, N, K)
+    _, _, da, dw, y, mag = epilogue_case(M, N, K)
     b, g = synth.normal(3, (N,), 0.5), synth.normal(5, (N,))
     r = synth.bf16_round(synth.normal(4, (M, N)))
     err = product_bound(y, mag, K)
@@ -139,7 +146,7 @@ def test_gemm_epilogues(contexts, M, N, K, mode, kind):
         if mode != "gateless":
             y, err, kw["gate"] = g * y, np.abs(g) * err + 2.0 ** -22 * np.abs(g * y), dev(g)
         y = r + y
-    ctx.op_gemm_fp4(matrix(*A), matrix(*W), C, **kw)
+    ctx.op_gemm_fp4(da, dw, C, **kw)
     assert ctx.device_errors() == 0
     assert (np.abs(host(C) - y) <= err + HALF[kind] * np.abs(y) + 2.0 ** -22 * np.abs(y)).all()
 
@@ -147,15 +154,22 @@ def test_gemm_epilogues(contexts, M, N, K, mode, kind):
 GATED = [(1, 8, 64), (5, 136, 192), (17, 256, 4160), (64, 1032, 1024), (100, 264, 2112), (129, 520, 576)] + SHAPES
 
 
+@functools.lru_cache(1)
+def gated_case(M, N, K):
+    A, W, da, dw, g, gmag = epilogue_case(M, N, K)
+    U = block4.quantize(synth.bf16_round(synth.normal(77, (N, K), K ** -0.5)))
+    a, u = block4.values(*A), block4.values(*U)
+    return da, dw, matrix(*U), g, gmag, a @ u.T, np.abs(a) @ np.abs(u).T
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K,bias", [s + (False,) for s in GATED] + [s + (True,) for s in SHAPES])
 @pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("M,N,K", GATED)
 def test_gated(contexts, M, N, K, gelu, bias, kind):
     """f's slope is at most 1.13, its own error 2^-18 of its value; the product adds each factor's."""
     ctx = contexts[kind]
-    A, W, g, gmag = product_case(31, M, N, K)
-    U = block4.quantize(synth.bf16_round(synth.normal(77, (N, K), K ** -0.5)))
-    u, umag = block4.values(*A) @ block4.values(*U).T, np.abs(block4.values(*A)) @ np.abs(block4.values(*U)).T
+    da, dw, du, g, gmag, u, umag = gated_case(M, N, K)
     ge, ue = product_bound(g, gmag, K), product_bound(u, umag, K)
     kw = dict(gelu=gelu)
     if bias:
@@ -166,7 +180,7 @@ def test_gated(contexts, M, N, K, gelu, bias, kind):
     fe = 1.13 * ge + 2.0 ** -18 * np.abs(f) + 1e-6
     want = f * u
     buf = torch.full((M + 1, N), 7.0, dtype=DTYPES[kind], device="cuda")
-    ctx.op_gated_fp4(matrix(*A), matrix(*W), matrix(*U), buf[:M], **kw)
+    ctx.op_gated_fp4(da, dw, du, buf[:M], **kw)
     assert ctx.device_errors() == 0
     err = fe * np.abs(u) + np.abs(f) * ue + fe * ue + 2.0 ** -22 * np.abs(want) + HALF[kind] * np.abs(want)
     assert (np.abs(host(buf[:M]) - want) <= err).all()
@@ -205,15 +219,56 @@ def test_nonfinite_rows_stay_in_their_rows(contexts, M):
     assert np.isfinite(rest).all() and np.allclose(rest, np.delete(np.delete(y, [5, 9, 11], 0), [20, 33], 1), rtol=1e-4, atol=1e-4)
 
 
+# (16, 32, 64 and 128 tokens a tile, alone and with K over 2, 4 and 8 CTAs, one of which ends short)
+FEW = [(1, 8, 4160), (3, 2056, 4160), (2, 8200, 8256), (17, 8, 64), (17, 8200, 8256), (20, 2056, 4160), (33, 8, 4160), (50, 2056, 4160),
+       (60, 8200, 8256), (65, 8, 4160), (90, 2056, 8256), (65, 8200, 16448), (130, 264, 4160)]
+
+
+@functools.lru_cache(1)
+def few_case(M, N, K):
+    A, W, y, mag = product_case(61, M, N, K)
+    return matrix(*A), matrix(*W), y, mag
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", FEW)                     # (the slowest of the three to vary)
+def test_every_way_for_few_rows(contexts, M, N, K, gated, kind):
+    ctx = contexts[kind]
+    a, w, y, mag = few_case(M, N, K)
+    e = product_bound(y, mag, K)
+    buf = torch.full((M + 1, N), 7.0, dtype=DTYPES[kind], device="cuda")
+    if gated:
+        ctx.op_gated_fp4(a, w, w, buf[:M])
+        f = block4.silu(y)
+        y, e = f * y, (1.13 * e + 2.0 ** -18 * np.abs(f) + 1e-6) * np.abs(y) + np.abs(f) * e + 3 * e * e + 2.0 ** -22 * np.abs(f * y)
+    else:
+        r = synth.bf16_round(synth.normal(4, (M, N)))
+        buf[:M] = dev(r)
+        ctx.op_gemm_fp4(a, w, buf[:M], res=buf[:M])
+        y, e = r + y, e + 2.0 ** -22 * np.abs(r)
+    assert ctx.device_errors() == 0
+    assert (np.abs(host(buf[:M]) - y) <= e + HALF[kind] * np.abs(y)).all()
+    assert bool((buf[M:] == 7.0).all())
+
+
+SPLIT = (1300, 3592, 8256)      # 90 tiles of 256 x 256 on 76 pairs: 14 are split over K
+
+
+@functools.lru_cache(1)
+def split_case():
+    return product_case(51, *SPLIT)
+
+
 def test_split_sums_repeat_themselves(contexts):
     """Parts of K are added in their order whichever comes last: the same bits every time, on any stream."""
-    A, W, y, mag = product_case(51, 1300, 1544, 8256)
+    A, W, y, mag = split_case()
     a, w, outs = matrix(*A), matrix(*W), []
     for i in range(6):
-        C = torch.empty(1300, 1544, device="cuda")
+        C = torch.empty(*SPLIT[:2], device="cuda")
         contexts["f32"].op_gemm_fp4(a, w, C)
         outs.append(C)
-    assert (np.abs(host(outs[0]) - y) <= product_bound(y, mag, 8256) + 2.0 ** -24 * np.abs(y)).all()
+    assert (np.abs(host(outs[0]) - y) <= product_bound(y, mag, SPLIT[2]) + 2.0 ** -24 * np.abs(y)).all()
     assert all(torch.equal(outs[0], c) for c in outs[1:]) and contexts["f32"].device_errors() == 0
 
 
@@ -510,10 +565,10 @@ def test_captured_on_another_stream_and_replayed(contexts):
 
 def test_two_contexts_at_once(contexts):
     """Split products of two contexts on two streams, each with its own workspace."""
-    A, W, _, _ = product_case(51, 1300, 1544, 8256)
+    A, W, _, _ = split_case()
     a, w = matrix(*A), matrix(*W)
     both = [contexts["bf16"], wdc.Context(wdc.make_config(dtype=wdc.BF16, **MODEL), 2)]
-    outs = [[torch.empty(1300, 1544, dtype=torch.bfloat16, device="cuda") for _ in range(4)] for _ in both]
+    outs = [[torch.empty(*SPLIT[:2], dtype=torch.bfloat16, device="cuda") for _ in range(4)] for _ in both]
     streams = [torch.cuda.Stream() for _ in both]
     torch.cuda.synchronize()
     for i in range(4):
@@ -527,12 +582,12 @@ def test_two_contexts_at_once(contexts):
 def test_after_a_wait_that_gave_up(contexts):
     """The context is as before: a split product's counters too."""
     ctx = contexts["f32"]
-    A, W, y, mag = product_case(51, 1300, 1544, 8256)
+    A, W, y, mag = split_case()
     ctx.selftest_wait_timeout(1000)
     assert ctx.device_errors() == 1
-    C = torch.empty(1300, 1544, device="cuda")
+    C = torch.empty(*SPLIT[:2], device="cuda")
     ctx.op_gemm_fp4(matrix(*A), matrix(*W), C)
-    assert (np.abs(host(C) - y) <= product_bound(y, mag, 8256) + 2.0 ** -24 * np.abs(y)).all() and ctx.device_errors() == 0
+    assert (np.abs(host(C) - y) <= product_bound(y, mag, SPLIT[2]) + 2.0 ** -24 * np.abs(y)).all() and ctx.device_errors() == 0
 
 
 # ---------------------------------------------------------------- offsets past 32 bits
