@@ -260,6 +260,8 @@ wdc_status op_add_norm(Ctx* c, const wdc_add_norm* n, int M, int D, cudaStream_t
     const int kinds = (n->out != nullptr) + (n->q8 != nullptr) + (n->q4 != nullptr);
     if (kinds != 1) return fail(c, WDC_ERR_INVALID_ARG, "residual norm: one of out, q8 and q4 is wanted");
     if (n->q4 && D % 64) return fail(c, WDC_ERR_UNSUPPORTED, "residual norm: e2m1 needs D % 64 == 0");
+    if (n->total && (n->total == n->out || n->total == n->q8))
+        return fail(c, WDC_ERR_INVALID_ARG, "residual norm: total and the result must be two places");
     if (n->gate && !n->delta) return fail(c, WDC_ERR_INVALID_ARG, "residual norm: a gate without a branch");
     if (n->ldx < D || (n->delta && n->ldd < D) || (n->total && n->ldt < D) || (n->out && n->ldo < D))
         return fail(c, WDC_ERR_INVALID_ARG, "residual norm: row stride below D");

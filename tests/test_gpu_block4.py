@@ -379,6 +379,30 @@ def test_add_norm_forms(contexts):
     assert np.allclose(host(C), a @ w.T, rtol=1e-4, atol=1e-4)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_addresses_that_are_multiples_of_16_bytes_only(contexts, kind):
+    """Rows and vectors that do not start on 32 bytes: the same bits as those that do."""
+    ctx, dt, D = contexts[kind], DTYPES[kind], 1088
+    x, kw = norm_case(9, D, kind, True, 4)
+    def moved(t, skip):
+        b = torch.full((t.shape[0] * (t.shape[1] + 16 * (t.dtype == dt)) + 64,), 3.0, dtype=t.dtype, device="cuda")
+        v = b[skip:].as_strided(t.shape, (t.shape[1] + 16 * (t.dtype == dt and t.shape[0] == 9), 1))
+        v.copy_(t)
+        assert v.data_ptr() % 32 == 16
+        return v
+    got = []
+    for shift in (False, True):
+        put = (lambda t: moved(t, 4 if t.dtype == torch.float32 else 8)) if shift else (lambda t: t)
+        d = {n: put(v) for n, v in to_device(kw, dt).items()}
+        xd, out, total, q = put(dev(x, dt)), put(dev(np.zeros((9, D)), dt)), put(dev(np.zeros((9, D)), dt)), wdc.Fp4Matrix.empty(9, D)
+        ctx.op_add_norm(xd, out, total=total, rows_per_set=4, center=True, **d)
+        ctx.op_quantize_fp4(xd, q)
+        got.append([out.clone(), total.clone(), q.codes, q.scale.view(torch.uint8), q.row_scale])
+        ctx.op_dequantize_fp4(q, out)
+        got[-1].append(out.clone())
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_add_norm_of_zeros_and_nonfinite_rows(contexts):
     ctx = contexts["f32"]
     x = np.ones((5, 256), np.float32)
@@ -689,9 +713,9 @@ def test_refusals_of_the_library(contexts):
     for want, M, D, kw in [(1, -1, 64, {}), (1, 4, 0, {}), (3, 4, 72, dict(ldx=72, ldo=72)), (3, 1, 16400, dict(ldx=16400, ldo=16400)), (1, 4, 64, dict(eps=-1.0)),
                            (1, 4, 64, dict(eps=float("nan"))), (1, 4, 64, dict(rows_per_set=-1)), (1, 4, 64, dict(out=None)),
                            (1, 4, 64, dict(q8=p, scale=p)), (1, 4, 64, dict(out=None, q8=p)), (1, 4, 64, dict(gate=p)), (1, 4, 64, dict(ldx=56)),
-                           (3, 4, 64, dict(ldo=68)), (1, 4, 64, dict(delta=p, ldd=32)), (1, 4, 64, dict(total=p)), (1, 4, 64, dict(x=p + 4)),
+                           (3, 4, 64, dict(ldo=68)), (1, 4, 64, dict(delta=p, ldd=32)), (1, 4, 64, dict(total=p + 512)), (1, 4, 64, dict(x=p + 4)),
                            (1, 4, 64, dict(x=None)), (3, 4, 80, dict(ldx=80, out=None, q4=q4)), (1, 4, 64, dict(out=None, q4=ctypes.pointer(off))),
-                           (1, 4, 64, dict(weight=p + 4)), (0, 0, 64, {})]:
+                           (1, 4, 64, dict(weight=p + 4)), (1, 4, 64, dict(total=p, ldt=64)), (0, 0, 64, {})]:
         assert L.wdc_op_add_norm(ctx._h, wdc.AddNorm(**dict(good, **kw)), M, D, s) == want, (M, D, kw)
     assert L.wdc_op_add_norm(ctx._h, None, 4, 64, s) == 1
 
