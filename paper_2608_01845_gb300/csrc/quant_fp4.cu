@@ -5,8 +5,8 @@
 //   value = code * (s * row).
 // The row's scale needs the whole row before the first code: a row stays in the
 // registers of its warps between the two, so x is read once.  Bound by memory (2.56
-// bytes an element for bf16, 4.56 for fp32) where rows are fp32: 4276 x 12288 to codes 47
-// us (5.1 TB/s) and back 38 (6.3).  bf16 rows are bound by the conversions, about 130
+// bytes an element for bf16, 4.56 for fp32) where rows are fp32: 4276 x 12288 to codes 44
+// us (5.5 TB/s; 48 with 4 pieces of 8 columns a thread) and back 38 (6.3).  bf16 rows are bound by the conversions, about 130
 // instructions for 8 columns with the row's: 17776 x 4096 to codes 49 us (3.8 TB/s), back 29
 // (6.4); with 4 pieces of 8 columns a thread instead of 2, a row of fewer threads, 54 ->
 // 49.  4 x 5120: 1.8 us either way, a launch.
@@ -28,7 +28,9 @@ struct Quant4Args {
 };
 
 constexpr int kHeld = 4;                           // pieces of 8 columns a thread holds at most
-constexpr int kMaxThreads = 512;                   // of a row
+constexpr int kMaxThreads = 512;                   // of a row of bf16; of fp32, twice as many with half the pieces
+template <typename T>
+constexpr int kRowThreads = sizeof(T) == 2 ? kMaxThreads : 2 * kMaxThreads;
 constexpr int kRowsAtOnce = 8;                     // of a block whose rows have a warp each
 
 __device__ __forceinline__ float warp_max(float a) {
@@ -41,8 +43,8 @@ __device__ __forceinline__ float warp_max(float a) {
 // kRowsAtOnce) one a warp; a thread has V pieces of 8 columns, and the next row's loads
 // are under way while one is worked on.  Rows past M (of the last 128) get scales of zero.
 template <typename T, int V>
-__global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_constant__ Quant4Args a) {
-    __shared__ float tops[2][kMaxThreads / 32];
+__global__ void __launch_bounds__(kRowThreads<T>) quantize4_kernel(const __grid_constant__ Quant4Args a) {
+    __shared__ float tops[2][32];
     chain_release();
     chain_wait();
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
@@ -80,9 +82,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize4_kernel(const __grid_con
         if (warps > 1) {
             if (lane == 0) tops[parity][threadIdx.x >> 5] = top;
             __syncthreads();
-            top = (lane & 15) < warps ? tops[parity][lane & 15] : 0.f;
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = warp_max(lane < warps ? tops[parity][lane] : 0.f);
         }
         const Row4 row(top);
         uint8_t* codes = a.codes + (size_t)m * (unsigned)a.K / 2;
@@ -175,7 +175,7 @@ template <typename T, int V>
 void launch_held(Ctx* c, const Quant4Args& a, int warps, cudaStream_t s) {
     const int per = warps == 1 ? kRowsAtOnce : 1;
     const long long rows = ((long long)(a.M - 1) / 128 + 1) * 128, blocks = (rows + per - 1) / per;
-    static PerDevice<int> held[kMaxThreads / 32 + 1];
+    static PerDevice<int> held[33];
     const int most = held[warps].get(c->device, [&](int& n) {
         n = resident_blocks(c, quantize4_kernel<T, V>, 32 * warps * per);
         return true;
@@ -186,15 +186,16 @@ void launch_held(Ctx* c, const Quant4Args& a, int warps, cudaStream_t s) {
 template <typename T>
 wdc_status launch(Ctx* c, const Quant4Args& a, cudaStream_t s) {
     const int eights = a.K / 8;                    // (bf16: wide threads, see above; fp32's hold twice the registers)
-    const int v = eights <= 32 ? 1 : (eights <= (sizeof(T) == 2 ? 64 : 2 * kMaxThreads) ? 2 : kHeld), warps = (eights + 32 * v - 1) / (32 * v);
+    const int most = sizeof(T) == 2 ? kHeld : 2;
+    const int v = eights <= 32 ? 1 : (eights <= 64 ? 2 : most), warps = (eights + 32 * v - 1) / (32 * v);
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_OTHER, s);
-        if (eights > kHeld * kMaxThreads)                  // (a block a row, those behind M of the last 128 too)
+        if (eights > most * kRowThreads<T>)                  // (a block a row, those behind M of the last 128 too)
             launch_kernel(quantize4_wide_kernel<T>, dim3(((unsigned)a.M + 127) / 128 * 128), 512, 0, s, 1, a);
         else if (v == 1) launch_held<T, 1>(c, a, warps, s);
         else if (v == 2) launch_held<T, 2>(c, a, warps, s);
-        else launch_held<T, kHeld>(c, a, warps, s);
+        else if constexpr (sizeof(T) == 2) launch_held<T, kHeld>(c, a, warps, s);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 quantize: ") + cudaGetErrorString(e));
