@@ -18,9 +18,10 @@ namespace wdc {
 namespace {
 
 constexpr int kGroups = 4;
-// Tokens of a V^T tile (17776 x 48 heads of 64: with 64 tokens the tiles took 65 us).
-template <typename T>
-constexpr int kVtTokens = sizeof(T) == 2 ? 128 : 64;
+// Tokens of a V^T tile (17776 x 48 heads of 64: tiles of 64 tokens took 65 us beside the
+// norms, of 128 48, of 256 43).
+template <typename T, int D>
+constexpr int kVtTokens = sizeof(T) == 2 ? 16384 / D : 64;
 
 struct NormArgs {
     const void* qkv;
@@ -107,7 +108,7 @@ template <typename T, int D>
 __device__ void transpose_v(const NormArgs& a, int tile) {
     using V = Vec<T>;
     using Out = typename std::conditional<sizeof(T) == 2, __half, float>::type;
-    constexpr int kTokens = kVtTokens<T>;
+    constexpr int kTokens = kVtTokens<T, D>;
     constexpr int LDS = kTokens + 4 / (int)sizeof(Out);      // (an odd number of words: columns meet different banks)
     __shared__ alignas(16) Out sm[D * LDS];
     const int tiles = (a.T + kTokens - 1) / kTokens;
@@ -457,7 +458,7 @@ wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int hea
     if (bf16 && T > 0x7fffffff - 7) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: T too large");
     a.q = q; a.k = k; a.v = vt;
     a.ldv = bf16 ? (T + 7) / 8 * 8 : T;
-    const int per_tile = bf16 ? kVtTokens<__nv_bfloat16> : kVtTokens<float>;
+    const int per_tile = bf16 ? (d == 64 ? kVtTokens<__nv_bfloat16, 64> : kVtTokens<__nv_bfloat16, 128>) : kVtTokens<float, 64>;
     const long long tiles = vt ? (long long)((T - 1) / per_tile + 1) * kv : 0;
     if (tiles > 0x3fffffff) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^30 thread blocks");
     if (bf16)
