@@ -28,11 +28,15 @@ namespace {
 // (4.5 TB/s: 120 CTAs, of whose 10 us about 4 are the launch, the ring's first tiles and the
 // end); with weights in L2 by the issue of a stage's copies and MMAs, 0.17 us for 16 KB of
 // codes (an issuer each for the two was no faster).
-constexpr int kNarrowThreads = 192;     // TMA producer, MMA issuer, 4 epilogue warps
 
 template <int BN, bool GATED>
 struct Narrow4Cfg {
     static constexpr int WS = GATED ? 2 : 1;                           // weights
+    // Epilogue warps for each quarter of the lanes, which take 16 tokens by turns: 128 x 4096 x
+    // 4096 with the residual 15.4 us with one, 11.0 with two, 9.2 with four; 64 x 4096 x 16384,
+    // whose K is split, 9.8, 9.1 and 9.8.
+    static constexpr int TURNS = BN == 16 ? 1 : (BN == 128 ? 4 : 2);
+    static constexpr int THREADS = 64 + 128 * TURNS;                   // TMA producer, MMA issuer, epilogue
     static constexpr uint32_t W_BYTES = 128 * 128, A_BYTES = BN * 128, S_BYTES = 4 * kPiece4;
     static constexpr uint32_t STAGE = WS * W_BYTES + A_BYTES + (WS + 1) * S_BYTES;
     static constexpr int SCALE_COLS = 16 * (WS + 1);                   // of a stage, in tensor memory
@@ -47,7 +51,7 @@ struct Narrow4Cfg {
 };
 
 template <typename T, int BN, bool GATED>
-__global__ void __launch_bounds__(kNarrowThreads, 1)
+__global__ void __launch_bounds__(Narrow4Cfg<BN, GATED>::THREADS, 1)
     gemm4_narrow_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmU,
                         const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmSW,
                         const __grid_constant__ CUtensorMap tmSU, const __grid_constant__ CUtensorMap tmSA,
@@ -163,6 +167,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
     }
 
     const int lg = warp & 3;                               // TMEM lane quarter this warp may access
+    const int turn = (warp - 2) >> 2;                      // and which of its warps it is
     const int row = lg * 32 + lane, n = nb * 128 + row;
     bool ok = true;
     float rw = 0.f, ru = 0.f, bias = 0.f, up_bias = 0.f, gate = 1.f;
@@ -170,7 +175,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
         // (fetched where they are used, a group of 16 tokens behind the other, they took 1 us each)
         const int c = threadIdx.x - 64;
         if (c < BN) token_scale[c] = m0 + c < g.M ? ld_chain(g.ra + m0 + c) : 0.f;
-        asm volatile("bar.sync 1, 128;" ::: "memory");     // the four warps
+        asm volatile("bar.sync 1, %0;" ::"n"(128 * C::TURNS) : "memory");      // the epilogue's warps
         if (n < g.N) {
             rw = ld_chain(g.rw + n);
             if (g.bias) bias = ld_chain(g.bias + n);
@@ -226,7 +231,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
     if (S == 1) {
         if (warp >= 2) {
 #pragma unroll 1
-            for (int c0 = 0; c0 < BN && m0 + c0 < g.M; c0 += 16) {
+            for (int c0 = 16 * turn; c0 < BN && m0 + c0 < g.M; c0 += 16 * C::TURNS) {
                 float v[16], u[16] = {};
                 load16(c0, v);
                 if (GATED) load16(BN + c0, u);
@@ -244,7 +249,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
 #pragma unroll
             for (int h = 0; h < C::WS; ++h)
 #pragma unroll 1
-                for (int c0 = 0; c0 < BN && m0 + c0 < g.M; c0 += 16) {
+                for (int c0 = 16 * turn; c0 < BN && m0 + c0 < g.M; c0 += 16 * C::TURNS) {
                     float v[16];
                     load16(h * BN + c0, v);
 #pragma unroll
@@ -275,9 +280,9 @@ __global__ void __launch_bounds__(kNarrowThreads, 1)
                 finish(4 * (rank * share + i), v[0], v[1]);
             };
             if (share % 4 == 0) {
-                for (int i = 0; i < share && m0 + 4 * (rank * share + i) < g.M; i += 4) join(i, std::integral_constant<int, 4>());
+                for (int i = 4 * turn; i < share && m0 + 4 * (rank * share + i) < g.M; i += 4 * C::TURNS) join(i, std::integral_constant<int, 4>());
             } else {
-                for (int i = 0; i < share && m0 + 4 * (rank * share + i) < g.M; ++i) join(i, std::integral_constant<int, 1>());
+                for (int i = turn; i < share && m0 + 4 * (rank * share + i) < g.M; i += C::TURNS) join(i, std::integral_constant<int, 1>());
             }
         }
     }
@@ -294,14 +299,20 @@ using NarrowKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtens
 struct Narrow {
     NarrowKernel kernel;
     size_t smem;
+    int threads;
 };
+template <typename T, int BN, bool GATED>
+Narrow narrow_of() {
+    using C = Narrow4Cfg<BN, GATED>;
+    return {gemm4_narrow_kernel<T, BN, GATED>, C::SMEM, C::THREADS};
+}
 template <typename T, bool GATED>
 Narrow narrow(int bn) {
     switch (bn) {
-        case 16: return {gemm4_narrow_kernel<T, 16, GATED>, Narrow4Cfg<16, GATED>::SMEM};
-        case 32: return {gemm4_narrow_kernel<T, 32, GATED>, Narrow4Cfg<32, GATED>::SMEM};
-        case 64: return {gemm4_narrow_kernel<T, 64, GATED>, Narrow4Cfg<64, GATED>::SMEM};
-        default: return {gemm4_narrow_kernel<T, 128, GATED>, Narrow4Cfg<128, GATED>::SMEM};
+        case 16: return narrow_of<T, 16, GATED>();
+        case 32: return narrow_of<T, 32, GATED>();
+        case 64: return narrow_of<T, 64, GATED>();
+        default: return narrow_of<T, 128, GATED>();
     }
 }
 
@@ -329,7 +340,7 @@ wdc_status launch_narrow(Ctx* c, Gemm4Args g, int bn, int split, cudaStream_t s)
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_GEMM, s);
         const Narrow k = narrow<T, GATED>(bn);
-        launch_kernel(k.kernel, dim3((unsigned)ctas), kNarrowThreads, k.smem, s, split, tw, tu, ta, tsw, tsu, tsa, g);
+        launch_kernel(k.kernel, dim3((unsigned)ctas), k.threads, k.smem, s, split, tw, tu, ta, tsw, tsu, tsa, g);
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 GEMM launch: ") + cudaGetErrorString(e));
