@@ -280,9 +280,11 @@ __global__ void __launch_bounds__(Narrow4Cfg<BN, GATED>::THREADS, 1)
                 finish(4 * (rank * share + i), v[0], v[1]);
             };
             if (share % 4 == 0) {
-                for (int i = 4 * turn; i < share && m0 + 4 * (rank * share + i) < g.M; i += 4 * C::TURNS) join(i, std::integral_constant<int, 4>());
+                for (int i = 4 * turn; i < share && m0 + 4 * (rank * share + i) < g.M;
+                     i += 4 * C::TURNS) join(i, std::integral_constant<int, 4>());
             } else {
-                for (int i = turn; i < share && m0 + 4 * (rank * share + i) < g.M; i += C::TURNS) join(i, std::integral_constant<int, 1>());
+                for (int i = turn; i < share && m0 + 4 * (rank * share + i) < g.M;
+                     i += C::TURNS) join(i, std::integral_constant<int, 1>());
             }
         }
     }
@@ -350,20 +352,22 @@ wdc_status launch_narrow(Ctx* c, Gemm4Args g, int bn, int split, cudaStream_t s)
 // The kernel for a shape is the one with the least estimated time, by fits to a sweep (us,
 // bf16, no residual, operands in L2; narrow kernel n<tokens a tile>,<CTAs a tile>; pair kernel p):
 //                          n16,1  n16,4  n32,1  n32,4  n64,1  n64,4  n128,1 n128,4    p
-//   4 x 1024 x 1024          3.6    4.4                                3.8           6.9
-//   4 x 4096 x 16384        13.9    7.2                               14.3   14.7   22.8
-//   4 x 15360 x 5120         6.7   17.9                               12.2          15.9
-//   32 x 4096 x 4096                       6.4    6.0                  6.5          10.1
-//   32 x 4096 x 16384                     14.6    8.1                 14.8    9.2   22.9
-//   64 x 27648 x 2048                                    11.3         14.0          12.7
-//   64 x 4096 x 16384                                    15.6    9.1  15.6   10.2   23.0
-//   100 x 1024 x 1024                                                  6.4           7.7
-//   200 x 4096 x 4096                                                  9.3   17.7   11.1
-//   200 x 15360 x 5120                                                19.2          12.9
-//   400 x 4096 x 16384                                                18.0          24.0
-//   700 x 4096 x 4096                                                 17.8          11.5
-//   gated 64 x 10240 x 4096                               9.7         10.6          16.9
-//   gated 200 x 10240 x 4096                                          23.1          17.3
+//   4 x 1024 x 1024          3.8                                       4.1           7.2
+//   4 x 4096 x 16384        14.0    7.3                               15.2   15.0   22.9
+//   4 x 15360 x 5120         6.7                                      13.0          16.3
+//   32 x 4096 x 4096                       6.2    5.6                  6.4    8.4   10.4
+//   32 x 4096 x 16384                     14.6    7.7                 14.6    9.7   23.0
+//   64 x 27648 x 2048                                     9.9         11.9          12.3
+//   64 x 4096 x 16384                                    14.9    8.5  14.9   10.0   23.1
+//   100 x 1024 x 1024                                                  5.2           8.0
+//   200 x 4096 x 4096                                                  7.6   15.0   11.2
+//   200 x 15360 x 5120                                                15.6          12.9
+//   400 x 4096 x 16384                                                16.1          24.0
+//   700 x 4096 x 4096                                                 14.2          11.6
+//   gated 64 x 10240 x 4096                               9.0          9.7          16.6
+//   gated 200 x 10240 x 4096                                          20.0          17.1
+//   gated 100 x 2048 x 2048                                            7.9    9.0    9.3
+//   gated 200 x 1024 x 8192                                           15.7   11.2   15.7
 // A narrow CTA takes kStage us for 256 of K and a little for each token; more CTAs than
 // the device holds (fewer than its SMs in clusters of 8) take turns; a cluster's launch
 // and exchange cost what `split` adds.
@@ -371,7 +375,7 @@ struct Choice {
     int bn, split;                     // split 0: the pair kernel
 };
 Choice choose(const Ctx* c, int M, int N, int K, bool gated) {
-    constexpr double kStage[2][4] = {{0.17, 0.17, 0.175, 0.17}, {0.28, 0.28, 0.30, 0.36}};
+    constexpr double kStage[2][4] = {{0.17, 0.17, 0.175, 0.175}, {0.26, 0.26, 0.30, 0.34}};
     const int kb = (K - 1) / kTileK4 + 1;
     Choice best{128, 1};
     double least = 1e30;
@@ -387,14 +391,14 @@ Choice choose(const Ctx* c, int M, int N, int K, bool gated) {
         const double tiles = (double)((M - 1) / bn + 1) * ((N - 1) / 128 + 1), tokens = M < bn ? M : bn;
         for (int split = 1; split <= 8 && split <= bn / 4 && (split == 1 || 2 * split <= kb); split *= 2) {
             const double held = split == 8 ? 0.74 * c->num_sms : c->num_sms;
-            const double turn = (kb + split - 1) / split * kStage[gated][i] + 1.6 + 0.024 * tokens / split;
-            const double join = (gated ? 2.0 : 1.4) + (gated ? 0.04 : 0.02) * tokens + (bn == 128 ? 1.0 : 0.0);
+            const double turn = (kb + split - 1) / split * kStage[gated][i] + 1.6 + (gated ? 0.016 : 0.01) * tokens / split;
+            const double join = (gated ? 1.4 : 1.2) + (gated ? 0.02 : 0.01) * tokens + (bn == 128 ? 1.3 : 0.0);
             offer(bn, split, 1.5 + ceil(tiles * split / held) * (turn + (split > 1 ? join : 0.0)));
         }
     }
     if (c->num_sms >= 2) {
         const double tiles = (double)((M - 1) / 256 + 1) * ((N - 1) / (gated ? 128 : 256) + 1);
-        offer(256, 0, 4.4 + ceil(tiles / (c->num_sms / 2)) * (kb * 0.265 + 1.4));
+        offer(256, 0, 5.8 + ceil(tiles / (c->num_sms / 2)) * (kb * 0.265 + 1.4));
     }
     return best;
 }

@@ -221,7 +221,8 @@ def test_nonfinite_rows_stay_in_their_rows(contexts, M):
 
 # (16, 32, 64 and 128 tokens a tile, alone and with K over 2, 4 and 8 CTAs, one of which ends short)
 FEW = [(1, 8, 4160), (3, 2056, 4160), (2, 8200, 8256), (17, 8, 64), (17, 8200, 8256), (20, 2056, 4160), (33, 8, 4160), (50, 2056, 4160),
-       (60, 8200, 8256), (65, 8, 4160), (90, 2056, 8256), (65, 8200, 16448), (130, 264, 4160)]
+       (60, 8200, 8256), (65, 8, 4160), (90, 2056, 8256), (65, 8200, 16448), (130, 264, 4160),
+       (65, 8, 8256)]
 
 
 @functools.lru_cache(1)
