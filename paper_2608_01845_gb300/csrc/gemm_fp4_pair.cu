@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             pending = true;
         };
-        for (int j = 0; j < jobs && ok; ++j) {
+        int j = 0;
+        for (; j < jobs && ok; ++j) {
             const Job t = job(j);
             const int m0 = t.mb * 256 + (int)rank * 128 + quarter * 32, n0 = t.nb * BN + side * COLS;
             const int end = min(n0 + COLS, g.N);
@@ -428,6 +429,16 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(vempty);
+        }
+        // The first job is left only by a wait that gave up before its part was counted: it is counted all
+        // the same (what its tile then holds is wrong, as the error word says), so that the counters
+        // are 0 for the next launch.
+        if (j < first && g.parts > 1 && lane == 0) {
+            const Job t = job(0);
+            const size_t piece = (size_t)(t.tail * 2 + (int)rank) * 8 + (warp - 4);
+            if (t.mb * 256 + (int)rank * 128 + quarter * 32 < g.M &&
+                atomicAdd(g.counters + piece, 1u) + 1 == (unsigned)g.parts)
+                g.counters[piece] = 0u;
         }
         if (lane == 0) bulk_wait_read<0>();                // the slabs stay until their stores have read them
         if (pending) {                                     // after a wait has given up: no copy is left in flight

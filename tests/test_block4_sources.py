@@ -48,3 +48,15 @@ def test_nothing_is_read_before_the_kernel_before_is_done(name):
         body = code[a:b]
         assert "chain_wait();" in body
         assert not re.search(r"tma_load|ld_chain|__ldcg|cp_async", body[:body.index("chain_wait();")])
+
+
+def test_every_part_is_counted():
+    """A warp whose wait gave up leaves its first job before that part is counted: it counts the part behind
+    the loop, and the last one makes the counter 0 there too, so that no launch finds parts of an earlier one."""
+    code = _code("gemm_fp4_pair.cu")
+    a, b = next((a, b) for a, b in _blocks(code, r"for \(; j < jobs && ok; \+\+j\) \{"))
+    loop = code[a:b]
+    assert "break;" not in loop[loop.index("atomicAdd("):].replace("if (col0 >= end) break;", "")
+    behind = code[b:code.index("__syncthreads();", b)]
+    a, b = next((a, b) for a, b in _blocks(behind, r"if \(j < first && g\.parts > 1 && lane == 0\) \{"))
+    assert "job(0)" in behind[a:b] and "atomicAdd(g.counters" in behind[a:b] and "g.counters[piece] = 0u" in behind[a:b]
