@@ -304,15 +304,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             pending = true;
         };
-        int j = 0;
-        for (; j < jobs && ok; ++j) {
+        // After a wait that gave up, a warp goes on to the end of its tile and stores nothing: what it
+        // hands back is handed back, and its part of a split tile is counted all the same (what that
+        // tile then holds is wrong, as the error word says), so that the counters are 0 for the next launch.
+        for (int j = 0; j < jobs && ok; ++j) {
             const Job t = job(j);
             const int m0 = t.mb * 256 + (int)rank * 128 + quarter * 32, n0 = t.nb * BN + side * COLS;
             const int end = min(n0 + COLS, g.N);
             bool rows = m0 < g.M;                          // the warp has something to finish
             if (RESID && rows && n0 < end && t.tail < 0) request(n0, m0);
             const float ra = m0 + lane < g.M ? ld_chain(g.ra + m0 + lane) : 0.f;
-            if (!mbar_wait_warp(tfull, tphase, abort_flag, g.err)) { ok = false; break; }
+            ok = mbar_wait_warp(tfull, tphase, abort_flag, g.err);
             tc_fence_after();
             // gated: 64 columns of each half; else 128 of one
             float acc[128];
@@ -325,7 +327,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_remote_relaxed(leader);
-            if (!mbar_wait_warp(vfull, tphase, abort_flag, g.err)) { ok = false; break; }
+            ok = mbar_wait_warp(vfull, tphase, abort_flag, g.err) && ok;
             tphase ^= 1u;
             if (t.tail >= 0 && rows) {
                 const size_t piece = (size_t)(t.tail * 2 + (int)rank) * 8 + (warp - 4);
@@ -429,16 +431,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(vempty);
-        }
-        // The first job is left only by a wait that gave up before its part was counted: it is counted all
-        // the same (what its tile then holds is wrong, as the error word says), so that the counters
-        // are 0 for the next launch.
-        if (j < first && g.parts > 1 && lane == 0) {
-            const Job t = job(0);
-            const size_t piece = (size_t)(t.tail * 2 + (int)rank) * 8 + (warp - 4);
-            if (t.mb * 256 + (int)rank * 128 + quarter * 32 < g.M &&
-                atomicAdd(g.counters + piece, 1u) + 1 == (unsigned)g.parts)
-                g.counters[piece] = 0u;
         }
         if (lane == 0) bulk_wait_read<0>();                // the slabs stay until their stores have read them
         if (pending) {                                     // after a wait has given up: no copy is left in flight

@@ -51,12 +51,13 @@ def test_nothing_is_read_before_the_kernel_before_is_done(name):
 
 
 def test_every_part_is_counted():
-    """A warp whose wait gave up leaves its first job before that part is counted: it counts the part behind
-    the loop, and the last one makes the counter 0 there too, so that no launch finds parts of an earlier one."""
+    """An epilogue warp whose wait gave up still counts its part of a split tile, so that no launch finds parts of
+    an earlier one: nothing leaves the job before, and the count does not ask whether the waits were answered."""
     code = _code("gemm_fp4_pair.cu")
-    a, b = next((a, b) for a, b in _blocks(code, r"for \(; j < jobs && ok; \+\+j\) \{"))
-    loop = code[a:b]
-    assert "break;" not in loop[loop.index("atomicAdd("):].replace("if (col0 >= end) break;", "")
-    behind = code[b:code.index("__syncthreads();", b)]
-    a, b = next((a, b) for a, b in _blocks(behind, r"if \(j < first && g\.parts > 1 && lane == 0\) \{"))
-    assert "job(0)" in behind[a:b] and "atomicAdd(g.counters" in behind[a:b] and "g.counters[piece] = 0u" in behind[a:b]
+    epilogue = code[code.index("setmaxnreg_inc<"):]
+    a, b = next((a, b) for a, b in _blocks(epilogue, r"for \(int j = 0; j < jobs && ok; \+\+j\) \{"))
+    loop = epilogue[a:b]
+    before = loop[:loop.index("atomicAdd(")]
+    assert not re.search(r"\b(break|return|continue|goto)\b", before)
+    assert [x for x in re.findall(r"if \([^{;]*?\)(?= \{| before)", before[before.index("tfull"):])] == ["if (t.tail >= 0 && rows)", "if (lane == 0)"]
+    assert re.search(r"bool rows = m0 < g\.M;", before)
