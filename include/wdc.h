@@ -617,8 +617,9 @@ wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_c
  * video's heads by frame, row and column.  As the chunk operators: asynchronous on
  * `stream`, checked before any launch, capturable, and nothing is launched where there
  * are no rows.  A product may split the sums of some of its tiles and join them through a
- * workspace of its own that the context owns: two calls of wdc_op_gemm_fp4 or
- * wdc_op_gated_fp4 of one context, and graphs that hold some, must not run concurrently.
+ * workspace of its own that the context owns: such calls of one context wait for one another on the
+ * device where their streams differ, but a graph that holds calls of wdc_op_gemm_fp4 or
+ * wdc_op_gated_fp4 must not run concurrently with another such graph or such a call of its context.
  * (The results of equal calls are equal bit for bit.) */
 
 /* Positions of several axes (frame, row and column of a video's token, say): the

@@ -1039,6 +1039,8 @@ wdc_status dit_create(Ctx* c) {
     if ((s = dalloc(c, (void**)&c->fp4_work, (size_t)c->fp4_parts * 256 * 256 * sizeof(float)))) return s;
     if ((s = dalloc(c, (void**)&c->fp4_counters, counted))) return s;
     if (cudaMemset(c->fp4_counters, 0, counted) != cudaSuccess) return fail(c, WDC_ERR_CUDA, "DiT init: fp4 product counters");
+    if (cudaEventCreateWithFlags(&c->fp4_done, cudaEventDisableTiming) != cudaSuccess)
+        return fail(c, WDC_ERR_CUDA, "DiT init: fp4 product event");
     const long long npe = (long long)t->Lv * t->D;
     LaunchScope ls(c, WDC_K_OTHER, 0);
     if (t->dtype == WDC_BF16)
@@ -1064,6 +1066,8 @@ void dit_destroy(Ctx* c) {
     c->fp4_work = nullptr;
     c->fp4_counters = nullptr;
     c->fp4_parts = 0;
+    if (c->fp4_done) cudaEventDestroy(c->fp4_done);
+    c->fp4_done = nullptr;
 }
 
 static uint16_t f32_to_bf16_bits(float f) {

@@ -461,6 +461,34 @@ PairKernel pair_kernel(int form) {
     }
 }
 
+// A split product on another stream than the last one's waits for that one, as they share the
+// context's workspace and counters.  (Not under capture: what a graph is ordered with is the
+// caller's.)
+struct SplitOrder {
+    Ctx* c;
+    cudaStream_t s;
+    bool on;
+    unsigned long long id = 0;
+    SplitOrder(Ctx* c_, bool split, cudaStream_t s_) : c(c_), s(s_), on(split) {
+        if (!on) return;
+        cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(s, &st) != cudaSuccess) cudaGetLastError();
+        on = st == cudaStreamCaptureStatusNone;
+    }
+    wdc_status begin() {
+        if (!on) return WDC_OK;
+        WDC_CUDA_TRY(c, cudaStreamGetId(s, &id));
+        if (id != c->fp4_stream) WDC_CUDA_TRY(c, cudaStreamWaitEvent(s, c->fp4_done, 0));
+        return WDC_OK;
+    }
+    wdc_status end() {
+        if (!on) return WDC_OK;
+        WDC_CUDA_TRY(c, cudaEventRecord(c->fp4_done, s));
+        c->fp4_stream = id;
+        return WDC_OK;
+    }
+};
+
 // Pairs resident at a time.
 int resident_pairs(const Ctx* c, PairKernel k) {
     static PerDevice<int> cap;
@@ -550,6 +578,8 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
     if (g.parts > c->fp4_parts / (g.tail > 0 ? g.tail : 1)) g.parts = 1;
     g.work = c->fp4_work;
     g.counters = c->fp4_counters;
+    SplitOrder order(c, g.parts > 1, s);
+    if (wdc_status st = order.begin()) return st;
     {
         OverlapScope ov(c, s);
         LaunchScope ls(c, WDC_K_GEMM, s);
@@ -558,7 +588,7 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(c, WDC_ERR_CUDA, std::string("fp4 GEMM launch: ") + cudaGetErrorString(e));
-    return WDC_OK;
+    return order.end();
 }
 
 }  // namespace

@@ -184,6 +184,10 @@ struct Ctx {
     float* fp4_work = nullptr;
     unsigned* fp4_counters = nullptr;
     int fp4_parts = 0;
+    // the last of them outside a graph: its end, and its stream's id (unlike its handle, never that of
+    // another stream)
+    cudaEvent_t fp4_done = nullptr;
+    unsigned long long fp4_stream = 0;
 
     // graph rollout (device-side control flow), built on first use
     GraphRollout* grollout = nullptr;

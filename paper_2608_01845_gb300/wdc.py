@@ -770,7 +770,8 @@ class Context:
         self._check(LIB.wdc_op_dequantize_fp4(self._h, self._fp4(what, "q", q, M, K), p, ld, M, K, self._op_stream(stream)), what)
 
     def op_gemm_fp4(self, A, W, C, bias=None, gelu=False, res=None, gate=None, stream=None):
-        """wdc_op_gemm_fp4: C = epilogue(A W^T) of Fp4Matrix operands, with the epilogues of op_gemm."""
+        """wdc_op_gemm_fp4: C = epilogue(A W^T) of Fp4Matrix operands, with the epilogues of op_gemm.  A graph that
+        holds fp4 products must not run at the same time as another one, or as fp4 products, of this context."""
         what, (dt, dev, _, f32, _) = "op_gemm_fp4", self._operand_types()
         (M, K), N = A.shape, W.shape[0]
         _tensor(what, "C", C, dt, (M, N), dev)
@@ -786,7 +787,7 @@ class Context:
 
     def op_gated_fp4(self, A, W_gate, W_up, C, gate_bias=None, up_bias=None, gelu=False, stream=None):
         """wdc_op_gated_fp4: C = f(A W_gate^T + gate_bias) * (A W_up^T + up_bias) of Fp4Matrix operands; f is SiLU,
-        or GELU (its tanh form)."""
+        or GELU (its tanh form).  Graphs: see op_gemm_fp4."""
         what, (dt, dev, _, f32, _) = "op_gated_fp4", self._operand_types()
         (M, K), N = A.shape, W_gate.shape[0]
         _tensor(what, "C", C, dt, (M, N), dev)

@@ -615,6 +615,48 @@ def test_after_a_wait_that_gave_up(contexts):
     assert (np.abs(host(C) - y) <= product_bound(y, mag, SPLIT[2]) + 2.0 ** -24 * np.abs(y)).all() and ctx.device_errors() == 0
 
 
+def test_two_streams_of_one_context(contexts):
+    """Split products of one context on streams by turns, none waiting on the host: one after the other on
+    the device, through the one workspace; and beside a stream that was left."""
+    A, W, _, _ = split_case()
+    a, w, ctx = matrix(*A), matrix(*W), contexts["bf16"]
+    new = lambda: torch.empty(*SPLIT[:2], dtype=torch.bfloat16, device="cuda")
+    want = new()
+    ctx.op_gemm_fp4(a, w, want)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [(st, new()) for _ in range(4) for st in streams]
+    torch.cuda.synchronize()
+    for st, o in outs:
+        ctx.op_gemm_fp4(a, w, o, stream=st)
+    ctx.op_gemm_fp4(a, w, outs[0][1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(want, o) for _, o in outs) and ctx.device_errors() == 0
+
+
+def test_split_products_beside_a_capture(contexts):
+    """A capture takes up no wait for products outside it, and those go on; replays give the same bits."""
+    A, W, _, _ = split_case()
+    a, w, ctx = matrix(*A), matrix(*W), contexts["bf16"]
+    new = lambda: torch.zeros(*SPLIT[:2], dtype=torch.bfloat16, device="cuda")
+    want, before, inside, after = new(), new(), new(), new()
+    ctx.op_gemm_fp4(a, w, want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ctx.op_gemm_fp4(a, w, before, stream=side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ctx.op_gemm_fp4(a, w, inside)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        inside.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want, inside)
+    ctx.op_gemm_fp4(a, w, after, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(want, before) and torch.equal(want, after) and ctx.device_errors() == 0
+
+
 # ---------------------------------------------------------------- offsets past 32 bits
 def ends(t, n=3):
     return torch.cat([t[:n], t[-n:]])
