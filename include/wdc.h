@@ -256,7 +256,8 @@ wdc_status wdc_gemm_launches(const wdc_ctx* ctx, unsigned long long* counts);
  * 4 = the two CTAs of a tensor-core pair saw different tensor-memory bases,
  * 8 = a bf16 model's QKV projection produced a value of V beyond fp16's range
  * (|v| > 65504), which was saturated to +-65504 when V^T was stored for the
- * attention (NaN is kept). */
+ * attention (NaN is kept).  Also makes the counters of split 4-bit products zero
+ * again, which products that ran at the same time against the rule may have left otherwise. */
 wdc_status wdc_device_errors(wdc_ctx* ctx, unsigned* bits);
 /* Self-test of the bounded device-side waits (the paper has no counterpart):
  * one CTA waits on an mbarrier that nothing completes, through the same
@@ -268,6 +269,10 @@ wdc_status wdc_device_errors(wdc_ctx* ctx, unsigned* bits);
  * check the timeout path and that the context stays usable afterwards,
  * without faulting or hanging the GPU.  Asynchronous on `stream`. */
 wdc_status wdc_selftest_wait_timeout(wdc_ctx* ctx, unsigned long long limit_ns, wdc_stream stream);
+/* Self-test of what wdc_device_errors puts right: leaves the counters of the split 4-bit products
+ * (see wdc_op_gemm_fp4) as products that ran at the same time may, so that the next of them would
+ * join sums too early.  Lets a test check that wdc_device_errors clears them.  Synchronises the device. */
+wdc_status wdc_selftest_fp4_counters(wdc_ctx* ctx);
 
 /* ------------------------------------------------------------------ weights */
 /* Copies one parameter tensor (host fp32, `count` elements, shape as listed in
@@ -619,7 +624,8 @@ wdc_status wdc_op_attention_paged(wdc_ctx* ctx, const void* q, const wdc_paged_c
  * are no rows.  A product may split the sums of some of its tiles and join them through a
  * workspace of its own that the context owns: such calls of one context wait for one another on the
  * device where their streams differ, but a graph that holds calls of wdc_op_gemm_fp4 or
- * wdc_op_gated_fp4 must not run concurrently with another such graph or such a call of its context.
+ * wdc_op_gated_fp4 must not run concurrently with another such graph or such a call of its context
+ * (the sums would be mixed, those of later calls too until wdc_device_errors is called).
  * (The results of equal calls are equal bit for bit.) */
 
 /* Positions of several axes (frame, row and column of a video's token, say): the

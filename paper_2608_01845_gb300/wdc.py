@@ -156,6 +156,7 @@ def _load():
         "wdc_profile_enable": (I, [P, I]),
         "wdc_device_errors": (I, [P, ctypes.POINTER(ctypes.c_uint)]),
         "wdc_selftest_wait_timeout": (I, [P, ctypes.c_ulonglong, P]),
+        "wdc_selftest_fp4_counters": (I, [P]),
         "wdc_profile_read": (I, [P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_ulonglong)]),
         "wdc_last_error": (ctypes.c_char_p, [P]),
         "wdc_latent_numel": (S, [P]),
@@ -446,6 +447,10 @@ class Context:
     def selftest_wait_timeout(self, limit_ns, stream=None):
         """wdc_selftest_wait_timeout: a bounded device wait that must time out."""
         self._check(LIB.wdc_selftest_wait_timeout(self._h, int(limit_ns), _stream(stream)), "selftest_wait_timeout")
+
+    def selftest_fp4_counters(self):
+        """wdc_selftest_fp4_counters: counters of split 4-bit products as calls at the same time may leave them."""
+        self._check(LIB.wdc_selftest_fp4_counters(self._h), "selftest_fp4_counters")
 
     def profile_enable(self, on=True):
         self._check(LIB.wdc_profile_enable(self._h, int(on)), "profile_enable")

@@ -657,6 +657,17 @@ def test_split_products_beside_a_capture(contexts):
     assert torch.equal(want, before) and torch.equal(want, after) and ctx.device_errors() == 0
 
 
+def test_device_errors_makes_the_counters_zero(contexts):
+    """Whatever counts calls at the same time have left, with no error bit set."""
+    ctx = contexts["f32"]
+    A, W, y, mag = split_case()
+    C = torch.empty(*SPLIT[:2], device="cuda")
+    ctx.selftest_fp4_counters()
+    assert ctx.device_errors() == 0
+    ctx.op_gemm_fp4(matrix(*A), matrix(*W), C)
+    assert (np.abs(host(C) - y) <= product_bound(y, mag, SPLIT[2]) + 2.0 ** -24 * np.abs(y)).all() and ctx.device_errors() == 0
+
+
 # ---------------------------------------------------------------- offsets past 32 bits
 def ends(t, n=3):
     return torch.cat([t[:n], t[-n:]])
