@@ -145,14 +145,15 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const __grid_cons
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         }
-        const float inv = rsqrtf(ss * a.by + a.eps), back = -mean * inv;
+        const float inv = rsqrtf(ss * a.by + a.eps);
 #pragma unroll
         for (int u = 0; u < V; ++u) {
             if (!live || col[u] >= a.D) continue;
             if (a.center) {
-                // (fused: what the product would be rounded by is far below the sum's own error)
+                // (the difference first: v inv - mean inv in one step adds mean inv's rounding, so that a row of
+                // 100.5s, whose mean is exact, came out as up to 4e-3 instead of 0 with eps 1e-6)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] = fmaf(v[u][i], inv, back);
+                for (int i = 0; i < 8; ++i) v[u][i] = (v[u][i] - mean) * inv;
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[u][i] *= inv;

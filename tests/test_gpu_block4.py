@@ -421,6 +421,23 @@ def test_add_norm_of_zeros_and_nonfinite_rows(contexts):
         assert r[0] == 0 and np.isnan(r[[1, 2]]).all() and np.isfinite(r[[3, 4]]).all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 256, 1024, 4096, 16384])
+def test_layer_norm_of_equal_values(contexts, D, kind):
+    """100.5 summed over a power of two of columns is exact, and so is the mean: the row less it is 0, whatever
+    1 / sqrt(eps) is, and the result is the shift."""
+    ctx, dt = contexts[kind], DTYPES[kind]
+    x = np.full((3, D), 100.5, np.float32)
+    x[1], x[2] = -0.75, 3.0
+    shift = synth.bf16_round(synth.normal(93, (1, D), 0.3))
+    for eps in (1e-6, 1e-5, 3e-7):
+        out, q, s = torch.empty(3, D, dtype=dt, device="cuda"), torch.empty(3, D, dtype=F8, device="cuda"), torch.empty(-(-D // 128), 3, device="cuda")
+        ctx.op_add_norm(dev(x, dt), out, center=True, eps=eps, weight=dev(np.full((1, D), 3.0)), shift=dev(shift))
+        assert np.array_equal(host(out), np.repeat(shift, 3, 0))
+        ctx.op_add_norm(dev(x, dt), q, scale=s, center=True, eps=eps)
+        assert bool((s == 0).all()) and bool((q.float() == 0).all())
+
+
 # ---------------------------------------------------------------- several axes
 def axes_case(seed, T, pairs, rows):
     r = np.random.default_rng(seed)
