@@ -700,7 +700,8 @@ wdc_status wdc_op_gated_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W_gat
  * before it is rounded into `total`.  One of out, q8 and q4 takes the result: in the model
  * dtype, in e4m3 as wdc_op_quantize_fp8 (block_rows 1) lays A out, or in e2m1 as
  * wdc_op_quantize_fp4 does, both from the fp32 values.  total and out may be x or delta
- * (the same rows), but not the same place.  D % 16 == 0 (q4: 64), at most 16384; row strides multiples of 8.  (The
+ * (the same rows, so the same row stride), but not the same place; q8, q4 and their scales have places of
+ * their own (WDC_ERR_INVALID_ARG where an address shows otherwise).  D % 16 == 0 (q4: 64), at most 16384; row strides multiples of 8.  (The
  * squares are fp32 too: a row with values above about 10^18 comes out as shift; without
  * eps, one of zeros, or centred one of equal values, is NaN.) */
 typedef struct wdc_add_norm {

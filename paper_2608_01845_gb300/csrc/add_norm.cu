@@ -261,13 +261,25 @@ wdc_status op_add_norm(Ctx* c, const wdc_add_norm* n, int M, int D, cudaStream_t
     const int kinds = (n->out != nullptr) + (n->q8 != nullptr) + (n->q4 != nullptr);
     if (kinds != 1) return fail(c, WDC_ERR_INVALID_ARG, "residual norm: one of out, q8 and q4 is wanted");
     if (n->q4 && D % 64) return fail(c, WDC_ERR_UNSUPPORTED, "residual norm: e2m1 needs D % 64 == 0");
-    if (n->total && (n->total == n->out || n->total == n->q8))
-        return fail(c, WDC_ERR_INVALID_ARG, "residual norm: total and the result must be two places");
     if (n->gate && !n->delta) return fail(c, WDC_ERR_INVALID_ARG, "residual norm: a gate without a branch");
     if (n->ldx < D || (n->delta && n->ldd < D) || (n->total && n->ldt < D) || (n->out && n->ldo < D))
         return fail(c, WDC_ERR_INVALID_ARG, "residual norm: row stride below D");
     if (n->ldx % 8 || (n->delta && n->ldd % 8) || (n->total && n->ldt % 8) || (n->out && n->ldo % 8))
         return fail(c, WDC_ERR_UNSUPPORTED, "residual norm: row strides must be multiples of 8");
+    // Places: an output over an input is its rows, read and written by the same threads; of the others each is
+    // one of its own (a block writes a row while others still read theirs).
+    const void* few[] = {n->q8, n->q8 ? n->scale : nullptr, n->q4 ? n->q4->codes : nullptr, n->q4 ? n->q4->scale : nullptr,
+                         n->q4 ? n->q4->row_scale : nullptr};
+    for (const void* p : few)
+        if (p && (p == n->x || p == n->delta || p == n->total))
+            return fail(c, WDC_ERR_INVALID_ARG, "residual norm: a result in few bits needs a place of its own");
+    if (n->total && n->total == n->out)
+        return fail(c, WDC_ERR_INVALID_ARG, "residual norm: total and the result must be two places");
+    auto shifted = [&](const void* p, long long ld) {
+        return M > 1 && p && ((p == n->x && ld != n->ldx) || (p == n->delta && ld != n->ldd));
+    };
+    if (shifted(n->out, n->ldo) || shifted(n->total, n->ldt))
+        return fail(c, WDC_ERR_INVALID_ARG, "residual norm: an output over an input must have its row stride");
     if (M == 0) return WDC_OK;
     if (!n->x || (n->q8 && !n->scale)) return fail(c, WDC_ERR_INVALID_ARG, "residual norm: null pointer");
     if (((uintptr_t)n->x | (uintptr_t)n->delta | (uintptr_t)n->total | (uintptr_t)n->out | (uintptr_t)n->q8 |

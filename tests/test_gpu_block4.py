@@ -804,6 +804,32 @@ def test_refusals_of_the_library(contexts):
     assert ctx.launches == before and ctx.device_errors() == 0
 
 
+def test_refusals_of_places(contexts):
+    """A row is read by one block while another writes its own: an output lies on an input row for row or not at
+    all, and a result in few bits on neither the inputs nor the sum."""
+    ctx, L = contexts["bf16"], wdc.LIB
+    s = torch.cuda.current_stream().cuda_stream
+    x, y, t = (torch.ones(4, 128, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    p, d, o = (v.data_ptr() for v in (x, y, t))
+    m = wdc.Fp4Matrix.empty(4, 64)
+    q4 = lambda **kw: dict(out=None, q4=ctypes.pointer(wdc.Fp4C(*(kw.get(n, getattr(m.c, n)) for n in ("codes", "scale", "row_scale")))))
+    good = dict(x=p, ldx=128, delta=d, ldd=128, out=o, ldo=64, eps=1e-6)
+    before = ctx.launches
+    for kw in [dict(out=p, ldo=64), dict(out=d, ldo=64), dict(total=p, ldt=64), dict(total=d, ldt=72), dict(out=p, ldo=128, ldx=64),
+               dict(total=o, ldt=64), dict(out=None, q8=p, scale=o), dict(out=None, q8=d, scale=o), dict(out=None, q8=o, scale=p),
+               dict(out=None, q8=o, scale=d), dict(out=None, q8=o, scale=p + 512, total=o, ldt=64),
+               dict(out=None, q8=o, scale=p + 512, total=p + 512, ldt=64)]:
+        assert L.wdc_op_add_norm(ctx._h, wdc.AddNorm(**dict(good, **kw)), 4, 64, s) == 1, kw
+    for field in ("codes", "scale", "row_scale"):
+        for at in (p, d):
+            assert L.wdc_op_add_norm(ctx._h, wdc.AddNorm(**dict(good, **q4(**{field: at}))), 4, 64, s) == 1
+        assert L.wdc_op_add_norm(ctx._h, wdc.AddNorm(**dict(good, total=o, ldt=64, **q4(**{field: o}))), 4, 64, s) == 1
+    assert ctx.launches == before
+    for M, kw in [(1, dict(out=p, ldo=64)), (4, dict(out=p, ldo=128)), (4, dict(total=d, ldt=128))]:
+        assert L.wdc_op_add_norm(ctx._h, wdc.AddNorm(**dict(good, **kw)), M, 64, s) == 0, kw
+    assert ctx.launches == before + 3 and ctx.device_errors() == 0
+
+
 def test_nothing_to_do(contexts):
     ctx, e = contexts["bf16"], lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda")
     before, m = ctx.launches, wdc.Fp4Matrix.empty(0, 64)
