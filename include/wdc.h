@@ -532,7 +532,8 @@ wdc_status wdc_op_quantize_fp8(wdc_ctx* ctx, const void* x, long long ldx, void*
  * in fp32 (the two scales are multiplied first, in fp32 too: their product is to
  * be 0 or a normal number).  bias, gelu, res, gate and C as in wdc_op_gemm (C and res
  * [M, N] in the model dtype, res may equal C); GELU's exponential and quotient
- * are approximations, together within 2^-18 of its value for either dtype.  N % 8 == 0 and K % 16 == 0, both at most
+ * are approximations, for either dtype: the result is within 2^-18 of its value for arguments above -5/2 and
+ * within 2^-15 below, and may be 0 where it is below 2^-54 in size.  N % 8 == 0 and K % 16 == 0, both at most
  * 2^31 - 512 (WDC_ERR_UNSUPPORTED otherwise). */
 wdc_status wdc_op_gemm_fp8(wdc_ctx* ctx, const void* A, const float* a_scale, const void* W, const float* w_scale,
                            const float* bias, void* C, int M, int N, int K, int gelu, const void* res,
@@ -687,7 +688,9 @@ wdc_status wdc_op_gemm_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W, con
                            int K, int gelu, const void* res, const float* gate, wdc_stream stream);
 /* A gated MLP's first half in one kernel: C [M, N] = f(A W_gate^T + gate_bias) * (A W_up^T +
  * up_bias) with f(x) = x / (1 + exp(-x)), or GELU_tanh with gelu != 0; W_gate and W_up [N, K],
- * the biases [N] fp32 or NULL.  The products as above; f is within 2^-18 of its value. */
+ * the biases [N] fp32 or NULL.  The products as above; f is within 2^-18
+ * of its value for arguments above -5/2 and within 2^-17 below (GELU: 2^-15), and may be 0 where it is below
+ * 2^-54 in size. */
 wdc_status wdc_op_gated_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W_gate, const wdc_fp4* W_up,
                             const float* gate_bias, const float* up_bias, void* C, int M, int N, int K, int gelu,
                             wdc_stream stream);

@@ -187,6 +187,45 @@ def test_gated(contexts, M, N, K, gelu, bias, kind):
     assert bool((buf[M:] == 7.0).all())
 
 
+def activation_arguments(n):
+    """From far below where the exponentials end to far above, closer around 0 and at the borders."""
+    x = np.concatenate([np.linspace(-60, 12, n - 2048), -np.geomspace(1e-6, 1e30, 1024), np.geomspace(1e-6, 1e30, 992), [0.0, -0.0],
+                        np.linspace(-7.1, -6.9, 15), np.linspace(-42, -41, 15)])
+    return x.astype(np.float32)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("op", ["gemm_fp8", "gemm_fp4", "gated_gelu", "gated_silu"])
+@pytest.mark.parametrize("M", [2, 2048])                   # (few rows, CTA pairs)
+def test_activations_over_their_whole_range(contexts, M, op, kind):
+    """The bias alone is the argument x, f(x) = x / (1 + 2^u).  u is off by 2^-21 of itself for GELU (three
+    roundings of its cubic term, the sum's, the constants' three and the product's: 8 of 2^-24) and by 2^-23 for
+    SiLU, so 2^u by |u| ln 2 times that, with |u| at most 60 before f is below 2^-54: 2^-15.6 and 2^-17.6; above
+    -5/2 |u| is below 7.4: 2^-18.6.  The exponential's 2^-22, the sum, quotient and products add 2^-20.5.
+    (The kernel for few rows has an exponential of 2 + 1.17 |x| ulp for SiLU: 2^-17.4 at -41.)"""
+    ctx, N = contexts[kind], 8192
+    x = activation_arguments(N)
+    zero = lambda rows, k: torch.zeros(rows, k, dtype=torch.uint8, device="cuda")
+    C = torch.full((M, N), 7.0, dtype=DTYPES[kind], device="cuda")
+    if op == "gemm_fp8":
+        one = torch.ones
+        ctx.op_gemm_fp8(zero(M, 128).view(F8), one(1, M, device="cuda"), zero(N, 128).view(F8), one(N // 128, 1, device="cuda"), C,
+                        bias=dev(x), gelu=True)
+    else:
+        m = lambda rows: wdc.Fp4Matrix(zero(rows, 32), zero(-(-rows // 128), 512).view(-1, 1, 512).view(F8), torch.ones(rows, device="cuda"))
+        if op == "gemm_fp4":
+            ctx.op_gemm_fp4(m(M), m(N), C, bias=dev(x), gelu=True)
+        else:
+            ctx.op_gated_fp4(m(M), m(N), m(N), C, gate_bias=dev(x), up_bias=dev(np.ones(N)), gelu=op == "gated_gelu")
+    xd = x.astype(np.float64)
+    with np.errstate(over="ignore"):
+        f = xd / (1 + np.exp(-xd if op == "gated_silu" else -2 * np.sqrt(2 / np.pi) * (xd + 0.044715 * xd ** 3)))
+    bound = np.where(xd > -2.5, 2.0 ** -18, 2.0 ** -17 if op == "gated_silu" else 2.0 ** -15) + HALF[kind]
+    bound = np.where(np.abs(f) < 2.0 ** -54, 1.01, bound)
+    got = host(C)
+    assert (got == got[:1]).all() and (np.abs(got[0] - f) <= bound * np.abs(f)).all() and ctx.device_errors() == 0
+
+
 @pytest.mark.parametrize("M,N,K", [(9, 264, 1088), (150, 520, 320), (900, 4104, 576)])
 def test_products_of_any_scales(contexts, M, N, K):
     """Scales are any e4m3 numbers, the rows' any fp32 ones of either sign; codes are all sixteen."""
