@@ -18,10 +18,12 @@ namespace wdc {
 namespace {
 
 constexpr int kGroups = 4;
-// Tokens of a V^T tile (17776 x 48 heads of 64: tiles of 64 tokens took 65 us beside the
-// norms, of 128 48, of 256 43).
-template <typename T, int D>
-constexpr int kVtTokens = sizeof(T) == 2 ? 16384 / D : 64;
+// Tokens of a V^T tile.  Of a long clip's (RUNS) as many as 32 KB of fp16 hold (17776 x 48 heads of 64: tiles
+// of 64 tokens took 65 us beside the norms, of 128 48, of 256 43); of a shorter one's, whose tiles are to be
+// on all SMs, 64.  (Tiles of 256 and 128 for every clip: 1350 tokens, 24 heads of 64 6.8 -> 8.4 us, 4 key heads of
+// 64 3.9 -> 5.7, 24 of 128 11.0 -> 12.9; 17776 tokens, 24 of 64 69 -> 62, 48 of 64 133 -> 113.)
+template <int D, bool RUNS>
+constexpr int kVtTokens = RUNS ? 16384 / D : 64;
 
 struct NormArgs {
     const void* qkv;
@@ -104,11 +106,11 @@ template <> struct Vec<__nv_bfloat16> {
 };
 
 // One tile of V^T: kTokens tokens of one head through shared memory.
-template <typename T, int D>
+template <typename T, int D, bool RUNS>
 __device__ void transpose_v(const NormArgs& a, int tile) {
     using V = Vec<T>;
     using Out = typename std::conditional<sizeof(T) == 2, __half, float>::type;
-    constexpr int kTokens = kVtTokens<T, D>;
+    constexpr int kTokens = kVtTokens<D, RUNS>;
     constexpr int LDS = kTokens + 4 / (int)sizeof(Out);      // (an odd number of words: columns meet different banks)
     __shared__ alignas(16) Out sm[D * LDS];
     const int tiles = (a.T + kTokens - 1) / kTokens;
@@ -158,7 +160,7 @@ __device__ void transpose_v(const NormArgs& a, int tile) {
 }
 
 // What turns the heads: nothing or one table of positions, or a table for each axis.
-// RUNS: a warp may have several chunks.
+// RUNS: a warp has several chunks (bf16).
 template <typename T, int D, bool APPEND, bool PAIRS, bool AXES, bool RUNS>
 __global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __grid_constant__ NormArgs a) {
     using V = Vec<T>;
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __gr
         // memory at other times (one behind the other 133 us, mixed 124 at 17776 x 72 heads of 128)
         const unsigned v = (unsigned)((unsigned long long)block * a.vt_tiles / gridDim.x);
         if ((unsigned)((unsigned long long)(block + 1) * a.vt_tiles / gridDim.x) > v) {
-            transpose_v<T, D>(a, (int)v);
+            transpose_v<T, D, RUNS>(a, (int)v);
             return;
         }
         block -= v;
@@ -207,7 +209,25 @@ __global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __gr
             }
         }
     };
-    load(chunk0);
+    // A chunk by itself of the dense form is widened at once (256 tokens of 24 + 24 heads of 128 3.24 us for 3.42,
+    // 4050 18.8 for 19.4), other chunks as they are used (64 appended tokens of those 3.66 for 3.76).
+    constexpr bool HELD = RUNS || APPEND;
+    float wide[HELD ? 1 : kGroups][E];
+    if constexpr (HELD) {
+        load(chunk0);
+    } else {
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int h = (chunk0 * kGroups + u) * HPW + lane / LPH;
+            if (h < n_heads) {
+                if constexpr (PAIRS) V::widen(load_bits(row + (size_t)h * D + ea), wide[u]);
+                else V::widen(load_bits(row + (size_t)h * D + ea, row + (size_t)h * D + eb), wide[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i) wide[u][i] = 0.f;
+            }
+        }
+    }
 
     // this token's place: its row of the cache and its position
     int place = t;
@@ -281,14 +301,21 @@ __global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __gr
 
     for (int chunk = chunk0; chunk < chunk1; ++chunk) {
         uint4 now[kGroups];
+        if constexpr (HELD) {
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) now[u] = bits[u];
-        if (RUNS && chunk + 1 < chunk1) load(chunk + 1);
+            for (int u = 0; u < kGroups; ++u) now[u] = bits[u];
+            if (RUNS && chunk + 1 < chunk1) load(chunk + 1);
+        }
 #pragma unroll
         for (int u = 0; u < kGroups; ++u) {
             const int h = (chunk * kGroups + u) * HPW + lane / LPH;
             float x[E], ss = 0.f;
-            V::widen(now[u], x);
+            if constexpr (HELD) {
+                V::widen(now[u], x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = wide[u][i];
+            }
 #pragma unroll
             for (int i = 0; i < E; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
@@ -362,15 +389,29 @@ __global__ void __launch_bounds__(256, RUNS ? 3 : 4) norm_rope_kernel(const __gr
 }
 
 template <typename T, int D, bool APPEND>
-wdc_status launch(Ctx* c, NormArgs& a, bool pairs, int vt_tiles, cudaStream_t s) {
+wdc_status launch(Ctx* c, NormArgs& a, bool pairs, cudaStream_t s) {
     constexpr int HPW = 32 / (D / Vec<T>::E);
     const int n_heads = APPEND ? a.heads + 2 * a.kv : a.heads + a.kv;
     a.chunks = (n_heads + kGroups * HPW - 1) / (kGroups * HPW);
-    // as many chunks a warp as leave four runs for each of the 24 warps an SM that the device holds
-    const long long most = (long long)a.T * a.chunks / (4 * 24 * c->num_sms);
-    a.per = most < 1 ? 1 : (most < a.chunks ? (int)most : a.chunks);
+    // Runs of bf16 heads: as few a token as leave 62 runs an SM (which holds 24 at a time), where they come out of
+    // equal length; of the dense form, whose tokens are looked up in no table, at most two and of three chunks
+    // at least.  us with runs of 1, 2, 3 and all chunks, dense with V^T: 9600 tokens of 24 + 24 heads of
+    // 64 40.1, 41.7, 36.4; 5000 of 48 + 48 41.9, 38.8, 37.5, 38.4; 5000 of 24 + 24 of 128 40.1, 41.8, 39.6,
+    // 41.7 and 17776 127.9, 131.0, 122.6, 121.2; 9600 of 24 + 2 34.8, 34.5, 36.8 (3 and 1), 30.0, and 4050 12.9,
+    // 14.1, 16.4, 14.9.  fp32 heads, twice the loads a chunk, lose: 9600 of 24 + 24 of 64 57.0, 63.3, 61.7, 61.3.
+    a.per = 1;
+    if constexpr (sizeof(T) == 2) {
+        const long long want = 62ll * c->num_sms, fewest = (want + a.T - 1) / a.T;
+        if (fewest < a.chunks && fewest <= (APPEND ? a.chunks : 2)) {
+            const int per = (a.chunks + (int)fewest - 1) / (int)fewest;
+            if (per >= (APPEND ? 2 : 3) && (a.chunks + per - 1) / per == fewest) a.per = per;
+        }
+    }
     a.runs = (a.chunks + a.per - 1) / a.per;
     const long long blocks = ((long long)a.T * a.runs + 7) / 8;
+    const int vt_tokens = a.per > 1 ? kVtTokens<D, true> : kVtTokens<D, false>;
+    const long long vt_tiles = !APPEND && a.v ? (long long)((a.T - 1) / vt_tokens + 1) * a.kv : 0;
+    if (vt_tiles > 0x3fffffff) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^30 thread blocks");
     if (blocks + vt_tiles > 0x7fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^31 - 1 thread blocks");
     a.vt_tiles = (unsigned)vt_tiles;
     const dim3 grid((unsigned)(blocks + vt_tiles));
@@ -380,8 +421,10 @@ wdc_status launch(Ctx* c, NormArgs& a, bool pairs, int vt_tiles, cudaStream_t s)
         auto go = [&](auto kernel) { launch_kernel(kernel, grid, 256, 0, s, 1, a); };
         auto of = [&](auto p, auto x) {
             constexpr bool P = decltype(p)::value, X = decltype(x)::value;
-            if (a.per > 1) go(norm_rope_kernel<T, D, APPEND, P, X, true>);
-            else go(norm_rope_kernel<T, D, APPEND, P, X, false>);
+            if constexpr (sizeof(T) == 2) {
+                if (a.per > 1) return go(norm_rope_kernel<T, D, APPEND, P, X, true>);
+            }
+            go(norm_rope_kernel<T, D, APPEND, P, X, false>);
         };
         if (a.axes > 0 && pairs) of(std::true_type(), std::true_type());
         else if (a.axes > 0) of(std::false_type(), std::true_type());
@@ -458,14 +501,11 @@ wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int hea
     if (bf16 && T > 0x7fffffff - 7) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: T too large");
     a.q = q; a.k = k; a.v = vt;
     a.ldv = bf16 ? (T + 7) / 8 * 8 : T;
-    const int per_tile = bf16 ? (d == 64 ? kVtTokens<__nv_bfloat16, 64> : kVtTokens<__nv_bfloat16, 128>) : kVtTokens<float, 64>;
-    const long long tiles = vt ? (long long)((T - 1) / per_tile + 1) * kv : 0;
-    if (tiles > 0x3fffffff) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: more than 2^30 thread blocks");
     if (bf16)
-        return d == 64 ? launch<__nv_bfloat16, 64, false>(c, a, n->interleaved, (int)tiles, s)
-                       : launch<__nv_bfloat16, 128, false>(c, a, n->interleaved, (int)tiles, s);
-    return d == 64 ? launch<float, 64, false>(c, a, n->interleaved, (int)tiles, s)
-                   : launch<float, 128, false>(c, a, n->interleaved, (int)tiles, s);
+        return d == 64 ? launch<__nv_bfloat16, 64, false>(c, a, n->interleaved, s)
+                       : launch<__nv_bfloat16, 128, false>(c, a, n->interleaved, s);
+    return d == 64 ? launch<float, 64, false>(c, a, n->interleaved, s)
+                   : launch<float, 128, false>(c, a, n->interleaved, s);
 }
 
 wdc_status check_cache(Ctx* c, const wdc_paged_cache* p, int* page_log2) {
@@ -503,8 +543,8 @@ wdc_status op_qk_norm_rope_append(Ctx* c, const void* qkv, long long ld, int T, 
     a.q = q; a.k = p->k; a.v = p->v;
     a.table = p->table; a.length = p->length; a.start = q_start;
     a.pages = p->pages; a.sequences = p->sequences; a.width = p->table_width;
-    return p->head_dim == 64 ? launch<__nv_bfloat16, 64, true>(c, a, n->interleaved, 0, s)
-                             : launch<__nv_bfloat16, 128, true>(c, a, n->interleaved, 0, s);
+    return p->head_dim == 64 ? launch<__nv_bfloat16, 64, true>(c, a, n->interleaved, s)
+                             : launch<__nv_bfloat16, 128, true>(c, a, n->interleaved, s);
 }
 
 }  // namespace wdc

@@ -534,6 +534,53 @@ def test_axes_append(contexts, d, H, kv, page, pairs, interleaved):
     assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,kv,d", [(9605, 24, 24, 64), (5003, 48, 48, 64), (4801, 48, 8, 128), (9431, 10, 3, 128)])
+@pytest.mark.parametrize("form", ["rot", "rot_halves", "axes"])
+def test_a_long_clip_is_its_pieces(contexts, T, H, kv, d, form, kind):
+    """Long clips take runs of heads and V^T tiles of more tokens (a whole token's heads a run, or two runs of
+    equal or unequal length): the same bits as calls of 700 tokens at a time, which take neither."""
+    ctx, dt = contexts[kind], DTYPES[kind]
+    r = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(T, (H + 2 * kv) * d, device="cuda", generator=r).to(dt)
+    w, tables = dev(1 + synth.normal(52, (d,), 0.2)), [dev(rotations(40, d // 2)), dev(rotations(9, d // 2))]
+    angles, place = dev(rotations(300, d)), torch.randint(0, 300, (T,), device="cuda", generator=r, dtype=torch.int32)
+    coords = torch.stack([place % 40, place % 9], 1).contiguous()
+
+    def run(t0, t1):
+        n = t1 - t0
+        q, k = torch.empty(H, n, d, dtype=dt, device="cuda"), torch.empty(kv, n, d, dtype=dt, device="cuda")
+        vt = torch.full((kv, d, -(-n // 8) * 8 if kind == "bf16" else n), 5.0, dtype=torch.half if kind == "bf16" else dt, device="cuda")
+        how = dict(axes=wdc.RotAxes(tables, coords[t0:t1])) if form == "axes" else dict(rot=angles, positions=place[t0:t1])
+        ctx.op_qk_norm_rope(x[t0:t1], q, k, vt=vt, q_weight=w, k_weight=w, interleaved=form != "rot_halves", **how)
+        assert bool((vt[:, :, n:] == 5.0).all())
+        return q, k, vt[:, :, :n].transpose(1, 2)
+    whole, parts = run(0, T), [run(t, min(t + 700, T)) for t in range(0, T, 700)]
+    assert all(torch.equal(a, torch.cat([p[i] for p in parts], 1)) for i, a in enumerate(whole)) and ctx.device_errors() == 0
+
+
+@pytest.mark.parametrize("T,H,kv,d", [(9431, 24, 4, 64), (4801, 48, 8, 128), (3301, 24, 24, 128)])
+@pytest.mark.parametrize("interleaved", [True, False])
+def test_a_long_chunk_is_its_pieces(contexts, T, H, kv, d, interleaved):
+    """The same for tokens appended to a cache: one sequence's all at once, and 700 at a time."""
+    ctx, got = contexts["bf16"], []
+    x = dev(synth.normal(62, (T, (H + 2 * kv) * d), 1.5), torch.bfloat16)
+    w, angles = dev(1 + synth.normal(63, (d,), 0.2)), dev(rotations(T, d))
+    for step in (T, 700):
+        page, pages = 64, -(-T // 64)
+        k, v = torch.zeros(pages, kv, page, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(pages, kv, page, d, dtype=torch.half, device="cuda")
+        table, length = torch.arange(pages, dtype=torch.int32, device="cuda").flip(0).view(1, -1).contiguous(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        cache, q = wdc.PagedCache(k, v, table, length), torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda")
+        for t in range(0, T, step):
+            n = min(step, T - t)
+            length.fill_(t + n)
+            ctx.op_qk_norm_rope_append(x[t:t + n], q[t:t + n], cache, dev(starts([n]), torch.int32), q_weight=w, k_weight=w, rot=angles,
+                                       interleaved=interleaved)
+        assert ctx.device_errors() == 0
+        got.append([a.view(torch.int16) for a in (q, k, v)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_coordinates_outside_their_table_are_reported(contexts):
     ctx = contexts["f32"]
     x = synth.normal(3, (3, 3 * 64))
