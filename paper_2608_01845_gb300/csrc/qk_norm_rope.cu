@@ -437,7 +437,8 @@ wdc_status launch(Ctx* c, NormArgs& a, bool pairs, cudaStream_t s) {
 }
 
 // What both forms check and take over.
-wdc_status take(Ctx* c, NormArgs& a, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n) {
+wdc_status take(Ctx* c, NormArgs& a, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n,
+                const wdc_rot_axes* axes) {
     if (!n) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: no wdc_head_norm");
     if (T < 0 || heads < 1 || kv < 1) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: T >= 0, heads and kv_heads >= 1 wanted");
     if (d != 64 && d != 128) return fail(c, WDC_ERR_UNSUPPORTED, "norm and rotation: head_dim must be 64 or 128");
@@ -450,7 +451,7 @@ wdc_status take(Ctx* c, NormArgs& a, const void* qkv, long long ld, int T, int h
     if (T > 0 && !qkv) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
     if (((uintptr_t)qkv | (uintptr_t)n->q_weight | (uintptr_t)n->k_weight | (uintptr_t)n->rot) & 15)
         return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: pointers must be 16-byte aligned");
-    if ((uintptr_t)n->positions & 3) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: positions must be 4-byte aligned");
+    if (!axes && ((uintptr_t)n->positions & 3)) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: positions must be 4-byte aligned");
     a.qkv = qkv; a.ld = ld; a.T = T; a.heads = heads; a.kv = kv;
     a.wq = n->q_weight; a.wk = n->k_weight; a.eps = n->eps;
     a.rot = n->rot_dim > 0 ? reinterpret_cast<const float2*>(n->rot) : nullptr;
@@ -473,11 +474,11 @@ wdc_status take_axes(Ctx* c, NormArgs& a, int d, const wdc_head_norm* n, const w
         if (x->pairs[i] == 0) continue;                        // (its table and coordinates are not looked at)
         if (x->rows[i] < 1) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: an axis' table needs rows >= 1");
         if (a.T > 0 && (!x->table[i] || !x->coords)) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
+        if ((uintptr_t)x->coords & 3) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: coords must be 4-byte aligned");
         if ((uintptr_t)x->table[i] & 7) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: an axis' table must be 8-byte aligned");
         a.axis_rot[i] = reinterpret_cast<const float2*>(x->table[i]);
         a.axis_rows[i] = x->rows[i];
     }
-    if ((uintptr_t)x->coords & 3) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: coords must be 4-byte aligned");
     if (pairs % 8) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: the axes' pairs must be a multiple of 8 in all");
     if (pairs == 0) return WDC_OK;                             // nothing is turned
     a.axes = x->axes;
@@ -491,7 +492,7 @@ wdc_status take_axes(Ctx* c, NormArgs& a, int d, const wdc_head_norm* n, const w
 wdc_status op_qk_norm_rope(Ctx* c, const void* qkv, long long ld, int T, int heads, int kv, int d, const wdc_head_norm* n,
                            const wdc_rot_axes* axes, void* q, void* k, void* vt, cudaStream_t s) {
     NormArgs a{};
-    if (wdc_status st = take(c, a, qkv, ld, T, heads, kv, d, n)) return st;
+    if (wdc_status st = take(c, a, qkv, ld, T, heads, kv, d, n, axes)) return st;
     if (wdc_status st = take_axes(c, a, d, n, axes)) return st;
     if (T == 0) return WDC_OK;
     if (!q || !k) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");
@@ -534,7 +535,7 @@ wdc_status op_qk_norm_rope_append(Ctx* c, const void* qkv, long long ld, int T, 
                                   cudaStream_t s) {
     NormArgs a{};
     if (wdc_status st = check_cache(c, p, &a.page_log2)) return st;
-    if (wdc_status st = take(c, a, qkv, ld, T, heads, p->kv_heads, p->head_dim, n)) return st;
+    if (wdc_status st = take(c, a, qkv, ld, T, heads, p->kv_heads, p->head_dim, n, axes)) return st;
     if (wdc_status st = take_axes(c, a, p->head_dim, n, axes)) return st;
     if (T == 0 || p->sequences == 0) return WDC_OK;
     if (!q || !q_start) return fail(c, WDC_ERR_INVALID_ARG, "norm and rotation: null pointer");

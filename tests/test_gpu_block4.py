@@ -890,6 +890,32 @@ def test_refusals_of_the_library(contexts):
     assert ctx.launches == before and ctx.device_errors() == 0
 
 
+def test_axes_look_at_nothing_else(contexts):
+    """With axes the norm's rot_positions, rot_dim and positions are not looked at, nor is what belongs to an axis
+    without pairs: whatever they hold, the call is taken and turns the heads as without them."""
+    ctx, L = contexts["bf16"], wdc.LIB
+    s = torch.cuda.current_stream().cuda_stream
+    x = dev(synth.normal(3, (5, 3 * 64)), torch.bfloat16)
+    tables, coords, axes = axes_case(3, 5, (4, 12), (7, 30))
+    outs = []
+    for positions, size, dim, skip in [(None, 0, 0, False), (x.data_ptr() + 2, -1, 7, False), (x.data_ptr() + 1, 3, 16, True)]:
+        a = wdc.RotAxesC(2, coords=axes.c.coords)
+        for i in range(2):
+            a.table[i], a.rows[i], a.pairs[i] = axes.c.table[i], axes.c.rows[i], axes.c.pairs[i]
+        q, k = torch.zeros(1, 5, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 5, 64, dtype=torch.bfloat16, device="cuda")
+        if skip:                                           # no axis has pairs: no coordinates either
+            a.coords = x.data_ptr() + 2
+            for i in range(2):
+                a.table[i], a.rows[i], a.pairs[i] = x.data_ptr() + 1, -5, 0
+        n = wdc.HeadNorm(None, None, 1e-6, None, size, dim, 1, positions)
+        assert L.wdc_op_qk_norm_rope_axes(ctx._h, x.data_ptr(), 192, 5, 1, 1, 64, n, a, q.data_ptr(), k.data_ptr(), None, s) == 0
+        outs.append((q, k))
+    plain = [torch.zeros(1, 5, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ctx.op_qk_norm_rope(x, *plain)
+    assert all(torch.equal(u, v) for u, v in zip(outs[0], outs[1])) and all(torch.equal(u, v) for u, v in zip(outs[2], plain))
+    assert not torch.equal(outs[0][0], plain[0]) and ctx.device_errors() == 0
+
+
 def test_refusals_of_places(contexts):
     """A row is read by one block while another writes its own: an output lies on an input row for row or not at
     all, and a result in few bits on neither the inputs nor the sum."""
