@@ -695,6 +695,12 @@ wdc_status wdc_op_gated_fp4(wdc_ctx* ctx, const wdc_fp4* A, const wdc_fp4* W_gat
                             const float* gate_bias, const float* up_bias, void* C, int M, int N, int K, int gelu,
                             wdc_stream stream);
 
+/* How the two take a shape (a diagnostic: the kernel is chosen from the shape): plan[0] rows of A a tile, 16 to
+ * 128, or 256 of the kernel of CTA pairs; plan[1] CTAs that share a tile's K (0: the pairs); plan[2] of the pairs'
+ * tiles those that are split over K, plan[3] the parts of each (0: none).  WDC_ERR_INVALID_ARG unless it is
+ * one that they take, with rows. */
+wdc_status wdc_fp4_plan(wdc_ctx* ctx, int M, int N, int K, int gated, int* plan);
+
 /* The residual's sum, its norm and its modulation, rows [M, D] in the model dtype:
  *   r = x + gate * delta                      (x alone without delta; gate NULL = 1)
  *   y = r / sqrt(mean(r^2) + eps)             (center: (r - mean r) / sqrt(var r + eps))

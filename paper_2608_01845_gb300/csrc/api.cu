@@ -1143,6 +1143,11 @@ wdc_status wdc_op_gemm_fp4(wdc_ctx* h, const wdc_fp4* A, const wdc_fp4* W, const
     return chunk_op(h, [&](Ctx* c) { return op_gemm_fp4(c, A, W, bias, C, M, N, K, gelu, res, gate, (cudaStream_t)stream); });
 }
 
+wdc_status wdc_fp4_plan(wdc_ctx* h, int M, int N, int K, int gated, int* plan) {
+    if (!plan) return WDC_ERR_INVALID_ARG;
+    return chunk_op(h, [&](Ctx* c) { return fp4_plan(c, M, N, K, gated != 0, plan); });
+}
+
 wdc_status wdc_op_gated_fp4(wdc_ctx* h, const wdc_fp4* A, const wdc_fp4* W_gate, const wdc_fp4* W_up, const float* gate_bias,
                             const float* up_bias, void* C, int M, int N, int K, int gelu, wdc_stream stream) {
     return chunk_op(h, [&](Ctx* c) {

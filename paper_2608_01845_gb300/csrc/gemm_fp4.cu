@@ -438,6 +438,24 @@ Gemm4Args args(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const float* bias, vo
 
 }  // namespace
 
+wdc_status fp4_plan(Ctx* c, int M, int N, int K, bool gated, int* plan) {
+    if (M <= 0 || N <= 0 || K <= 0 || N > kMaxWidth4 || K > kMaxWidth4 || M > kMaxRows4 || N % 8 || K % 64)
+        return fail(c, WDC_ERR_INVALID_ARG, "fp4 plan: not a shape of the products");
+    const Choice ch = choose(c, M, N, K, gated);
+    plan[0] = ch.bn;
+    plan[1] = ch.split;
+    plan[2] = plan[3] = 0;
+    if (ch.split > 0) return WDC_OK;
+    Gemm4Args g{};
+    const uint8_t none = 0;
+    g.M = M; g.N = N; g.K = K;
+    g.U = gated ? &none : nullptr;
+    if (!plan_gemm4_pair(c, g)) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 plan: the pair kernel cannot take it");
+    plan[2] = g.parts > 1 ? g.tail : 0;
+    plan[3] = g.parts > 1 ? g.parts : 0;
+    return WDC_OK;
+}
+
 wdc_status op_gemm_fp4(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const float* bias, void* C, int M, int N, int K, int gelu,
                        const void* res, const float* gate, cudaStream_t s) {
     bool none;

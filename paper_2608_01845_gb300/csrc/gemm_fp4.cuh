@@ -43,6 +43,7 @@ inline bool encode_scales(CUtensorMap* m, const void* scale, int rows, int piece
 __device__ __forceinline__ float silu_f(float x) { return __fdividef(x, 1.0f + __expf(-x)); }
 
 // gemm_fp4_pair.cu
+bool plan_gemm4_pair(const Ctx* c, Gemm4Args& g);   // its tiles (from M, N, K and whether there is a U); false: it cannot
 wdc_status launch_gemm4_pair(Ctx* c, const Gemm4Args& g, cudaStream_t s);
 
 }  // namespace wdc

@@ -528,10 +528,11 @@ int tail_parts(int tail, int pairs, int kb) {
     return best;
 }
 
+// Lets the kernels take their shared memory; false: their registers do not allow the warpgroups' split.
 template <typename T>
-wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
+bool ready(const Ctx* c) {
     static PerDevice<bool> fits;
-    const bool regs_ok = fits.get(c->device, [](bool& ok) {
+    return fits.get(c->device, [](bool& ok) {
         bool smem = ok = true;
         for (int f = 0; f < 6; ++f) {
             const PairKernel k = pair_kernel<T>(f);
@@ -545,16 +546,31 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
         cudaGetLastError();
         return smem && ok;
     });
-    if (!regs_ok) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM kernel's register allocation is below its warpgroup split");
+}
+
+// The tiles, and which of them are split over K; false: too many.
+bool plan(const Ctx* c, PairKernel k, Gemm4Args& g, int* pairs) {
+    g.m_tiles = (g.M - 1) / 256 + 1;
+    g.n_tiles = (g.N - 1) / (g.U ? 128 : 256) + 1;
+    g.kb = (g.K - 1) / kTileK4 + 1;
+    const long long tiles = (long long)g.m_tiles * g.n_tiles;
+    if (tiles > 0x3fffffffll) return false;
+    *pairs = resident_pairs(c, k);
+    g.tail = (int)(tiles % *pairs);
+    g.whole = (int)(tiles - g.tail);
+    g.parts = g.whole > 0 ? tail_parts(g.tail, *pairs, g.kb) : 1;
+    if (g.parts > c->fp4_parts / (g.tail > 0 ? g.tail : 1)) g.parts = 1;
+    return true;
+}
+
+template <typename T>
+wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
+    if (!ready<T>(c)) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM kernel's register allocation is below its warpgroup split");
     const bool gated = g.U != nullptr;
     const PairKernel k = pair_kernel<T>(gated ? (g.gelu ? kGeluGated : kSiluGated)
                                               : (g.res ? (g.gelu ? kGeluResid : kResid) : (g.gelu ? kGelu : kStore)));
-    const int bn = gated ? 128 : 256;
-    g.m_tiles = (g.M - 1) / 256 + 1;
-    g.n_tiles = (g.N - 1) / bn + 1;
-    g.kb = (g.K - 1) / kTileK4 + 1;
-    const long long tiles = (long long)g.m_tiles * g.n_tiles;
-    if (tiles > 0x3fffffffll) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM: more than 2^30 tiles");
+    int pairs;
+    if (!plan(c, k, g, &pairs)) return fail(c, WDC_ERR_UNSUPPORTED, "fp4 GEMM: more than 2^30 tiles");
     // raster groups whose rows of W (at most about 40 MB) stay in L2 while A
     // streams past them once a group
     int gn = (int)(40.0e6 / (256.0 * g.K * 0.5625));
@@ -571,11 +587,6 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
         !encode_tmap_2d(&tc, g.out, N, M, ldc, 128 / sizeof(T), 32, &why, kOut) ||
         !encode_tmap_2d(&tr, g.res ? g.res : g.out, N, M, ldc, 128 / sizeof(T), 32, &why, kOut))
         return fail(c, WDC_ERR_CUDA, why);
-    const int pairs = resident_pairs(c, k);
-    g.tail = (int)(tiles % pairs);
-    g.whole = (int)(tiles - g.tail);
-    g.parts = g.whole > 0 ? tail_parts(g.tail, pairs, g.kb) : 1;
-    if (g.parts > c->fp4_parts / (g.tail > 0 ? g.tail : 1)) g.parts = 1;
     g.work = c->fp4_work;
     g.counters = c->fp4_counters;
     SplitOrder order(c, g.parts > 1, s);
@@ -592,6 +603,13 @@ wdc_status launch(Ctx* c, Gemm4Args g, cudaStream_t s) {
 }
 
 }  // namespace
+
+bool plan_gemm4_pair(const Ctx* c, Gemm4Args& g) {
+    int pairs;
+    const bool bf16 = c->cfg.dtype == WDC_BF16;
+    return (bf16 ? ready<__nv_bfloat16>(c) : ready<float>(c)) &&
+           plan(c, bf16 ? pair_kernel<__nv_bfloat16>(kStore) : pair_kernel<float>(kStore), g, &pairs);
+}
 
 wdc_status launch_gemm4_pair(Ctx* c, const Gemm4Args& g, cudaStream_t s) {
     return c->cfg.dtype == WDC_BF16 ? launch<__nv_bfloat16>(c, g, s) : launch<float>(c, g, s);

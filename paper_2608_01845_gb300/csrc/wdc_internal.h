@@ -374,6 +374,7 @@ wdc_status op_gemm_fp4(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const float* 
                        const void* res, const float* gate, cudaStream_t s);
 wdc_status op_gated_fp4(Ctx* c, const wdc_fp4* A, const wdc_fp4* W, const wdc_fp4* U, const float* gate_bias,
                         const float* up_bias, void* C, int M, int N, int K, int gelu, cudaStream_t s);
+wdc_status fp4_plan(Ctx* c, int M, int N, int K, bool gated, int* plan);
 wdc_status op_add_norm(Ctx* c, const wdc_add_norm* n, int M, int D, cudaStream_t s);
 // Checks an e2m1 matrix' pointers.
 wdc_status check_fp4(Ctx* c, const wdc_fp4* q);

@@ -199,6 +199,7 @@ def _load():
         "wdc_op_quantize_fp4": (I, [P, P, ctypes.c_longlong, ctypes.POINTER(Fp4C), I, I, P]),
         "wdc_op_dequantize_fp4": (I, [P, ctypes.POINTER(Fp4C), P, ctypes.c_longlong, I, I, P]),
         "wdc_op_gemm_fp4": (I, [P, ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), P, P, I, I, I, I, P, P, P]),
+        "wdc_fp4_plan": (I, [P, I, I, I, I, ctypes.POINTER(I)]),
         "wdc_op_gated_fp4": (I, [P, ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), ctypes.POINTER(Fp4C), P, P, P, I, I, I, I,
                                  P]),
         "wdc_observe_noalloc": (I, [ctypes.POINTER(P), I, ctypes.POINTER(D), P, P, P, S, ctypes.c_uint32, P]),
@@ -803,6 +804,13 @@ class Context:
         self._check(LIB.wdc_op_gated_fp4(self._h, self._fp4(what, "A", A, M, K), self._fp4(what, "W_gate", W_gate, N, K),
                                          self._fp4(what, "W_up", W_up, N, K), _address(gate_bias), _address(up_bias),
                                          C.data_ptr(), M, N, K, int(gelu), self._op_stream(stream)), what)
+
+    def fp4_plan(self, M, N, K, gated=False):
+        """wdc_fp4_plan: (rows of A a tile, CTAs over a tile's K, tiles split over K, parts of each) of a product."""
+        _sizes("fp4_plan", M, N, K)
+        plan = (ctypes.c_int * 4)()
+        self._check(LIB.wdc_fp4_plan(self._h, M, N, K, int(gated), plan), "fp4_plan")
+        return tuple(plan)
 
     def op_add_norm(self, x, out, delta=None, gate=None, total=None, weight=None, weight_offset=0.0, shift=None,
                     center=False, eps=1e-6, rows_per_set=0, scale=None, stream=None):

@@ -312,6 +312,116 @@ def test_split_sums_repeat_themselves(contexts):
     assert all(torch.equal(outs[0], c) for c in outs[1:]) and contexts["f32"].device_errors() == 0
 
 
+def planned(ctx, want, M, N, K, gated=False):
+    """A test for a kernel's path has reached it (the choices are those for 152 SMs)."""
+    if torch.cuda.get_device_properties(0).multi_processor_count == 152:
+        got = ctx.fp4_plan(M, N, K, gated)
+        assert all(w is None or w == g for w, g in zip(want, got)), got
+
+
+class Drawn:
+    """Rows drawn from 48 different ones, each with a scale of its own: long products that fp64 is quick to give."""
+
+    def __init__(self, seed, rows, K, std=1.0):
+        r = np.random.default_rng(seed)
+        code, s, row = block4.quantize(synth.bf16_round(synth.normal(seed, (48, K), std)))
+        self.pick = r.integers(0, 48, rows)
+        self.row = (row[self.pick] * (0.5 + r.random(rows))).astype(np.float32)
+        self.base = code * np.asarray(s, np.float64).repeat(16, 1)
+        self.m = wdc.Fp4Matrix(torch.from_numpy(block4.pack(code)).cuda()[torch.from_numpy(self.pick).cuda()].contiguous(),
+                               dev(block4.to_pieces(s[self.pick], np.nan), F8), dev(self.row))
+
+    def product(self, w):
+        """(A W^T, of the magnitudes)"""
+        scales = self.row[:, None].astype(np.float64) * w.row[None]
+        return [(f(self.base) @ f(w.base).T)[self.pick][:, w.pick] * scales for f in (np.asarray, np.abs)]
+
+
+@functools.lru_cache(3)
+def drawn_case(M, N, K, gated):
+    A, W = Drawn(31, M, K), Drawn(32, N, K, K ** -0.5)
+    U = Drawn(33, N, K, K ** -0.5) if gated else None
+    return A, W, U, A.product(W), A.product(U) if gated else None
+
+
+# (a round of 76 tiles and some behind it that are split over K in so many parts; M, N and K ragged)
+SPLITS = [(1300, 3592, 8256, 14, 3), (1250, 3976, 8256, 4, 3), (1282, 4616, 16448, 38, 2)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["store", "bias", "gelu", "resid", "resid_gelu", "gateless"])
+@pytest.mark.parametrize("M,N,K,tail,parts", SPLITS)
+def test_split_epilogues(contexts, M, N, K, tail, parts, mode, kind):
+    """test_gemm_epilogues where the last tiles' sums are joined from parts, the residual in place fetched behind that."""
+    ctx = contexts[kind]
+    planned(ctx, (256, 0, tail, parts), M, N, K)
+    A, W, _, (y, mag), _ = drawn_case(M, N, K, False)
+    b, g = synth.normal(3, (N,), 0.5), synth.normal(5, (N,))
+    r = synth.bf16_round(synth.normal(4, (M, N)))
+    err, kw = product_bound(y, mag, K), {}
+    if mode != "store":
+        y, kw = y + b, dict(bias=dev(b))
+        err = err + 2.0 ** -22 * np.abs(y)
+    if "gelu" in mode:
+        y, err, kw["gelu"] = dit.gelu_tanh(y), 1.13 * err + 2.0 ** -18 * np.abs(y) + 1e-6, True
+    buf = torch.full((M + 1, N), 7.0, dtype=DTYPES[kind], device="cuda")
+    C = buf[:M]
+    if mode in ("resid", "resid_gelu", "gateless"):
+        C.copy_(dev(r))
+        kw["res"] = C
+        if mode != "gateless":
+            y, err, kw["gate"] = g * y, np.abs(g) * err + 2.0 ** -22 * np.abs(g * y), dev(g)
+        y = r + y
+    ctx.op_gemm_fp4(A.m, W.m, C, **kw)
+    assert (np.abs(host(C) - y) <= err + HALF[kind] * np.abs(y) + 2.0 ** -22 * np.abs(y)).all()
+    assert bool((buf[M:] == 7.0).all()) and ctx.device_errors() == 0
+
+
+GATED_SPLITS = [(1100, 2184, 8256, 14, 3), (1282, 2312, 16448, 38, 2), (1250, 1992, 16448, 4, 8)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("M,N,K,tail,parts", GATED_SPLITS)
+def test_split_gated(contexts, M, N, K, tail, parts, bias, gelu, kind):
+    """test_gated where both sums of the last tiles are joined from parts."""
+    ctx = contexts[kind]
+    planned(ctx, (256, 0, tail, parts), M, N, K, True)
+    A, W, U, (g, gmag), (u, umag) = drawn_case(M, N, K, True)
+    ge, ue, kw = product_bound(g, gmag, K), product_bound(u, umag, K), dict(gelu=gelu)
+    if bias:
+        bg, bu = synth.normal(3, (N,), 0.5), synth.normal(5, (N,), 0.5)
+        g, u, kw = g + bg, u + bu, dict(kw, gate_bias=dev(bg), up_bias=dev(bu))
+        ge, ue = ge + 2.0 ** -22 * np.abs(g), ue + 2.0 ** -22 * np.abs(u)
+    want, f = block4.gated(g, u, gelu), block4.gated(g, 1.0, gelu)
+    fe = 1.13 * ge + 2.0 ** -18 * np.abs(f) + 1e-6
+    buf = torch.full((M + 1, N), 7.0, dtype=DTYPES[kind], device="cuda")
+    ctx.op_gated_fp4(A.m, W.m, U.m, buf[:M], **kw)
+    err = fe * np.abs(u) + np.abs(f) * ue + fe * ue + 2.0 ** -22 * np.abs(want) + HALF[kind] * np.abs(want)
+    assert (np.abs(host(buf[:M]) - want) <= err).all()
+    assert bool((buf[M:] == 7.0).all()) and ctx.device_errors() == 0
+
+
+@pytest.mark.parametrize("M,N,K,gated,want", [
+    (3, 264, 576, False, (16, 1)), (3, 2056, 4160, False, (16, 4)), (2, 8200, 8256, False, (16, 2)), (1, 8, 4160, False, (32, 8)),
+    (17, 8, 64, False, (32, 1)), (17, 8200, 8256, False, (32, 2)), (20, 2056, 4160, False, (32, 4)), (33, 8, 4160, False, (64, 8)),
+    (50, 2056, 4160, False, (64, 4)), (60, 8200, 8256, False, (64, 2)), (100, 1544, 4160, False, (128, 1)),
+    (65, 8200, 16448, False, (128, 2)), (90, 2056, 8256, False, (128, 4)), (65, 8, 8256, False, (128, 8)),
+    (40, 392, 8256, True, (64, 8)), (100, 1544, 4160, True, (128, 8)), (300, 1032, 16448, True, (128, 4)), (17, 8, 64, True, (32, 1)),
+    (1030, 2056, 1088, False, (256, 0, 0, 0)), (2309, 3080, 576, True, (256, 0, 0, 0)), (*SPLIT, False, (256, 0, 14, 3))])
+def test_the_shapes_above_take_every_way(contexts, M, N, K, gated, want):
+    """Tokens a tile and CTAs a tile's K, the pairs and their split tiles: what the tests of the products reach."""
+    for ctx in contexts.values():
+        planned(ctx, want, M, N, K, gated)
+
+
+def test_plans_of_no_products(contexts):
+    for bad in [(0, 8, 64), (4, 0, 64), (4, 8, 0), (4, 4, 64), (4, 8, 32), (4, 8, 2 ** 31 - 64), (-1, 8, 64)]:
+        with pytest.raises((wdc.WdcError, ValueError)):
+            contexts["bf16"].fp4_plan(*bad)
+
+
 # ---------------------------------------------------------------- residual and norm
 def norm_case(M, D, kind, add, per, seed=91):
     sets = -(-M // per) if per else 1
