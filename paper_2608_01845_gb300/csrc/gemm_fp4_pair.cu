@@ -25,7 +25,10 @@
 // into registers 175, the arrival at the issuer; the first copies are under way by then: gated
 // 1576 x 10240 x 4096 52.5 -> 51.6).  Tiles of 192 columns with
 // room for two left the scales 2.7 stages, and waiting for their columns cost more: 159 us.
-// Parts of the last tiles before the whole ones: 1350 x 4096 x 16384 44.6 -> 36 us.
+// Parts of the last tiles before the whole ones: 1350 x 4096 x 16384 44.6 -> 36 us.  K is split behind a
+// whole round only, and where the tiles behind it are at most half the pairs: 1024 x 2560 x 16384 (40
+// tiles) 25 us, for 11 of operations.  The 128 sums a thread leave 40 of the launch's registers for the
+// rest of the epilogue: nine of the twelve forms spill 20 to 32 bytes.
 #include "gemm_fp4.cuh"
 #include "pair_epilogue.cuh"
 

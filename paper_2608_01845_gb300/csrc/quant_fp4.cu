@@ -6,9 +6,9 @@
 // The row's scale needs the whole row before the first code: a row stays in the
 // registers of its warps between the two, so x is read once.  Bound by memory (2.56
 // bytes an element for bf16, 4.56 for fp32) where rows are fp32: 4276 x 12288 to codes 44
-// us (5.5 TB/s; 48 with 4 pieces of 8 columns a thread) and back 38 (6.3).  bf16 rows are bound by the conversions, about 130
-// instructions for 8 columns with the row's: 17776 x 4096 to codes 49 us (3.8 TB/s), back 29
-// (6.4); with 4 pieces of 8 columns a thread instead of 2, a row of fewer threads, 54 ->
+// us (5.5 TB/s; 48 with 4 pieces of 8 columns a thread) and back 38 (6.3).  bf16 rows are bound by their instructions, about
+// 130 for 8 columns, 50 of them the conversions (two lanes work out each scale; 68% of the issue slots):
+// 17776 x 4096 to codes 45 to 49 us (3.8 to 4.1 TB/s), back 29 (6.4); with 4 pieces of 8 columns a thread instead of 2, a row of fewer threads, 54 ->
 // 49.  4 x 5120: 1.8 us either way, a launch.
 #include <type_traits>
 
